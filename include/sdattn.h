@@ -18,6 +18,7 @@
  * Conventions shared by every entry point
  * ---------------------------------------
  * Memory.    Every tensor argument is a device pointer owned by the caller.
+ *            (but `pairs` of sdattn_norm_rotate, as said there).
  *            The library allocates nothing, frees nothing and keeps no state
  *            beyond a thread-local copy of the last HIP error.
  * Layout.    Dense row-major, innermost dimension last, no strides.
@@ -169,6 +170,105 @@ typedef enum {
 int sdattn_linear(const void *x, const void *w, const void *bias, void *y, int B, int L, int K,
                   int N, int H, sdattn_layout x_layout, sdattn_layout y_layout, sdattn_dtype dtype,
                   void *stream);
+
+/*
+ * sdattn_linear with low-rank adapters of many requests beside the shared
+ * weights.  Batch item b, whose adapter is i = ids[b], gets
+ *   y[b, l, :] = w x + bias + scales[i] * up_i (down_i x),     x = x[b, l, :]
+ * and an item whose ids[b] lies outside [0, A) what sdattn_linear gives.
+ *
+ *   down   [A, R, K] of `dtype`; up [A, N, R] of `dtype`
+ *   ids    [B] 32-bit integers; scales [A] fp32, or NULL (for 1)
+ *   workspace: at least sdattn_linear_adapters_workspace(B, L, R) bytes, owned by
+ *   the caller; it receives scales[i] * down_i x, rounded to `dtype`
+ *
+ * The other arguments are sdattn_linear's.  Adapters of different ranks share a
+ * call with the smaller ones' missing ranks as zeros in down (rows) and up
+ * (columns).  An adapter's values reach the rows of its own requests alone.  Two
+ * launches on `stream`.
+ *
+ * Requirements: sdattn_linear's; 1 <= R <= 65536; A >= 1; down, up and workspace
+ * 16-byte aligned, ids and scales 4-byte; y and the workspace must not overlap each
+ * other or an input.  Fastest when R % 8 == 0.
+ */
+long long sdattn_linear_adapters_workspace(int B, int L, int R);
+int sdattn_linear_adapters(const void *x, const void *w, const void *bias, const void *down,
+                           const void *up, const int *ids, const float *scales, void *y,
+                           void *workspace, long long workspace_bytes, int B, int L, int K, int N,
+                           int R, int A, int H, sdattn_layout x_layout, sdattn_layout y_layout,
+                           sdattn_dtype dtype, void *stream);
+
+/*
+ * Norms of queries and keys for each head, and the rotation of each head's pairs
+ * by the tokens' positions on several axes (time, height and width of a video, the
+ * sides of an image), in one pass.  Of a head's row x of D values
+ *   y = x / sqrt(mean_d x_d^2 + eps) * gamma     (SDATTN_NORM_RMS; y = x with SDATTN_NORM_NONE)
+ *   (a, b) -> (a cos t - b sin t, b cos t + a sin t)
+ *   for pair p < P:  t = pos[b, l, axis of p] * freqs[p]
+ * The first pairs[0] pairs turn with the first axis, the next pairs[1] with the
+ * second, ...; P is their sum.  The pairs are values (2p, 2p + 1) with
+ * SDATTN_PAIR_ADJACENT, (p, P + p) with SDATTN_PAIR_HALVES; values from 2P on are
+ * not turned.  The angles are reduced in 64 bits, the rest is fp32, rounded once.
+ *
+ *   q, k      token rows of H heads of D values in `x_layout`, `dtype` (fp16 or bf16);
+ *             k and ko NULL: q alone
+ *   qo, ko    the same in `y_layout`; with equal layouts qo may be q, and ko k
+ *   gamma_q, gamma_k  [D] of `dtype` or NULL (for 1)
+ *   pos       [pos_batches, L, axes] 32-bit integers, pos_batches = B, or 1 where all
+ *             batch items have the same positions; freqs [P] fp32
+ *   pairs     `axes` integers in HOST memory, read during the call
+ *
+ * Requirements: D % 8 == 0, D <= 256; 0 <= axes <= 4 (with none, pos, freqs and pairs
+ * are not looked at); pairs >= 1, P <= D / 2; eps finite and >= 0; q, k, qo, ko 16-byte
+ * aligned, gammas 8-byte, pos and freqs 4-byte; no output may overlap another
+ * argument otherwise.
+ */
+typedef enum {
+    SDATTN_NORM_NONE = 0,
+    SDATTN_NORM_RMS = 1
+} sdattn_norm;
+typedef enum {
+    SDATTN_PAIR_ADJACENT = 0,
+    SDATTN_PAIR_HALVES = 1
+} sdattn_pairing;
+int sdattn_norm_rotate(const void *q, const void *k, const void *gamma_q, const void *gamma_k,
+                       const int *pos, const float *freqs, void *qo, void *ko, int B, int H, int L,
+                       int D, int axes, const int *pairs, int pos_batches, sdattn_norm norm,
+                       float eps, sdattn_pairing pairing, sdattn_layout x_layout,
+                       sdattn_layout y_layout, sdattn_dtype dtype, void *stream);
+
+/*
+ * Attention over a part of the keys, for sequences where all pairs are too many.
+ * Keys go in blocks of SDATTN_SPARSE_BLOCK, queries in blocks of `qblock` (64 or
+ * 128), the last ones shorter.  A mask says which key blocks a query block reads:
+ *   mask  [B, H, ceil(Lq / qblock), ceil(NB / 64)] 64-bit words, NB = ceil(Lk / 64):
+ *         bit j % 64 of word j / 64 stands for key block j; bits past NB are ignored
+ * Masks can be written by hand, or joined with | to ones of
+ *
+ * sdattn_block_means: means [B, H, ceil(L / 64), D] fp32 of the blocks of x [B, H, L, D];
+ *
+ * sdattn_select_blocks: sets for every query block i the bits of the `keep` key
+ * blocks j with the largest scores s_ij = mq_i . means_j, where mq_i is the mean of the
+ * block's queries, rounded to fp32 like the keys'; of equal scores the lower j, and
+ * all blocks where keep >= NB.  Sums and products are held in 64 bits.  means is what
+ * sdattn_block_means gives for the keys, once for keys that stay.
+ *
+ * sdattn_sparse_forward: out = softmax(scale q k^T) v over the keys of the named
+ * blocks; zeros where none is named.  Keys and values of other blocks are not read.
+ *
+ * Requirements: x, q, k, v, out and means 16-byte aligned, mask 8-byte; sizes >= 1,
+ * L, Lq and Lk at most 2^30; 8 <= D <= 256 with D % 8 == 0 for the first two (at most
+ * 16384 key blocks for the second), 32 <= D <= 160 with D % 8 == 0 and D != 152 for
+ * sdattn_sparse_forward; finite scale; fp16 or bf16; no output may overlap an input.
+ */
+#define SDATTN_SPARSE_BLOCK 64
+int sdattn_block_means(const void *x, float *means, int B, int H, int L, int D, sdattn_dtype dtype,
+                       void *stream);
+int sdattn_select_blocks(const void *q, const float *means, void *mask, int B, int H, int Lq, int NB,
+                         int D, int qblock, int keep, sdattn_dtype dtype, void *stream);
+int sdattn_sparse_forward(const void *q, const void *k, const void *v, const void *mask, void *out,
+                          int B, int H, int Lq, int Lk, int D, int qblock, float scale,
+                          sdattn_dtype dtype, void *stream);
 
 /*
  * SD's attention block around Eq. 3 (multi-head attention of latent tokens x

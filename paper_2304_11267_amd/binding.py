@@ -7,9 +7,10 @@ arithmetic of the attention happens here.  The library is loaded from the
 package directory on first use; a missing library raises, there is no other
 code path.
 
-Ten functions are marshalled by the extension module _marshal (csrc/marshal.cpp):
+Fifteen functions are marshalled by the extension module _marshal (csrc/marshal.cpp):
 forward, forward_ex, softmax_rows, logits, softmax_pv, attention_block,
-attention_block_kv, group_norm, geglu and conv3x3, in 3 us a call where Python
+attention_block_kv, group_norm, geglu, conv3x3, linear_adapters, norm_rotate,
+block_means, select_blocks and sparse_forward, in 3 us a call where Python
 and ctypes take 10, as long as two of the smaller kernels.  linear,
 attention_block_static, project_kv and winograd_weights go through ctypes below,
 as does what the module does not take (it answers None); errors are raised there.
@@ -41,10 +42,18 @@ EXPORTS = ("sdattn_forward", "sdattn_forward_ex", "sdattn_softmax_rows", "sdattn
            "sdattn_attention_block_kv",
            "sdattn_group_norm", "sdattn_geglu", "sdattn_winograd_weights_elems",
            "sdattn_winograd_weights", "sdattn_conv3x3_workspace", "sdattn_conv3x3",
+           "sdattn_linear_adapters_workspace", "sdattn_linear_adapters", "sdattn_norm_rotate",
+           "sdattn_block_means", "sdattn_select_blocks", "sdattn_sparse_forward",
            "sdattn_status_str", "sdattn_last_hip_error", "sdattn_version")
 
 LAYOUT_ROWS = 0
 LAYOUT_HEADS = 1
+
+NORM_NONE = 0
+NORM_RMS = 1
+PAIR_ADJACENT = 0
+PAIR_HALVES = 1
+SPARSE_BLOCK = 64
 
 _lib = None
 _native = None   # the extension module; None: not loaded (or not built)
@@ -110,6 +119,18 @@ def load_library():
     lib.sdattn_conv3x3_workspace.restype = i64
     lib.sdattn_conv3x3.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, i32, i32, vp]
     lib.sdattn_conv3x3.restype = i32
+    lib.sdattn_linear_adapters_workspace.argtypes = [i32, i32, i32]
+    lib.sdattn_linear_adapters_workspace.restype = i64
+    lib.sdattn_linear_adapters.argtypes = [vp] * 9 + [i64] + [i32] * 10 + [vp]
+    lib.sdattn_linear_adapters.restype = i32
+    lib.sdattn_norm_rotate.argtypes = [vp] * 8 + [i32] * 5 + [vp, i32, i32, f32, i32, i32, i32, i32, vp]
+    lib.sdattn_norm_rotate.restype = i32
+    lib.sdattn_block_means.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp]
+    lib.sdattn_block_means.restype = i32
+    lib.sdattn_select_blocks.argtypes = [vp, vp, vp] + [i32] * 8 + [vp]
+    lib.sdattn_select_blocks.restype = i32
+    lib.sdattn_sparse_forward.argtypes = [vp] * 5 + [i32] * 6 + [f32, i32, vp]
+    lib.sdattn_sparse_forward.restype = i32
     lib.sdattn_status_str.argtypes = [i32]
     lib.sdattn_status_str.restype = ctypes.c_char_p
     lib.sdattn_last_hip_error.argtypes = []
@@ -194,6 +215,15 @@ def _expect(t, shape, like, name):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if like is not None and t.dtype != like.dtype:
         raise TypeError(f"{name} is {t.dtype}, expected {like.dtype}")
+
+
+def _here(t, name):
+    """_dev for a tensor that has to live on the current device, whose stream the call takes."""
+    import torch
+    p = _dev(t, name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return p
 
 
 def forward(q, k, v, out, scale: float, stream=None):
@@ -466,3 +496,180 @@ def conv3x3(x, u, y, workspace, bias=None, stream=None):
         B, Ci, Co, H, W, _dtype_code(x), _stream(stream))
     _check("sdattn_conv3x3", status)
     return y
+
+
+def linear_adapters_workspace(B, L, R):
+    """Bytes of workspace sdattn_linear_adapters needs."""
+    return int(load_library().sdattn_linear_adapters_workspace(B, L, R))
+
+
+def linear_adapters(x, w, y, down, up, ids, workspace, scales=None, bias=None, heads=1, x_layout=LAYOUT_ROWS,
+                    y_layout=LAYOUT_ROWS, stream=None):
+    """linear with a low-rank adapter for each batch item: y[b] also gets
+    scales[i] * up[i] down[i] x[b], i = ids[b] (none outside [0, A)).  down [A, R, K],
+    up [A, N, R], ids [B] int32, scales [A] fp32 or None; workspace of at least
+    linear_adapters_workspace(B, L, R) bytes."""
+    if _native and _done("sdattn_linear_adapters", _native.linear_adapters(
+            _fn["sdattn_linear_adapters"], x, w, y, down, up, ids, workspace, scales, bias, heads, x_layout, y_layout,
+            stream)):
+        return y
+    import torch
+    if x_layout == LAYOUT_HEADS:
+        B, H, L, hw = x.shape
+        K = H * hw
+        if H != heads:
+            raise ValueError("x's head count differs from heads")
+    else:
+        B, L, K = x.shape
+    N = w.shape[0]
+    A, R = down.shape[:2]
+    _expect(w, (N, K), x, "w")
+    _expect(down, (A, R, K), x, "down")
+    _expect(up, (A, N, R), x, "up")
+    _expect(ids, (B,), None, "ids")
+    if ids.dtype != torch.int32:
+        raise TypeError(f"ids is {ids.dtype}, expected torch.int32")
+    if scales is not None:
+        _expect(scales, (A,), None, "scales")
+        if scales.dtype != torch.float32:
+            raise TypeError(f"scales is {scales.dtype}, expected torch.float32")
+    if bias is not None:
+        _expect(bias, (N,), x, "bias")
+    if y_layout == LAYOUT_HEADS:
+        if heads < 1 or N % heads:
+            raise ValueError("heads must divide the output channels")
+        _expect(y, (B, heads, L, N // heads), x, "y")
+    else:
+        _expect(y, (B, L, N), x, "y")
+    status = load_library().sdattn_linear_adapters(
+        _here(x, "x"), _here(w, "w"), _here(bias, "bias") if bias is not None else None, _here(down, "down"),
+        _here(up, "up"), _here(ids, "ids"), _here(scales, "scales") if scales is not None else None, _here(y, "y"),
+        _here(workspace, "workspace"), workspace.numel() * workspace.element_size(), B, L, K, N, R, A, heads, x_layout,
+        y_layout, _dtype_code(x), _stream(stream))
+    _check("sdattn_linear_adapters", status)
+    return y
+
+
+def norm_rotate(q, qo, heads, k=None, ko=None, gamma_q=None, gamma_k=None, pos=None, freqs=None, pairs=(),
+                norm=NORM_RMS, eps=1e-6, pairing=PAIR_ADJACENT, x_layout=LAYOUT_HEADS, y_layout=LAYOUT_HEADS,
+                stream=None):
+    """Norms of each head of q (and k) and the rotation of its pairs by pos * freqs, into
+    qo (and ko), in rows layout [B, L, H*D] or heads layout [B, H, L, D].  pos int32
+    [B or 1, L, axes]; pairs: how many pairs turn with each axis; freqs fp32 [sum(pairs)];
+    gammas [D] or None.  Returns qo, or (qo, ko)."""
+    result = qo if k is None else (qo, ko)
+    if _native and _done("sdattn_norm_rotate", _native.norm_rotate(
+            _fn["sdattn_norm_rotate"], q, qo, heads, k, ko, gamma_q, gamma_k, pos, freqs, pairs, norm, eps, pairing,
+            x_layout, y_layout, stream)):
+        return result
+    import torch
+    if x_layout == LAYOUT_HEADS:
+        B, H, L, D = q.shape
+        if H != heads:
+            raise ValueError("q's head count differs from heads")
+    else:
+        B, L, C = q.shape
+        if heads < 1 or C % heads:
+            raise ValueError("heads must divide the channels")
+        H, D = heads, C // heads
+    into = (B, H, L, D) if y_layout == LAYOUT_HEADS else (B, L, H * D)
+    _expect(qo, into, q, "qo")
+    if (k is None) != (ko is None):
+        raise ValueError("k and ko go together")
+    if k is not None:
+        _expect(k, q.shape, q, "k")
+        _expect(ko, into, q, "ko")
+    for t, name in ((gamma_q, "gamma_q"), (gamma_k, "gamma_k")):
+        if t is not None:
+            _expect(t, (D,), q, name)
+    pairs = tuple(pairs)
+    batches = 1
+    if pairs:
+        if pos is None or freqs is None:
+            raise ValueError("pairs need pos and freqs")
+        batches = pos.shape[0]
+        if batches != 1:
+            batches = B
+        _expect(pos, (batches, L, len(pairs)), None, "pos")
+        _expect(freqs, (sum(pairs),), None, "freqs")
+        if pos.dtype != torch.int32:
+            raise TypeError(f"pos is {pos.dtype}, expected torch.int32")
+        if freqs.dtype != torch.float32:
+            raise TypeError(f"freqs is {freqs.dtype}, expected torch.float32")
+    status = load_library().sdattn_norm_rotate(
+        _here(q, "q"), _here(k, "k") if k is not None else None,
+        _here(gamma_q, "gamma_q") if gamma_q is not None else None,
+        _here(gamma_k, "gamma_k") if gamma_k is not None else None,
+        _here(pos, "pos") if pairs else None, _here(freqs, "freqs") if pairs else None,
+        _here(qo, "qo"), _here(ko, "ko") if ko is not None else None, B, H, L, D, len(pairs),
+        (ctypes.c_int * max(1, len(pairs)))(*pairs), batches, norm, ctypes.c_float(eps), pairing, x_layout, y_layout,
+        _dtype_code(q), _stream(stream))
+    _check("sdattn_norm_rotate", status)
+    return result
+
+
+def _blocks(n, block=SPARSE_BLOCK):
+    return (n + block - 1) // block
+
+
+def block_means(x, means, stream=None):
+    """means [B, H, ceil(L / 64), D] fp32 = the means of the 64-row blocks of x [B, H, L, D]."""
+    if _native and _done("sdattn_block_means", _native.block_means(_fn["sdattn_block_means"], x, means, stream)):
+        return means
+    B, H, L, D = x.shape
+    _expect_means(means, (B, H, _blocks(L), D))
+    status = load_library().sdattn_block_means(_here(x, "x"), _here(means, "means"), B, H, L, D, _dtype_code(x),
+                                               _stream(stream))
+    _check("sdattn_block_means", status)
+    return means
+
+
+def _expect_means(means, shape):
+    import torch
+    _expect(means, shape, None, "means")
+    if means.dtype != torch.float32:
+        raise TypeError(f"means is {means.dtype}, expected torch.float32")
+
+
+def _expect_mask(mask, B, H, Lq, qblock, nb):
+    import torch
+    if qblock < 1:
+        raise ValueError("qblock must be 64 or 128")
+    _expect(mask, (B, H, _blocks(Lq, qblock), _blocks(nb)), None, "mask")
+    if mask.dtype != torch.int64:
+        raise TypeError(f"mask is {mask.dtype}, expected torch.int64")
+
+
+def select_blocks(q, means, mask, keep, qblock=64, stream=None):
+    """Sets in mask int64 [B, H, ceil(Lq / qblock), ceil(NB / 64)] the bits of the `keep` key
+    blocks whose means [B, H, NB, D] score best with the mean of each block of queries."""
+    if _native and _done("sdattn_select_blocks", _native.select_blocks(
+            _fn["sdattn_select_blocks"], q, means, mask, keep, qblock, stream)):
+        return mask
+    B, H, Lq, D = q.shape
+    NB = means.shape[2]
+    _expect_means(means, (B, H, NB, D))
+    _expect_mask(mask, B, H, Lq, qblock, NB)
+    status = load_library().sdattn_select_blocks(_here(q, "q"), _here(means, "means"), _here(mask, "mask"), B, H, Lq, NB,
+                                                 D, qblock, keep, _dtype_code(q), _stream(stream))
+    _check("sdattn_select_blocks", status)
+    return mask
+
+
+def sparse_forward(q, k, v, mask, out, scale: float, qblock=64, stream=None):
+    """out = softmax(scale * q k^T) v over the 64-key blocks whose bits mask (as
+    select_blocks writes it) has for each block of `qblock` queries; zeros where none."""
+    if _native and _done("sdattn_sparse_forward", _native.sparse_forward(
+            _fn["sdattn_sparse_forward"], q, k, v, mask, out, scale, qblock, stream)):
+        return out
+    B, H, Lq, D = q.shape
+    Lk = k.shape[2]
+    _expect(k, (B, H, Lk, D), q, "k")
+    _expect(v, (B, H, Lk, D), q, "v")
+    _expect(out, q.shape, q, "out")
+    _expect_mask(mask, B, H, Lq, qblock, _blocks(Lk))
+    status = load_library().sdattn_sparse_forward(
+        _here(q, "q"), _here(k, "k"), _here(v, "v"), _here(mask, "mask"), _here(out, "out"), B, H, Lq, Lk, D, qblock,
+        ctypes.c_float(scale), _dtype_code(q), _stream(stream))
+    _check("sdattn_sparse_forward", status)
+    return out

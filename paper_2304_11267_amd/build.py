@@ -23,8 +23,9 @@ PROBE_SOURCES = ["probes.hip"]
 MARSHAL = os.path.join(HERE, "_marshal.so")
 ARCH = "gfx950"
 
-SOURCES = ["attn_fwd.hip", "attn_fwd_bf16.hip", "attn_fwd_stats.hip", "attn_fwd_short.hip", "attn_fwd_generic.hip", "softmax_rows.hip",
-           "twopass.hip", "linear.hip", "norm_act.hip", "winograd.hip",
+SOURCES = ["attn_fwd.hip", "attn_fwd_bf16.hip", "attn_fwd_stats.hip", "attn_fwd_short.hip", "attn_fwd_generic.hip",
+           "attn_sparse.hip", "attn_sparse_bf16.hip", "block_select.hip", "softmax_rows.hip",
+           "twopass.hip", "linear.hip", "norm_act.hip", "norm_rotate.hip", "winograd.hip",
            "sdattn_api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -48,6 +49,7 @@ CFLAGS = [
 _NO_NANS = ["-fno-honor-nans"]
 EXTRA_FLAGS = {
     "attn_fwd.hip": _NO_NANS, "attn_fwd_bf16.hip": _NO_NANS, "attn_fwd_stats.hip": _NO_NANS,
+    "attn_sparse.hip": _NO_NANS, "attn_sparse_bf16.hip": _NO_NANS,
     "attn_fwd_short.hip": ["-mllvm", "-amdgpu-kernarg-preload-count=14"],
 }
 

@@ -77,12 +77,25 @@ constexpr float kPBias = 8.0f;
 constexpr float kRescaleLimit = 15.0f;
 constexpr int kDirectTiles = 4;         // tiles per key split up to which m moves from the start
 
-template <int ET, int D, bool STATS, bool OROWS, int GEO>
+// The key blocks that each block of queries reads (attn_sparse.hip), 64 a word: bit
+// j % 64 of word j / 64 of a row stands for the keys 64 j .. 64 j + 63.
+struct BlockMask {
+    const unsigned long long* words;   // [B, H, query blocks, nw]
+    int nw;
+};
+__device__ __forceinline__ BlockMask mask_of() { return BlockMask{nullptr, 0}; }
+__device__ __forceinline__ BlockMask mask_of(BlockMask m) { return m; }
+
+// MASK: nothing (all keys), or a BlockMask.  With one, tile t is the t-th block that
+// the workgroup's query block reads, and everything else stays as it is.
+template <int ET, int D, bool STATS, bool OROWS, int GEO, typename... MASK>
 __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerSimd)) void attn_fwd_lds_kernel(
     const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
     uint16_t* __restrict__ O, float* __restrict__ LS, int Lq, int Lk, float scale_abs, float c,
-    float bias, int neg, int nqb, int oh) {
+    float bias, int neg, int nqb, int oh, const MASK... masks) {
     using G = Geom<D, GEO>;
+    constexpr bool SPARSE = sizeof...(MASK) > 0;
+    static_assert(!SPARSE || (!STATS && !OROWS), "");
     static_assert(!G::kStream || G::QB == 2, "the streaming loop's step x works on query block x");
     constexpr int DK = G::DK;
     constexpr int DN = G::DN;
@@ -117,10 +130,88 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
     // tiles s * nh .. s * nh + nh - 1 (nh = ceil(ntiles / kKS)), the last
     // ones what remains, possibly none; all run nh steps.
     constexpr int kTK = G::kTK;
-    const int ntiles = (Lk + kTK - 1) / kTK;
+    const int nblocks = (Lk + kTK - 1) / kTK;
+    int ntiles = nblocks;
+    // SPARSE: the mask row's words lie in the lanes, 64 at a time (4096 blocks), and a
+    // cursor of this wave's own walks over the bits in the order of the tiles' copies.
+    [[maybe_unused]] const BlockMask mask = mask_of(masks...);
+    [[maybe_unused]] const unsigned long long* const mrow = SPARSE ? mask.words + (size_t)tile * mask.nw : nullptr;
+    [[maybe_unused]] uint64_t word = 0, bits = 0;   // this lane's word; what is left of the cursor's
+    [[maybe_unused]] int part = 0, at = 0;          // 64 words from 64 part on; the cursor's among them
+    [[maybe_unused]] bool ragged = false;           // the last tile ends past Lk
+    [[maybe_unused]] auto load_words = [&]() __attribute__((always_inline)) {
+        const int i = part * 64 + lane;
+        word = i < mask.nw ? mrow[i] : 0;
+        if (i == mask.nw - 1 && nblocks % 64 != 0) word &= (1ull << nblocks % 64) - 1;   // no blocks past Lk
+    };
+    [[maybe_unused]] auto word_of = [&](int i) __attribute__((always_inline)) -> uint64_t {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)word, i) |
+               (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(word >> 32), i) << 32;
+    };
+    // bits set in the words of the lanes up to this one
+    [[maybe_unused]] auto bits_upto = [&]() __attribute__((always_inline)) -> int {
+        int n = __popcll(word);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int below = __shfl_up(n, o, 64);
+            n += lane >= o ? below : 0;
+        }
+        return n;
+    };
+    if constexpr (SPARSE) {
+        ntiles = 0;
+        for (part = 0; part * 64 < mask.nw; ++part) {
+            load_words();
+            ntiles += __builtin_amdgcn_readlane(bits_upto(), 63);
+        }
+        --part;   // the last words are in the lanes
+        ragged = Lk % kTK != 0 && (word_of((mask.nw - 1) % 64) >> (nblocks - 1) % 64 & 1);
+        if (ntiles == 0) {   // nothing to attend to
+            if (kh == 0)
+                for (int r = q0; r < min(q0 + 32 * QB, Lq); ++r)
+                    for (int d = lane * 8; d < D; d += 512) *(u32x4*)(O + ((size_t)bh * Lq + r) * D + d) = u32x4{0u, 0u, 0u, 0u};
+            return;
+        }
+    }
     const int nh = (ntiles + G::kKS - 1) / G::kKS;
     const int t_first = kh * nh;
     const int t_count = min(nh, max(0, ntiles - t_first));
+    // whether tile t has all of its keys, and the first of them where it has not
+    auto whole = [&](int t) __attribute__((always_inline)) {
+        return SPARSE ? !ragged || t != ntiles - 1 : (t + 1) * kTK <= Lk;
+    };
+    auto first_key = [&](int t) __attribute__((always_inline)) { return SPARSE ? (nblocks - 1) * kTK : t * kTK; };
+    // the cursor to bit t_first
+    [[maybe_unused]] auto seek = [&]() __attribute__((always_inline)) {
+        int before = 0;
+        for (part = 0; part * 64 < mask.nw; ++part) {
+            load_words();
+            const int upto = before + bits_upto();
+            const uint64_t past = __ballot(upto > t_first);
+            if (past) {
+                at = __builtin_ctzll(past);
+                bits = word_of(at);
+                for (int skip = t_first - (__builtin_amdgcn_readlane(upto, at) - __popcll(bits)); skip > 0; --skip)
+                    bits &= bits - 1;
+                return;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+        }
+    };
+    // the cursor's block, and one on (past the last bit, which no caller asks for, the last block)
+    [[maybe_unused]] auto next_block = [&]() __attribute__((always_inline)) -> int {
+        while (bits == 0 && part * 64 + at < mask.nw) {
+            if (++at == 64) {
+                at = 0;
+                ++part;
+                load_words();
+            }
+            bits = word_of(at);
+        }
+        const int j = min((part * 64 + at) * 64 + (bits ? __builtin_ctzll(bits) : 0), nblocks - 1);
+        bits &= bits - 1;
+        return __builtin_amdgcn_readfirstlane(j);
+    };
 
     // Copy tile t of this split into its buffer b (the split's kQW waves issue
     // the 1 KiB pieces wq, wq + kQW, ...).  What lies past the last key repeats
@@ -129,15 +220,23 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
         // a tile is one contiguous run of K (and of V) rows; byte offsets inside a
         // head fit 32 bits (the launch checks Lk * D)
         const uint32_t dst = lds0 + hbase + b * G::kBufBytes;
-        const uint32_t tile_off = (uint32_t)t * TB + lane * 16;
-        const uint32_t last = (uint32_t)Lk * (2 * D) - 16;   // a head's last 16 bytes
+        const char *Kt = Kh, *Vt = Vh;
+        uint32_t tile_off = (uint32_t)t * TB + lane * 16;
+        uint32_t last = (uint32_t)Lk * (2 * D) - 16;   // a head's last 16 bytes
+        if constexpr (SPARSE) {   // the block's own start in 64 bits, offsets from there
+            const int j = next_block();
+            Kt += (size_t)j * TB;
+            Vt += (size_t)j * TB;
+            tile_off = lane * 16;
+            last = (uint32_t)min(Lk - j * kTK, kTK) * (2 * D) - 16;
+        }
 #pragma unroll
         for (int i = 0; i < (2 * G::kChunks + kQW - 1) / kQW; ++i) {
             const int cidx = wq + kQW * i;
             if (cidx < 2 * G::kChunks) {
                 const bool isv = cidx >= G::kChunks;
                 const uint32_t off = tile_off + (isv ? cidx - G::kChunks : cidx) * 1024;
-                copy16_to_lds(isv ? Vh : Kh, min(off, last), dst + cidx * 1024);
+                copy16_to_lds(isv ? Vt : Kt, min(off, last), dst + cidx * 1024);
             }
         }
     };
@@ -155,6 +254,9 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
         __builtin_amdgcn_sched_barrier(0);
     };
 
+    if constexpr (SPARSE && G::kStream) {
+        if (t_count > 0) seek();
+    }
     if constexpr (G::kStream) {
 #pragma unroll
         for (int i = 0; i < G::kSlots - G::kStep; ++i)
@@ -484,12 +586,12 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
     // mode mode0_c, the others in mode_c.
     auto consume = [&](auto mode0_c, auto mode_c, int t, int b) __attribute__((always_inline)) {
         const int buf = hbase + b * G::kBufBytes;
-        const int kbase = t * kTK;
+        const int kbase = first_key(t);
         // (kFirst is the pipeline's kOnline with nothing before it; the streaming
         // kernels' kFixed has its own loop)
         constexpr bool kPipelined = decltype(mode_c)::value == kOnline ||
                                     (!G::kStream && decltype(mode0_c)::value == kFixed);
-        if (kbase + kTK <= Lk) {
+        if (whole(t)) {
             if constexpr (kPipelined) {
                 tile_pipe(mode_c, buf);
             } else {
@@ -508,6 +610,9 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
     // all tiles of this half: the first tile opens with kFirst, every other
     // sub-tile runs in mode_c (kFixed, or kOnline for the fallback)
     auto run_tiles = [&](auto mode_c) __attribute__((always_inline)) {
+        if constexpr (SPARSE) {
+            if (t_count > 0) seek();
+        }
         if (t_count > 0) issue_tile(t_first, 0);
         barrier(0);
         if (t_count > 0) {
@@ -525,7 +630,7 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
             const int b = i & 1;
             if (i + 1 < t_count) issue_tile(t_first + i + 1, b ^ 1);
             if (i < t_count) {
-                if ((t_first + i + 1) * kTK <= Lk) consume(mode_c, mode_c, t_first + i, b);
+                if (whole(t_first + i)) consume(mode_c, mode_c, t_first + i, b);
                 else pend = i;
             }
             barrier(0);
@@ -553,7 +658,8 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
         constexpr int NQ = DK;                                 // MFMAs of S^T
         constexpr int NP = 2 * DD + (G::kSparse ? 1 : 0);      // MFMAs of O^T
         constexpr int NM = NQ + NP;
-        const int n_whole = max(0, min(t_count, Lk / kTK - t_first));
+        const int n_whole = SPARSE ? t_count - (t_count > 0 && !whole(t_first + t_count - 1) ? 1 : 0)
+                                   : max(0, min(t_count, Lk / kTK - t_first));
 
         barrier(min(t_count, SL - G::kStep) - 1);   // tile 0 (the first SL - kStep were issued above)
 
@@ -893,15 +999,15 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
     }
 }
 
-template <int ET, int D, bool STATS, bool OROWS, int GEO>
-hipError_t launch_kernel(const AttnArgs& a) {
+template <int ET, int D, bool STATS, bool OROWS, int GEO, typename... MASK>
+hipError_t launch_kernel(const AttnArgs& a, const MASK... mask) {
     using G = Geom<D, GEO>;
     const int nqb = (a.Lq + G::kBQ - 1) / G::kBQ;
     const long long nblk = (long long)a.B * a.H * nqb;
     const float scale_abs = a.scale < 0 ? -a.scale : a.scale;
     const float c = scale_abs * kLog2e;
     const float bias = c > 1e-30f ? kPBias / c : 0.0f;   // scale 0: every weight is 1 whatever m
-    auto kern = attn_fwd_lds_kernel<ET, D, STATS, OROWS, GEO>;
+    auto kern = attn_fwd_lds_kernel<ET, D, STATS, OROWS, GEO, MASK...>;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize,
                                                        G::kLdsBytes);
@@ -909,7 +1015,7 @@ hipError_t launch_kernel(const AttnArgs& a) {
     hipLaunchKernelGGL(kern, dim3((unsigned)nblk), dim3(G::kThreads), G::kLdsBytes,
                        (hipStream_t)a.stream, (const uint16_t*)a.q, (const uint16_t*)a.k,
                        (const uint16_t*)a.v, (uint16_t*)a.out, a.ls, a.Lq, a.Lk, scale_abs, c, bias,
-                       a.scale < 0 ? 1 : 0, nqb, a.o_rows ? a.H : 0);
+                       a.scale < 0 ? 1 : 0, nqb, a.o_rows ? a.H : 0, mask...);
     return hipGetLastError();
 }
 

@@ -1,0 +1,51 @@
+// attn_sparse.h -- attention over the blocks of 64 keys that a bit mask names for
+// each block of 64 or 128 queries: the tiled kernel of attn_fwd_kernel.h, whose tiles
+// are those blocks, in the geometries whose workgroup is one query block.
+//
+//   out_i = sum over the keys j of the blocks in the mask of i's query block of
+//           softmax_j(scale q_i . k_j) v_j;  0 where the mask is empty
+//
+// Its work is 4 D operations for every (query, key) pair of those blocks; each block
+// is read once per query block that names it, from the XCD's L2 mostly.
+#pragma once
+
+#include "attn_fwd_kernel.h"
+
+namespace sdattn {
+
+namespace {
+
+// 64 queries: kGeoSmall; 128: kGeoNormal, or kGeoPair past one round over the CUs
+// (attn_geom.h).
+template <int ET, int D>
+hipError_t launch_sparse_d(const SparseArgs& s) {
+    const AttnArgs a{s.q, s.k, s.v, s.out, nullptr, s.B, s.H, s.Lq, s.Lk, D, s.scale, s.dtype, s.stream};
+    const int nw = ((s.Lk + kSparseBlock - 1) / kSparseBlock + 63) / 64;
+    const BlockMask mask{(const unsigned long long*)s.mask, nw};
+    if (s.qblock == 64) return launch_kernel<ET, D, false, false, kGeoSmall>(a, mask);
+    if constexpr (Geom<D, kGeoPair>::kFits) {
+        if ((long long)s.B * s.H * ((s.Lq + 127) / 128) > kCus) return launch_kernel<ET, D, false, false, kGeoPair>(a, mask);
+    }
+    return launch_kernel<ET, D, false, false, kGeoNormal>(a, mask);
+}
+
+// The widths whose tiles fit the LDS in both geometries: D = 32, 40, ..., 160, but 152
+// (whose tiles and block of ones together do not).
+template <int ET, int... I>
+hipError_t dispatch_sparse(const SparseArgs& s, std::integer_sequence<int, I...>) {
+    hipError_t r = hipErrorInvalidValue;
+    auto one = [&](auto i_c) {
+        constexpr int D = kSparseMinD + 8 * decltype(i_c)::value;
+        static_assert(sparse_width(D) == (Geom<D, kGeoNormal>::kFits && Geom<D, kGeoSmall>::kFits), "");
+        if constexpr (sparse_width(D)) {
+            if (s.D == D) r = launch_sparse_d<ET, D>(s);
+        }
+    };
+    (one(std::integral_constant<int, I>{}), ...);
+    return r;
+}
+using SparseWidths = std::make_integer_sequence<int, (kSparseMaxD - kSparseMinD) / 8 + 1>;
+
+}  // namespace
+
+}  // namespace sdattn

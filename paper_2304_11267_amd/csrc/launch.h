@@ -90,6 +90,18 @@ hipError_t launch_linear(const LinearArgs& a);
 constexpr int kMaxLinearProblems = 3;
 hipError_t launch_linear_group(const LinearArgs* a, int n);
 
+// A product with low-rank adapters beside it, one for each batch item (linear.hip).
+struct AdapterArgs {
+    const void* down;     // [count, R, K]
+    const void* up;       // [count, N, R]
+    const int* ids;       // [B]; none outside [0, count)
+    const float* scales;  // [count] or null
+    void* t;              // [B L, adapter_rank_padded(R)] workspace
+    int R, count;
+};
+constexpr int adapter_rank_padded(int R) { return (R + 15) / 16 * 16; }
+hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& d);
+
 // Group normalisation and GEGLU (norm_act.hip).
 struct GroupNormArgs {
     const void* x;        // [B, C, HW]
@@ -114,6 +126,70 @@ struct GegluArgs {
     void* stream;
 };
 hipError_t launch_geglu(const GegluArgs& a);
+
+// Per-head norms and position rotation of queries and keys (norm_rotate.hip).
+struct NormRotateArgs {
+    const void* q;
+    const void* k;        // or null: q alone
+    const void* gamma_q;  // [D] or null
+    const void* gamma_k;  // [D] or null
+    const int* pos;       // [pos_batches, L, axes]
+    const float* freqs;   // [sum of pairs]
+    void* qo;             // may be q
+    void* ko;             // may be k
+    int B, H, L, D;
+    int axes;             // at most 4
+    int pairs[4];
+    int pos_batches;      // 1 or B
+    bool x_heads, y_heads, norm, halves;
+    float eps;
+    int dtype;
+    void* stream;
+};
+hipError_t launch_norm_rotate(const NormRotateArgs& a);
+
+// Means of key blocks, the choice of blocks by them (block_select.hip), and the
+// attention over the chosen ones (attn_sparse.hip).
+constexpr int kSparseBlock = 64;     // keys of a block
+constexpr int kSparseMinD = 32;      // head widths of the attention
+constexpr int kSparseMaxD = 160;
+constexpr bool sparse_width(int D) { return D >= kSparseMinD && D <= kSparseMaxD && D % 8 == 0 && D != 152; }
+struct BlockMeansArgs {
+    const void* x;        // [B, H, L, D]
+    float* means;         // [B, H, ceil(L / 64), D]
+    int B, H, L, D;
+    int dtype;
+    void* stream;
+};
+hipError_t launch_block_means(const BlockMeansArgs& a);
+
+struct SelectArgs {
+    const void* q;        // [B, H, Lq, D]
+    const float* means;   // [B, H, NB, D]
+    void* mask;           // [B, H, ceil(Lq / qblock), words] of 64 bits
+    int B, H, Lq, NB, D;
+    int qblock, keep;
+    int dtype;
+    void* stream;
+};
+constexpr int kSelectMaxBlocks = 16384;
+hipError_t launch_select_blocks(const SelectArgs& a);
+
+struct SparseArgs {
+    const void* q;
+    const void* k;
+    const void* v;
+    const void* mask;
+    void* out;
+    int B, H, Lq, Lk, D;
+    int qblock;           // 64 or 128
+    float scale;
+    int dtype;
+    void* stream;
+};
+hipError_t launch_attn_sparse(const SparseArgs& a);
+// the bf16 instantiations (a translation unit of their own)
+hipError_t launch_attn_sparse_bf16(const SparseArgs& a);
 
 // Winograd F(4x4, 3x3) convolution (winograd.hip).
 struct WinoFilterArgs {

@@ -30,6 +30,11 @@
 // B = 16 channels x 32 token rows, one token row per lane; each lane ends with
 // 4 consecutive output channels per register group; the tile goes out through
 // LDS so that each lane stores 16 contiguous bytes.
+//
+// Low-rank adapters of many requests ride beside the shared product: row m of batch
+// item b adds s_i up_i (down_i x_m), i = ids[b].  A first launch (adapter_down_kernel)
+// writes T = s_i down_i x_m, and both kernels above then carry T up_i^T as a few more
+// steps of their reduced dimension.
 #include "device.h"
 #include "launch.h"
 
@@ -98,6 +103,67 @@ __device__ __forceinline__ size_t chan_offset(int c, int L, int hw, float inv_hw
     }
 }
 
+// The adapters of a product's rows: T holds their rows' inner products.
+struct AdapterSet {
+    const uint16_t* t;      // [M, Rp]; rows without an adapter unwritten
+    const uint16_t* up;     // [count, N, R]
+    const int* ids;         // [B]: the adapter of a batch item; none outside [0, count)
+    int count, R, Rp;
+};
+__device__ __forceinline__ AdapterSet adapters_of() { return AdapterSet{}; }
+__device__ __forceinline__ AdapterSet adapters_of(const AdapterSet& a) { return a; }
+
+// Ranks r0 .. r0 + 7 of an adapter's row of R, zeros from R on; rows of whole 16-byte
+// chunks are read as such.
+__device__ __forceinline__ u32x4 adapter_chunk(const uint16_t* row, int r0, int R) {
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (R % 8 == 0) {
+        if (r0 < R) v = *(const u32x4*)(row + r0);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (r0 + e < R) v[e >> 1] |= (uint32_t)row[r0 + e] << (16 * (e & 1));
+    }
+    return v;
+}
+
+// acc[b] += up T^T for the 32 token rows from row0 and the 32 channels from n0 + 32 b,
+// 16 ranks a step.  The rows of one batch item at a time, summed apart and added to its
+// rows alone: other requests' rows see nothing of an adapter, not even its infinities,
+// and a request's bits do not depend on its neighbours in a tile.
+template <int ET, int NB>
+__device__ __forceinline__ void add_adapters(const AdapterSet& ad, int row0, int n0, int M, int N, int L,
+                                             f32x16 (&acc)[NB]) {
+    if (row0 >= M) return;
+    const int l32 = lane_id() & 31, half = lane_id() >> 5;
+    const int row = min(row0 + l32, M - 1);
+    const int last = min(row0 + 31, M - 1) / L;
+    for (int b = row0 / L; b <= last; ++b) {
+        const int id = __builtin_amdgcn_readfirstlane(ad.ids[b]);
+        if (id < 0 || id >= ad.count) continue;
+        const bool mine = (long long)row >= (long long)b * L && (long long)row < (long long)(b + 1) * L;
+        f32x16 sum[NB];
+#pragma unroll
+        for (int t = 0; t < NB; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[t][r] = 0.0f;
+        for (int s = 0; s < ad.Rp / 16; ++s) {
+            const int r0 = 16 * s + 8 * half;
+            u32x4 tf = {0u, 0u, 0u, 0u};
+            if (mine) tf = *(const u32x4*)(ad.t + (size_t)row * ad.Rp + r0);
+#pragma unroll
+            for (int t = 0; t < NB; ++t) {
+                const int n = min(n0 + 32 * t + l32, N - 1);
+                sum[t] = mfma32x32x16<ET>(adapter_chunk(ad.up + ((size_t)id * N + n) * ad.R, r0, ad.R), tf, sum[t]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NB; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[t][r] += mine ? sum[t][r] : 0.0f;
+    }
+}
+
 // Wait until at most `ahead` slices of this wave's copies are still in flight.
 __device__ __forceinline__ void wait_slices(int ahead) {
     static_assert(kStages == 3, "wait_slices covers ahead = 0 and 1");
@@ -113,8 +179,9 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-template <int ET, bool XH, bool YH, bool FOLD>
-__global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp) {
+// AD: nothing, or an AdapterSet (of one product with batch 1)
+template <int ET, bool XH, bool YH, bool FOLD, typename... AD>
+__global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const AD... ad) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = lane_id();
     const int l32 = lane & 31;
@@ -297,6 +364,8 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp) {
         for (int i = i0 + 1; i < min(i0 + run, nk); ++i) slice(i, std::false_type{}, acc, [] {});
     }
 
+    if constexpr (sizeof...(AD) > 0) add_adapters<ET>(adapters_of(ad...), m0 + 32 * wave, n0, M, N, L, acc);
+
     // Stage the 128 x 64 output tile (bias added, rounded) in LDS, rows of
     // kOutStride bytes: lane (l32, half) holds channels 32t + 8g + 4*half + (0..3)
     // of tile row 32*wave + l32.
@@ -383,8 +452,8 @@ __device__ __forceinline__ void ks_wait(int n) {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES * N) : "memory");
 }
 
-template <int ET, bool YH, int TM, int TN, int ST>
-__global__ __launch_bounds__(256) void linear_ksplit_kernel(const LinGroup grp) {
+template <int ET, bool YH, int TM, int TN, int ST, typename... AD>
+__global__ __launch_bounds__(256) void linear_ksplit_kernel(const LinGroup grp, const AD... ad) {
     using G = KsGeom<TM, TN, ST>;
     constexpr int MB = TM / 32, NB = TN / 32, KS = kBK / 16;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -486,6 +555,15 @@ __global__ __launch_bounds__(256) void linear_ksplit_kernel(const LinGroup grp) 
                 for (int b = 0; b < NB; ++b) acc[a][b] = mfma32x32x16<ET>(wf[b][s], xf[a][s], acc[a][b]);
     }
 
+    // the adapters' steps follow the last channels, as in the shared tiles (and so have
+    // the same bits)
+    if constexpr (sizeof...(AD) > 0) {
+        if (wave == (ns - 1) / per) {
+#pragma unroll
+            for (int a = 0; a < MB; ++a) add_adapters<ET>(adapters_of(ad...), m0 + 32 * a, n0, M, N, L, acc[a]);
+        }
+    }
+
     // 16 bytes per lane: chunk q = tid + 256j is tile row q / (TN / 8), channels
     // n = n0 + 8 (q % (TN / 8)) .. + 7, the same n for every j
     constexpr int kCols = TN / 8;
@@ -542,25 +620,114 @@ __global__ __launch_bounds__(256) void linear_ksplit_kernel(const LinGroup grp) 
     }
 }
 
+// T = s_i down_i x for the rows of the batch items that have an adapter: a workgroup
+// takes 16 rows of one item and 16 RB ranks, its four waves a quarter of the channels
+// each.  T^T = down x^T on 16x16x32 MFMAs, whose operands come straight from memory, 16
+// bytes a lane: a row's 64 bytes meet in one instruction, and the next one takes the
+// other half of its cache lines.  Bound by reading x once (rows of other items, and the
+// adapters, are read from the cache).  T is rounded to the tensors' type, the type that
+// the second product's matrix instructions take; the scale goes in before, in fp32.
+constexpr int kDownSteps = 4;   // steps of 32 channels in flight
+struct DownKernel {
+    const uint16_t* x;
+    const uint16_t* down;   // [count, R, K]
+    const int* ids;
+    const float* scales;    // [count] or null
+    uint16_t* t;            // [B L, Rp]
+    int L, K, xhw, R, Rp, count;
+    int tiles;              // row tiles of an item
+};
+
+template <int ET>
+__device__ __forceinline__ f32x4 mfma16x16x32(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (ET == kF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <int ET, bool XH, int RB>
+__global__ __launch_bounds__(256) void adapter_down_kernel(const DownKernel a) {
+    __shared__ f32x4 part[kRuns - 1][RB][64];
+    const int lane = lane_id();
+    const int l16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int b = blockIdx.x / a.tiles, l0 = (blockIdx.x - b * a.tiles) * 16;
+    const int r0 = blockIdx.y * 16 * RB;
+    const int id = a.ids[b];
+    if (id < 0 || id >= a.count) return;
+    const float inv_xhw = 1.0f / (float)a.xhw;
+    const int l = min(l0 + l16, a.L - 1);
+    const uint16_t* x = a.x + row_base<XH>(b * a.L + l, a.L, a.K, a.xhw);
+    const uint16_t* d[RB];
+#pragma unroll
+    for (int j = 0; j < RB; ++j) d[j] = a.down + ((size_t)id * a.R + min(r0 + 16 * j + l16, a.R - 1)) * a.K;
+
+    f32x4 acc[RB];
+#pragma unroll
+    for (int j = 0; j < RB; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int steps = (a.K + 31) / 32;
+    const int per = (steps + kRuns - 1) / kRuns;
+    const int first = wave * per, end = min(first + per, steps);
+    for (int s0 = first; s0 < end; s0 += kDownSteps) {
+        u32x4 xv[kDownSteps], dv[kDownSteps][RB];
+#pragma unroll
+        for (int u = 0; u < kDownSteps; ++u) {
+            const int c = 32 * (s0 + u) + 8 * quad, cc = min(c, a.K - 8);
+            xv[u] = *(const u32x4*)(x + chan_offset<XH>(cc, a.L, a.xhw, inv_xhw));
+#pragma unroll
+            for (int j = 0; j < RB; ++j) dv[u][j] = *(const u32x4*)(d[j] + cc);
+        }
+#pragma unroll
+        for (int u = 0; u < kDownSteps; ++u) {
+            // past this wave's channels both factors are zeros (a zero and a NaN are no zero)
+            const bool out = s0 + u >= end || 32 * (s0 + u) + 8 * quad >= a.K;
+            if (out) xv[u] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int j = 0; j < RB; ++j) acc[j] = mfma16x16x32<ET>(out ? xv[u] : dv[u][j], xv[u], acc[j]);
+        }
+    }
+    if (wave > 0) {
+#pragma unroll
+        for (int j = 0; j < RB; ++j) part[wave - 1][j][lane] = acc[j];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    const float scale = a.scales ? a.scales[id] : 1.0f;
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+#pragma unroll
+        for (int w = 0; w < kRuns - 1; ++w) acc[j] += part[w][j][lane];
+        // this lane's 4 ranks of its row; ranks from R on are zeros
+        const int r = r0 + 16 * j + 4 * quad;
+        if (l0 + l16 < a.L && r < a.Rp) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = r + e < a.R ? acc[j][e] * scale : 0.0f;
+            *(u32x2*)(a.t + (size_t)(b * a.L + l) * a.Rp + r) = u32x2{pack2<ET>(v[0], v[1]), pack2<ET>(v[2], v[3])};
+        }
+    }
+}
+
 // tm x tn tiles of one batch item
 long long tiles_of(const LinearArgs& a, int tm, int tn) {
     return ((long long)a.B * a.L + tm - 1) / tm * ((a.N + tn - 1) / tn);
 }
 
-template <int ET, bool XH, bool YH, bool FOLD>
-hipError_t launch_t(const LinGroup& g, long long nblk, void* stream) {
+template <int ET, bool XH, bool YH, bool FOLD, typename... AD>
+hipError_t launch_t(const LinGroup& g, long long nblk, void* stream, const AD&... ad) {
+    auto k = linear_kernel<ET, XH, YH, FOLD, AD...>;
     static const hipError_t attr = hipFuncSetAttribute(
-        reinterpret_cast<const void*>(&linear_kernel<ET, XH, YH, FOLD>),
-        hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+        reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((linear_kernel<ET, XH, YH, FOLD>), dim3((unsigned)nblk), dim3(256), kLdsBytes,
-                       (hipStream_t)stream, g);
+    hipLaunchKernelGGL(k, dim3((unsigned)nblk), dim3(256), kLdsBytes, (hipStream_t)stream, g, ad...);
     return hipGetLastError();
 }
 
-template <int ET, bool XH, bool YH>
-hipError_t launch_f(const LinGroup& g, long long nblk, bool fold, void* stream) {
-    return fold ? launch_t<ET, XH, YH, true>(g, nblk, stream) : launch_t<ET, XH, YH, false>(g, nblk, stream);
+template <int ET, bool XH, bool YH, typename... AD>
+hipError_t launch_f(const LinGroup& g, long long nblk, bool fold, void* stream, const AD&... ad) {
+    return fold ? launch_t<ET, XH, YH, true>(g, nblk, stream, ad...)
+                : launch_t<ET, XH, YH, false>(g, nblk, stream, ad...);
 }
 
 // Number the TM x TN tiles of the group's products (tile0, per_batch, nnt);
@@ -577,16 +744,16 @@ long long number_tiles(LinGroup& g, const LinearArgs* a, int tm, int tn) {
     return nblk;
 }
 
-template <int ET, bool YH, int TM, int TN, int ST>
-hipError_t launch_ks(LinGroup& g, const LinearArgs* a) {
+template <int ET, bool YH, int TM, int TN, int ST, typename... AD>
+hipError_t launch_ks(LinGroup& g, const LinearArgs* a, const AD&... ad) {
     using G = KsGeom<TM, TN, ST>;
     const long long nblk = number_tiles(g, a, TM, TN);
     if (nblk > 0x7fffffff) return hipErrorInvalidValue;
-    auto k = linear_ksplit_kernel<ET, YH, TM, TN, ST>;
+    auto k = linear_ksplit_kernel<ET, YH, TM, TN, ST, AD...>;
     static const hipError_t attr = hipFuncSetAttribute(
         reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL(k, dim3((unsigned)nblk), dim3(256), G::kLds, (hipStream_t)a[0].stream, g);
+    hipLaunchKernelGGL(k, dim3((unsigned)nblk), dim3(256), G::kLds, (hipStream_t)a[0].stream, g, ad...);
     return hipGetLastError();
 }
 
@@ -595,21 +762,21 @@ hipError_t launch_ks(LinGroup& g, const LinearArgs* a) {
 // enough (two per CU), 32 x 64 between.  Measured (us, 32x32 / 32x64 / 64x64):
 // 128x1280x1280 5.1 / 6.0 / 7+; 512x1280x1280 10.0 / 9.2 / 9.1; 36 products
 // 48x1280x1280 - / 34.5 / 30.3; 36 of 64x640x640 12.2 / 9.5 / 10.3.
-template <int ET, bool YH>
-hipError_t launch_ksplit(LinGroup& g, const LinearArgs* a) {
+template <int ET, bool YH, typename... AD>
+hipError_t launch_ksplit(LinGroup& g, const LinearArgs* a, const AD&... ad) {
     long long n32 = 0, n64 = 0, rows = 0;
     for (int i = 0; i < g.n; ++i) {
         n32 += tiles_of(a[i], 32, 32) * a[i].batch;
         n64 += tiles_of(a[i], 64, 64) * a[i].batch;
         rows = rows > g.p[i].M ? rows : g.p[i].M;
     }
-    if (n32 <= 256) return launch_ks<ET, YH, 32, 32, 2>(g, a);
-    if (rows > 32 && n64 >= 512) return launch_ks<ET, YH, 64, 64, 1>(g, a);
-    return launch_ks<ET, YH, 32, 64, 1>(g, a);
+    if (n32 <= 256) return launch_ks<ET, YH, 32, 32, 2>(g, a, ad...);
+    if (rows > 32 && n64 >= 512) return launch_ks<ET, YH, 64, 64, 1>(g, a, ad...);
+    return launch_ks<ET, YH, 32, 64, 1>(g, a, ad...);
 }
 
-template <int ET>
-hipError_t launch_group_e(LinGroup& g, const LinearArgs* a) {
+template <int ET, typename... AD>
+hipError_t launch_group_e(LinGroup& g, const LinearArgs* a, const AD&... ad) {
     const bool xh = a[0].x_heads, yh = a[0].y_heads;
     // Split K over the waves where 128-row tiles leave the chip idle (at most
     // 128 of them: half of the CUs) or mostly compute padding (at most 64 rows):
@@ -629,31 +796,40 @@ hipError_t launch_group_e(LinGroup& g, const LinearArgs* a) {
             may = may && a[i].K > kSplitMinK;
         }
         if (may && (tiles <= 128 || few_rows))
-            return yh ? launch_ksplit<ET, true>(g, a) : launch_ksplit<ET, false>(g, a);
+            return yh ? launch_ksplit<ET, true>(g, a, ad...) : launch_ksplit<ET, false>(g, a, ad...);
     }
     const long long nblk = number_tiles(g, a, kBM, kBN);
     if (nblk > 0x7fffffff) return hipErrorInvalidValue;
     bool fold = false;
     for (int i = 0; i < g.n; ++i) fold = fold || a[i].K > kSplitMinK;
     void* s = a[0].stream;
-    if (xh) return yh ? launch_f<ET, true, true>(g, nblk, fold, s) : launch_f<ET, true, false>(g, nblk, fold, s);
-    return yh ? launch_f<ET, false, true>(g, nblk, fold, s) : launch_f<ET, false, false>(g, nblk, fold, s);
+    if (xh)
+        return yh ? launch_f<ET, true, true>(g, nblk, fold, s, ad...) : launch_f<ET, true, false>(g, nblk, fold, s, ad...);
+    return yh ? launch_f<ET, false, true>(g, nblk, fold, s, ad...) : launch_f<ET, false, false>(g, nblk, fold, s, ad...);
 }
 
-}  // namespace
-
-long long linear_grid(int B, int L, int N) {
-    // (the split-K kernel's smaller tiles are taken for at most 128 of these, or 64 rows)
-    LinearArgs a{};
-    a.B = B;
-    a.L = L;
-    a.N = N;
-    return tiles_of(a, kBM, kBN);
+template <int ET, bool XH>
+hipError_t launch_down(const LinearArgs& a, const AdapterArgs& d) {
+    DownKernel k{(const uint16_t*)a.x, (const uint16_t*)d.down, d.ids, d.scales, (uint16_t*)d.t,
+                 a.L, a.K, a.x_heads ? a.K / a.H : 1, d.R, adapter_rank_padded(d.R), d.count, (a.L + 15) / 16};
+    const int rb = d.R <= 16 ? 1 : d.R <= 32 ? 2 : 4;
+    const dim3 grid((unsigned)(a.B * k.tiles), (unsigned)((d.R + 16 * rb - 1) / (16 * rb)));
+    auto f = rb == 1 ? adapter_down_kernel<ET, XH, 1> : rb == 2 ? adapter_down_kernel<ET, XH, 2> : adapter_down_kernel<ET, XH, 4>;
+    hipLaunchKernelGGL(f, grid, dim3(256), 0, (hipStream_t)a.stream, k);
+    return hipGetLastError();
 }
 
-hipError_t launch_linear_group(const LinearArgs* a, int n) {
+template <int ET>
+hipError_t launch_adapters_e(LinGroup& g, const LinearArgs& a, const AdapterArgs& d) {
+    const hipError_t e = a.x_heads ? launch_down<ET, true>(a, d) : launch_down<ET, false>(a, d);
+    if (e != hipSuccess) return e;
+    const AdapterSet set{(const uint16_t*)d.t, (const uint16_t*)d.up, d.ids, d.count, d.R, adapter_rank_padded(d.R)};
+    return launch_group_e<ET>(g, &a, set);
+}
+
+// The group's products; an error for those that cannot share a launch.
+hipError_t make_group(LinGroup& g, const LinearArgs* a, int n) {
     if (n < 1 || n > kMaxLinearProblems) return hipErrorInvalidValue;
-    LinGroup g{};
     g.n = n;
     for (int i = 0; i < n; ++i) {
         if (a[i].dtype != a[0].dtype || a[i].x_heads != a[0].x_heads ||
@@ -674,9 +850,34 @@ hipError_t launch_linear_group(const LinearArgs* a, int n) {
         p.sw = a[i].sw;
         p.sy = a[i].sy;
     }
+    return hipSuccess;
+}
+
+}  // namespace
+
+long long linear_grid(int B, int L, int N) {
+    // (the split-K kernel's smaller tiles are taken for at most 128 of these, or 64 rows)
+    LinearArgs a{};
+    a.B = B;
+    a.L = L;
+    a.N = N;
+    return tiles_of(a, kBM, kBN);
+}
+
+hipError_t launch_linear_group(const LinearArgs* a, int n) {
+    LinGroup g{};
+    const hipError_t e = make_group(g, a, n);
+    if (e != hipSuccess) return e;
     return a[0].dtype == kF16 ? launch_group_e<kF16>(g, a) : launch_group_e<kBF16>(g, a);
 }
 
 hipError_t launch_linear(const LinearArgs& a) { return launch_linear_group(&a, 1); }
+
+hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& d) {
+    LinGroup g{};
+    const hipError_t e = make_group(g, &a, 1);
+    if (e != hipSuccess) return e;
+    return a.dtype == kF16 ? launch_adapters_e<kF16>(g, a, d) : launch_adapters_e<kBF16>(g, a, d);
+}
 
 }  // namespace sdattn

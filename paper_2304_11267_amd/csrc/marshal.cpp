@@ -53,6 +53,15 @@ struct Args {
         if (!ok || i >= n || !PyFloat_CheckExact(v[i])) return fail(), 0.0f;
         return (float)PyFloat_AS_DOUBLE(v[i]);
     }
+    // stream, where every tensor so far has to live on the current device
+    void* stream_here(Py_ssize_t i) {
+        PyObject* dev = ok && current_device ? PyObject_CallNoArgs(current_device) : nullptr;
+        const long now = dev && PyLong_Check(dev) ? PyLong_AsLong(dev) : -1;
+        Py_XDECREF(dev);
+        for (Py_ssize_t j = 1; ok && j < i; ++j)
+            if (THPVariable_CheckExact(v[j]) && THPVariable_Unpack(v[j]).device().index() != now) fail();
+        return stream(i);
+    }
     // the stream argument: None for the current stream of the current device
     void* stream(Py_ssize_t i) {
         if (!ok || i >= n) return fail();
@@ -290,6 +299,130 @@ PyObject* conv3x3(Args& a) {
                 (int)B, (int)Ci, (int)Co, (int)H, (int)W, code, s);
 }
 
+// a layout's sizes: rows [B, L, C] or heads [B, H, L, C / H]
+bool row_sizes(const at::Tensor& t, long long layout, int64_t heads, int64_t* B, int64_t* L, int64_t* C) {
+    if (layout == 1) {
+        if (t.dim() != 4 || t.size(1) != heads) return false;
+        *B = t.size(0), *L = t.size(2), *C = heads * t.size(3);
+    } else {
+        if (layout != 0 || t.dim() != 3) return false;
+        *B = t.size(0), *L = t.size(1), *C = t.size(2);
+    }
+    return true;
+}
+bool is_rows(const at::Tensor* t, long long layout, int64_t heads, int64_t B, int64_t L, int64_t C, c10::ScalarType type) {
+    int64_t b, l, c;
+    return t && t->scalar_type() == type && row_sizes(*t, layout, heads, &b, &l, &c) && b == B && l == L && c == C;
+}
+
+// fn, x, w, y, down, up, ids, workspace, scales, bias, heads, x_layout, y_layout, stream
+PyObject* linear_adapters(Args& a) {
+    const at::Tensor *x = a.tensor(1), *w = a.tensor(2), *y = a.tensor(3), *down = a.tensor(4), *ws = a.tensor(7);
+    const long long heads = a.integer(10), xl = a.integer(11), yl = a.integer(12);
+    int64_t B, L, K;
+    if (!a.ok || w->dim() != 2 || down->dim() != 3 || heads < 1 || !row_sizes(*x, xl, heads, &B, &L, &K)) return nullptr;
+    const auto type = x->scalar_type();
+    const int64_t N = w->size(0), A = down->size(0), R = down->size(1);
+    const int64_t wsz[] = {N, K}, ds[] = {A, R, K}, us[] = {A, N, R}, b1[] = {B}, a1[] = {A}, n1[] = {N};
+    a.tensor(2, wsz, type);
+    a.tensor(4, ds, type);
+    const at::Tensor *up = a.tensor(5, us, type), *ids = a.tensor(6, b1, c10::kInt), *scales = a.maybe(8, a1, c10::kFloat),
+                     *bias = a.maybe(9, n1, type);
+    void* s = a.stream_here(13);
+    const int code = type_code(*x);
+    if (!a.ok || code < 0 || !is_rows(y, yl, heads, B, L, N, type) || !fits({B, L, K, N, R, A})) return nullptr;
+    return call(a.fn(), ptr(x), ptr(w), ptr(bias), ptr(down), ptr(up), ptr(ids), ptr(scales), ptr(y), ptr(ws),
+                (long long)(ws->numel() * ws->element_size()), (int)B, (int)L, (int)K, (int)N, (int)R, (int)A, (int)heads,
+                (int)xl, (int)yl, code, s);
+}
+
+// fn, q, qo, heads, k, ko, gamma_q, gamma_k, pos, freqs, pairs, norm, eps, pairing, x_layout, y_layout, stream
+PyObject* norm_rotate(Args& a) {
+    const at::Tensor *q = a.tensor(1), *qo = a.tensor(2);
+    const long long H = a.integer(3), norm = a.integer(11), pairing = a.integer(13), xl = a.integer(14), yl = a.integer(15);
+    const float eps = a.real(12);
+    int64_t B, L, C;
+    if (!a.ok || H < 1 || !row_sizes(*q, xl, H, &B, &L, &C) || C % H) return nullptr;
+    const auto type = q->scalar_type();
+    const int64_t D = C / H, d1[] = {D};
+    const at::Tensor *k = a.maybe(4, q->sizes(), type), *ko = a.maybe(5, qo->sizes(), type),
+                     *gq = a.maybe(6, d1, type), *gk = a.maybe(7, d1, type);
+    if (!a.ok || !k != !ko || !PyTuple_CheckExact(a.v[10])) return nullptr;
+    const Py_ssize_t axes = PyTuple_GET_SIZE(a.v[10]);
+    int pairs[4] = {0, 0, 0, 0};
+    int64_t P = 0, batches = 1;
+    if (axes > 4) return nullptr;
+    for (Py_ssize_t i = 0; i < axes; ++i) {
+        PyObject* o = PyTuple_GET_ITEM(a.v[10], i);
+        const long n = PyLong_CheckExact(o) ? PyLong_AsLong(o) : -1;
+        if (n < 1 || n > 65536) return nullptr;
+        pairs[i] = (int)n;
+        P += n;
+    }
+    const at::Tensor *pos = nullptr, *freqs = nullptr;
+    if (axes) {
+        pos = a.tensor(8);
+        if (!pos || pos->dim() != 3 || pos->scalar_type() != c10::kInt) return nullptr;
+        batches = pos->size(0);
+        if ((batches != 1 && batches != B) || pos->size(1) != L || pos->size(2) != axes) return nullptr;
+        const int64_t p1[] = {P};
+        freqs = a.tensor(9, p1, c10::kFloat);
+    }
+    void* s = a.stream_here(16);
+    const int code = type_code(*q);
+    if (!a.ok || code < 0 || !is_rows(qo, yl, H, B, L, C, type) || !fits({B, H, L, D})) return nullptr;
+    return call(a.fn(), ptr(q), ptr(k), ptr(gq), ptr(gk), ptr(pos), ptr(freqs), ptr(qo), ptr(ko), (int)B, (int)H, (int)L,
+                (int)D, (int)axes, (const int*)pairs, (int)batches, (int)norm, eps, (int)pairing, (int)xl, (int)yl, code, s);
+}
+
+int64_t blocks(int64_t n, int64_t block) { return (n + block - 1) / block; }
+
+// fn, x, means, stream
+PyObject* block_means(Args& a) {
+    const at::Tensor* x = a.tensor(1);
+    if (!x || x->dim() != 4) return nullptr;
+    const int64_t B = x->size(0), H = x->size(1), L = x->size(2), D = x->size(3), ms[] = {B, H, blocks(L, 64), D};
+    const at::Tensor* means = a.tensor(2, ms, c10::kFloat);
+    void* s = a.stream_here(3);
+    const int code = type_code(*x);
+    if (!a.ok || code < 0 || !fits({B, H, L, D})) return nullptr;
+    return call(a.fn(), ptr(x), ptr(means), (int)B, (int)H, (int)L, (int)D, code, s);
+}
+
+// fn, q, means, mask, keep, qblock, stream
+PyObject* select_blocks(Args& a) {
+    const at::Tensor *q = a.tensor(1), *means = a.tensor(2);
+    const long long keep = a.integer(4), qblock = a.integer(5);
+    if (!a.ok || q->dim() != 4 || means->dim() != 4 || qblock < 1) return nullptr;
+    const int64_t B = q->size(0), H = q->size(1), Lq = q->size(2), D = q->size(3), NB = means->size(2);
+    const int64_t ms[] = {B, H, NB, D}, ws[] = {B, H, blocks(Lq, qblock), blocks(NB, 64)};
+    a.tensor(2, ms, c10::kFloat);
+    const at::Tensor* mask = a.tensor(3, ws, c10::kLong);
+    void* s = a.stream_here(6);
+    const int code = type_code(*q);
+    if (!a.ok || code < 0 || !fits({B, H, Lq, D, NB})) return nullptr;
+    return call(a.fn(), ptr(q), ptr(means), ptr(mask), (int)B, (int)H, (int)Lq, (int)NB, (int)D, (int)qblock, (int)keep,
+                code, s);
+}
+
+// fn, q, k, v, mask, out, scale, qblock, stream
+PyObject* sparse_forward(Args& a) {
+    const at::Tensor *q = a.tensor(1), *k = a.tensor(2);
+    const long long qblock = a.integer(7);
+    if (!a.ok || q->dim() != 4 || k->dim() != 4 || qblock < 1) return nullptr;
+    const auto type = q->scalar_type();
+    const int64_t B = q->size(0), H = q->size(1), Lq = q->size(2), D = q->size(3), Lk = k->size(2);
+    const int64_t kv[] = {B, H, Lk, D}, ws[] = {B, H, blocks(Lq, qblock), blocks(blocks(Lk, 64), 64)};
+    a.tensor(2, kv, type);
+    const at::Tensor *v = a.tensor(3, kv, type), *mask = a.tensor(4, ws, c10::kLong), *out = a.tensor(5, q->sizes(), type);
+    const float scale = a.real(6);
+    void* s = a.stream_here(8);
+    const int code = type_code(*q);
+    if (!a.ok || code < 0 || !fits({B, H, Lq, Lk, D})) return nullptr;
+    return call(a.fn(), ptr(q), ptr(k), ptr(v), ptr(mask), ptr(out), (int)B, (int)H, (int)Lq, (int)Lk, (int)D, (int)qblock,
+                scale, code, s);
+}
+
 PyObject* use_streams(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (n == 2) {
         Py_INCREF(v[0]);
@@ -304,6 +437,7 @@ PyObject* use_streams(PyObject*, PyObject* const* v, Py_ssize_t n) {
 PyMethodDef methods[] = {{"use_streams", (PyCFunction)(void (*)(void))use_streams, METH_FASTCALL, nullptr},
                          FAST(forward), FAST(forward_ex), FAST(softmax_rows), FAST(logits), FAST(softmax_pv), FAST(attention_block),
                          FAST(attention_block_kv), FAST(group_norm), FAST(geglu), FAST(conv3x3),
+                         FAST(linear_adapters), FAST(norm_rotate), FAST(block_means), FAST(select_blocks), FAST(sparse_forward),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -171,6 +171,30 @@ int check_linear(const void* x, const void* w, const void* bias, void* y, int B,
     return SDATTN_OK;
 }
 
+// fp16 or bf16
+int check_16bit(int dtype) {
+    if (dtype == SDATTN_F16 || dtype == SDATTN_BF16) return SDATTN_OK;
+    return dtype == SDATTN_F32 ? SDATTN_ERR_UNSUPPORTED : SDATTN_ERR_INVALID_ARG;
+}
+
+bool is_layout(int layout) { return layout == SDATTN_ROWS || layout == SDATTN_HEADS; }
+
+// whether [p, p + n) meets any of the inputs, of which absent ones are NULL
+struct Span {
+    const void* p;
+    unsigned long long n;
+};
+bool meets(const void* p, unsigned long long n, std::initializer_list<Span> inputs) {
+    for (const Span& s : inputs)
+        if (s.p && overlap(p, n, s.p, s.n)) return true;
+    return false;
+}
+
+// blocks of a sequence, and the words of a mask row over NB blocks
+constexpr int kMaxSparseLength = 1 << 30;
+int blocks_of(int L, int block) { return (L + block - 1) / block; }
+int mask_words(int nb) { return (nb + 63) / 64; }
+
 // Q, K, V (heads layout) and O (heads merged), each rounded up to 256 bytes
 long long block_part(long long elems) { return (2 * elems + 255) / 256 * 256; }
 
@@ -250,6 +274,140 @@ int sdattn_linear(const void* x, const void* w, const void* bias, void* y, int B
     if (st != SDATTN_OK) return st;
     (void)hipGetLastError();
     return finish(sdattn::launch_linear(args));
+}
+
+long long sdattn_linear_adapters_workspace(int B, int L, int R) {
+    if (B < 1 || L < 1 || R < 1 || R > 65536) return -1;
+    const long long n = checked_mul({B, L, sdattn::adapter_rank_padded(R)});
+    return n < 0 ? -1 : block_part(n);
+}
+
+int sdattn_linear_adapters(const void* x, const void* w, const void* bias, const void* down,
+                           const void* up, const int* ids, const float* scales, void* y,
+                           void* workspace, long long workspace_bytes, int B, int L, int K, int N,
+                           int R, int A, int H, sdattn_layout x_layout, sdattn_layout y_layout,
+                           sdattn_dtype dtype, void* stream) {
+    if (!down || !up || !ids || !workspace) return SDATTN_ERR_INVALID_ARG;
+    if (R < 1 || A < 1) return SDATTN_ERR_INVALID_ARG;
+    sdattn::LinearArgs args;
+    const int st = check_linear(x, w, bias, y, B, L, K, N, H, (int)x_layout, (int)y_layout,
+                                (int)dtype, stream, &args);
+    if (st != SDATTN_OK) return st;
+    const long long need = sdattn_linear_adapters_workspace(B, L, R);
+    const long long nd = checked_mul({A, R, K}), nu = checked_mul({A, N, R});
+    // a workgroup takes 16 rows of an item
+    if (need < 0 || nd < 0 || nu < 0 || (long long)B * ((L + 15) / 16) > INT_MAX) return SDATTN_ERR_UNSUPPORTED;
+    if (workspace_bytes < need) return SDATTN_ERR_INVALID_ARG;
+    if (!aligned(down, 16) || !aligned(up, 16) || !aligned(workspace, 16) || !aligned(ids, 4) ||
+        (scales && !aligned(scales, 4)))
+        return SDATTN_ERR_MISALIGNED;
+    const unsigned long long xb = 2ULL * B * L * K, yb = 2ULL * B * L * N, wb = 2ULL * N * K;
+    const std::initializer_list<Span> more = {{down, 2ULL * nd}, {up, 2ULL * nu}, {ids, 4ULL * B}, {scales, 4ULL * A}};
+    if (meets(y, yb, more) || meets(workspace, (unsigned long long)need, more) ||
+        meets(workspace, (unsigned long long)need, {{x, xb}, {w, wb}, {bias, 2ULL * N}, {y, yb}}))
+        return SDATTN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    return finish(sdattn::launch_linear_adapters(args, {down, up, ids, scales, workspace, R, A}));
+}
+
+int sdattn_norm_rotate(const void* q, const void* k, const void* gamma_q, const void* gamma_k,
+                       const int* pos, const float* freqs, void* qo, void* ko, int B, int H, int L,
+                       int D, int axes, const int* pairs, int pos_batches, sdattn_norm norm,
+                       float eps, sdattn_pairing pairing, sdattn_layout x_layout,
+                       sdattn_layout y_layout, sdattn_dtype dtype, void* stream) {
+    if (!q || !qo || !k != !ko) return SDATTN_ERR_INVALID_ARG;
+    if (B < 1 || H < 1 || L < 1 || D < 1 || axes < 0) return SDATTN_ERR_INVALID_ARG;
+    if (!is_layout((int)x_layout) || !is_layout((int)y_layout)) return SDATTN_ERR_INVALID_ARG;
+    if ((norm != SDATTN_NORM_NONE && norm != SDATTN_NORM_RMS) ||
+        (pairing != SDATTN_PAIR_ADJACENT && pairing != SDATTN_PAIR_HALVES))
+        return SDATTN_ERR_INVALID_ARG;
+    if (!isfinite(eps) || eps < 0.0f) return SDATTN_ERR_INVALID_ARG;
+    const int st = check_16bit((int)dtype);
+    if (st != SDATTN_OK) return st;
+    if (D % 8 != 0 || D > 256 || axes > 4) return SDATTN_ERR_UNSUPPORTED;
+    sdattn::NormRotateArgs a{q, k, gamma_q, gamma_k, pos, freqs, qo, ko, B, H, L, D, axes, {0, 0, 0, 0}, 1,
+                             x_layout == SDATTN_HEADS, y_layout == SDATTN_HEADS, norm == SDATTN_NORM_RMS,
+                             pairing == SDATTN_PAIR_HALVES, eps, (int)dtype, stream};
+    long long P = 0;
+    if (axes > 0) {
+        if (!pos || !freqs || !pairs) return SDATTN_ERR_INVALID_ARG;
+        if (pos_batches != 1 && pos_batches != B) return SDATTN_ERR_INVALID_ARG;
+        a.pos_batches = pos_batches;
+        for (int i = 0; i < axes; ++i) {
+            a.pairs[i] = pairs[i];
+            if (pairs[i] < 1) return SDATTN_ERR_INVALID_ARG;
+            P += pairs[i];
+        }
+        if (P > D / 2) return SDATTN_ERR_INVALID_ARG;
+    }
+    const long long n = checked_mul({B, H, L, D});
+    if (n < 0 || (long long)B * L > INT_MAX / 2 || (long long)H * 16 > INT_MAX / 2) return SDATTN_ERR_UNSUPPORTED;
+    if (!aligned(q, 16) || !aligned(qo, 16) || (k && (!aligned(k, 16) || !aligned(ko, 16))) ||
+        (gamma_q && !aligned(gamma_q, 8)) || (gamma_k && !aligned(gamma_k, 8)) ||
+        (axes > 0 && (!aligned(pos, 4) || !aligned(freqs, 4))))
+        return SDATTN_ERR_MISALIGNED;
+    const unsigned long long nb = 2ULL * n, pb = 4ULL * a.pos_batches * L * axes;
+    const bool same = x_layout == y_layout;
+    const std::initializer_list<Span> small = {{gamma_q, 2ULL * D}, {gamma_k, 2ULL * D}, {axes > 0 ? pos : nullptr, pb},
+                                               {axes > 0 ? freqs : nullptr, 4ULL * P}};
+    // in place or clear of each other
+    if (!(same && qo == q) && overlap(qo, nb, q, nb)) return SDATTN_ERR_INVALID_ARG;
+    if (meets(qo, nb, small) || meets(qo, nb, {{k, nb}, {ko, nb}})) return SDATTN_ERR_INVALID_ARG;
+    if (k) {
+        if (!(same && ko == k) && overlap(ko, nb, k, nb)) return SDATTN_ERR_INVALID_ARG;
+        if (meets(ko, nb, small) || overlap(ko, nb, q, nb)) return SDATTN_ERR_INVALID_ARG;
+    }
+    (void)hipGetLastError();
+    return finish(sdattn::launch_norm_rotate(a));
+}
+
+int sdattn_block_means(const void* x, float* means, int B, int H, int L, int D, sdattn_dtype dtype,
+                       void* stream) {
+    if (!x || !means) return SDATTN_ERR_INVALID_ARG;
+    if (B < 1 || H < 1 || L < 1 || D < 1) return SDATTN_ERR_INVALID_ARG;
+    const int st = check_16bit((int)dtype);
+    if (st != SDATTN_OK) return st;
+    if (D % 8 != 0 || D > 256 || L > kMaxSparseLength) return SDATTN_ERR_UNSUPPORTED;
+    const int nb = blocks_of(L, SDATTN_SPARSE_BLOCK);
+    const long long nx = checked_mul({B, H, L, D}), nm = checked_mul({B, H, nb, D});
+    if (nx < 0 || nm < 0 || checked_mul({B, H, nb}) > INT_MAX) return SDATTN_ERR_UNSUPPORTED;
+    if (!aligned(x, 16) || !aligned(means, 16)) return SDATTN_ERR_MISALIGNED;
+    if (overlap(means, 4ULL * nm, x, 2ULL * nx)) return SDATTN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    return finish(sdattn::launch_block_means({x, means, B, H, L, D, (int)dtype, stream}));
+}
+
+int sdattn_select_blocks(const void* q, const float* means, void* mask, int B, int H, int Lq, int NB,
+                         int D, int qblock, int keep, sdattn_dtype dtype, void* stream) {
+    if (!q || !means || !mask) return SDATTN_ERR_INVALID_ARG;
+    if (B < 1 || H < 1 || Lq < 1 || NB < 1 || D < 1 || keep < 1) return SDATTN_ERR_INVALID_ARG;
+    if (qblock != 64 && qblock != 128) return SDATTN_ERR_INVALID_ARG;
+    const int st = check_16bit((int)dtype);
+    if (st != SDATTN_OK) return st;
+    if (D % 8 != 0 || D > 256 || Lq > kMaxSparseLength || NB > sdattn::kSelectMaxBlocks) return SDATTN_ERR_UNSUPPORTED;
+    const int nq = blocks_of(Lq, qblock), nw = mask_words(NB);
+    const long long nx = checked_mul({B, H, Lq, D}), nm = checked_mul({B, H, NB, D}), nk = checked_mul({B, H, nq, nw});
+    if (nx < 0 || nm < 0 || nk < 0 || checked_mul({B, H, nq}) > INT_MAX) return SDATTN_ERR_UNSUPPORTED;
+    if (!aligned(q, 16) || !aligned(means, 16) || !aligned(mask, 8)) return SDATTN_ERR_MISALIGNED;
+    if (meets(mask, 8ULL * nk, {{q, 2ULL * nx}, {means, 4ULL * nm}})) return SDATTN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    return finish(sdattn::launch_select_blocks({q, means, mask, B, H, Lq, NB, D, qblock, keep, (int)dtype, stream}));
+}
+
+int sdattn_sparse_forward(const void* q, const void* k, const void* v, const void* mask, void* out,
+                          int B, int H, int Lq, int Lk, int D, int qblock, float scale,
+                          sdattn_dtype dtype, void* stream) {
+    if (!mask || (qblock != 64 && qblock != 128)) return SDATTN_ERR_INVALID_ARG;
+    if (Lq > kMaxSparseLength || Lk > kMaxSparseLength) return SDATTN_ERR_UNSUPPORTED;
+    const int st = check_attention(q, k, v, out, nullptr, B, H, Lq, Lk, D, scale, (int)dtype);
+    if (st != SDATTN_OK) return st;
+    if (!sdattn::sparse_width(D)) return SDATTN_ERR_UNSUPPORTED;
+    const long long nk = checked_mul({B, H, blocks_of(Lq, qblock), mask_words(blocks_of(Lk, SDATTN_SPARSE_BLOCK))});
+    if (nk < 0) return SDATTN_ERR_UNSUPPORTED;
+    if (!aligned(mask, 8)) return SDATTN_ERR_MISALIGNED;
+    if (overlap(out, 2ULL * B * H * Lq * D, mask, 8ULL * nk)) return SDATTN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    return finish(sdattn::launch_attn_sparse({q, k, v, mask, out, B, H, Lq, Lk, D, qblock, scale, (int)dtype, stream}));
 }
 
 long long sdattn_attention_block_workspace(int B, int Lq, int Lk, int C) {

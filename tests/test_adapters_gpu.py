@@ -1,0 +1,152 @@
+"""Projections with low-rank adapters of many requests against the 64-bit form: ranks
+that are and are not multiples of 8 and 16, requests of one token, of a few and of many
+tiles, requests without an adapter or sharing one, every layout pair and type."""
+import numpy as np
+import pytest
+
+import operators_ref as ref
+import paper_2304_11267_amd as sd
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _needs_gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    sd.load_library()
+
+
+def make(B, L, K, N, R, A, dtype, seed, bias=True, scales=True):
+    import torch
+    g = ref.generator(seed)
+    t = dict(x=ref.randn(g, B, L, K, dtype=dtype), w=ref.randn(g, N, K, dtype=dtype, sigma=K ** -0.5),
+             down=ref.randn(g, A, R, K, dtype=dtype, sigma=K ** -0.5), up=ref.randn(g, A, N, R, dtype=dtype),
+             bias=ref.randn(g, N, dtype=dtype) if bias else None,
+             scales=torch.rand(A, device="cuda", generator=g) * 2 - 0.5 if scales else None)
+    ids = np.random.default_rng(seed).integers(-1, A + 1, B).astype(np.int32)   # -1 and A: none
+    t["ids"] = torch.from_numpy(ids).cuda()
+    return t
+
+
+def call(t, y, heads=1, xl=0, yl=0, ws=None):
+    import torch
+    B, L = (t["x"].shape[0], t["x"].shape[2 if xl else 1])
+    if ws is None:
+        ws = torch.empty(sd.linear_adapters_workspace(B, L, t["down"].shape[1]), dtype=torch.uint8, device="cuda")
+    return sd.linear_adapters(t["x"], t["w"], y, t["down"], t["up"], t["ids"], ws, scales=t["scales"], bias=t["bias"],
+                              heads=heads, x_layout=xl, y_layout=yl)
+
+
+def expected(t, dtype, x=None):
+    h = {n: None if t[n] is None else ref.host(t[n]) for n in ("w", "down", "up", "bias", "scales")}
+    return ref.adapters(ref.host(t["x"]) if x is None else x, h["w"], h["bias"], h["down"], h["up"],
+                        t["ids"].cpu().numpy(), h["scales"], dtype)
+
+
+def check(g, r, off, dtype):
+    bound = off + ref.half_step(g, r, dtype) * (1 + 2.0 ** -10)
+    assert np.all(np.abs(g - r) <= bound), float(np.max(np.abs(g - r) / bound))
+
+
+# (B, L, K, N, R, A)
+SHAPES = [
+    (1, 1, 8, 8, 1, 1), (5, 1, 320, 64, 4, 3), (16, 1, 1280, 1280, 8, 16), (70, 1, 328, 320, 12, 5),
+    (3, 7, 768, 640, 16, 2), (9, 31, 520, 72, 20, 4), (2, 32, 1288, 136, 33, 3), (4, 77, 768, 320, 64, 4),
+    (2, 130, 40, 200, 128, 2), (3, 257, 320, 320, 16, 2), (2, 1100, 648, 640, 8, 3), (1, 33, 64, 96, 300, 1),
+    (6, 500, 320, 960, 32, 2), (140, 3, 640, 320, 5, 7),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_matches_the_formula(shape, dtype):
+    import torch
+    B, L, K, N, R, A = shape
+    t = make(*shape, dtype, 31 + B + L + K + N + R, bias=R % 2 == 0, scales=L != 7)
+    y = torch.full((B, L, N), 7.0, dtype=ref.t_type(dtype), device="cuda")
+    call(t, y)
+    torch.cuda.synchronize()
+    check(ref.host(y), *expected(t, dtype), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("xl,yl", [(0, 1), (1, 0), (1, 1)], ids=["rows_heads", "heads_rows", "heads_heads"])
+@pytest.mark.parametrize("shape", [(5, 1, 320, 160, 4, 3), (3, 100, 768, 640, 16, 2), (2, 33, 64, 1280, 24, 2)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_layouts(shape, xl, yl, dtype):
+    import torch
+    B, L, K, N, R, A = shape
+    H = 4
+    t = make(*shape, dtype, 77 + L + K)
+    x = ref.host(t["x"])
+    if xl:
+        t["x"] = t["x"].view(B, L, H, K // H).transpose(1, 2).contiguous()
+    y = torch.full((B, H, L, N // H) if yl else (B, L, N), 7.0, dtype=ref.t_type(dtype), device="cuda")
+    call(t, y, H, xl, yl)
+    torch.cuda.synchronize()
+    g = ref.host(y)
+    check(ref.heads_to_rows(g) if yl else g, *expected(t, dtype, x), dtype)
+
+
+@pytest.mark.parametrize("shape", [(6, 1, 1280, 320, 8, 2), (3, 90, 320, 320, 16, 2), (2, 600, 640, 640, 4, 2)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_no_adapter_gives_the_plain_projections_bits(shape):
+    """Requests without an adapter, beside ones that have it, and values of adapters that
+    no request names are not read."""
+    import torch
+    B, L, K, N, R, A = shape
+    t = make(*shape, "f16", 5)
+    t["ids"] = torch.arange(B, dtype=torch.int32, device="cuda") % 2 - 1   # -1, 0, -1, ...
+    t["down"][1] = float("nan")
+    t["up"][1] = float("inf")
+    y, plain = (torch.empty(B, L, N, dtype=torch.float16, device="cuda") for _ in range(2))
+    sd.linear(t["x"], t["w"], plain, bias=t["bias"])
+    call(t, y)
+    torch.cuda.synchronize()
+    assert torch.equal(y[0::2], plain[0::2])
+    assert torch.isfinite(y).all() and not torch.equal(y[1], plain[1])
+
+
+def test_large_values_of_one_request_stay_in_it():
+    """An adapter that overflows its own request's rows leaves the neighbours in a tile alone."""
+    import torch
+    t = make(8, 5, 320, 128, 8, 8, "f16", 6)
+    t["ids"] = torch.arange(8, dtype=torch.int32, device="cuda")
+    t["up"][3] = float("inf")
+    t["down"][5] = float("nan")
+    y = torch.empty(8, 5, 128, dtype=torch.float16, device="cuda")
+    call(t, y)
+    torch.cuda.synchronize()
+    ok = [0, 1, 2, 4, 6, 7]
+    assert torch.isfinite(y[ok]).all() and not torch.isfinite(y[3]).all() and torch.isnan(y[5]).all()
+
+
+def test_writes_its_rows_alone_and_the_workspace_it_asked_for():
+    import torch
+    t = make(3, 21, 328, 72, 20, 2, "f16", 8)
+    need = sd.linear_adapters_workspace(3, 21, 20)
+    ws = torch.full((need + 512,), 9, dtype=torch.uint8, device="cuda")
+    buf = torch.full((3 * 21 * 72 + 64,), 7.0, dtype=torch.float16, device="cuda")
+    call(t, buf[:3 * 21 * 72].view(3, 21, 72), ws=ws[:need])
+    torch.cuda.synchronize()
+    assert (buf[3 * 21 * 72:] == 7).all() and (ws[need:] == 9).all()
+
+
+@pytest.mark.parametrize("B,L,K,N", [(4, 40, 640, 320), (90, 40, 584, 640), (300, 1, 1280, 640), (300, 1, 320, 640)],
+                         ids=lambda v: str(v))
+def test_a_requests_bits_do_not_depend_on_the_others(B, L, K, N):
+    """One request alone (the split kernel past 512 channels), and among others with other
+    adapters (the shared tiles where they are many)."""
+    import torch
+    t = make(B, L, K, N, 16, 3, "bf16", 9)
+    t["ids"] = (torch.arange(B, dtype=torch.int32, device="cuda") + 2) % 3
+    y = torch.empty(B, L, N, dtype=torch.bfloat16, device="cuda")
+    call(t, y)
+    for b in (0, 1, 2, B - 1):
+        one = dict(t, x=t["x"][b:b + 1].contiguous(), ids=t["ids"][b:b + 1].contiguous())
+        alone = torch.empty(1, L, N, dtype=torch.bfloat16, device="cuda")
+        call(one, alone)
+        torch.cuda.synchronize()
+        assert torch.equal(alone[0], y[b]), b
