@@ -218,7 +218,7 @@ int sdattn_linear_adapters(const void *x, const void *w, const void *bias, const
  *             batch items have the same positions; freqs [P] fp32
  *   pairs     `axes` integers in HOST memory, read during the call
  *
- * Requirements: D % 8 == 0, D <= 256; 0 <= axes <= 4 (with none, pos, freqs and pairs
+ * Requirements: D % 8 == 0, D <= 256; H <= 65536; 0 <= axes <= 4 (with none, pos, freqs and pairs
  * are not looked at); pairs >= 1, P <= D / 2; eps finite and >= 0; q, k, qo, ko 16-byte
  * aligned, gammas 8-byte, pos and freqs 4-byte; no output may overlap another
  * argument otherwise.

@@ -341,7 +341,7 @@ int sdattn_norm_rotate(const void* q, const void* k, const void* gamma_q, const 
         if (P > D / 2) return SDATTN_ERR_INVALID_ARG;
     }
     const long long n = checked_mul({B, H, L, D});
-    if (n < 0 || (long long)B * L > INT_MAX / 2 || (long long)H * 16 > INT_MAX / 2) return SDATTN_ERR_UNSUPPORTED;
+    if (n < 0 || (long long)B * L > INT_MAX / 2 || H > 65536) return SDATTN_ERR_UNSUPPORTED;
     if (!aligned(q, 16) || !aligned(qo, 16) || (k && (!aligned(k, 16) || !aligned(ko, 16))) ||
         (gamma_q && !aligned(gamma_q, 8)) || (gamma_k && !aligned(gamma_k, 8)) ||
         (axes > 0 && (!aligned(pos, 4) || !aligned(freqs, 4))))
