@@ -223,6 +223,21 @@ def test_choice(Lq, nb, D, keep, qblock, dtype):
     assert np.array_equal(sel, want)
 
 
+@pytest.mark.parametrize("qblock", [64, 128])
+@pytest.mark.parametrize("nb,D,keep,dtype", [(19, 40, 5, "f16"), (100, 8, 30, "bf16"), (257, 256, 100, "f16"),
+                                             (600, 160, 77, "bf16"), (1100, 72, 300, "f16"), (4000, 64, 64, "bf16")],
+                         ids=lambda v: str(v))
+def test_choice_for_many_queries(nb, D, keep, dtype, qblock):
+    """More query blocks than two for each CU: several of them a workgroup."""
+    import torch
+    g = ref.generator(nb + D)
+    B, H, Lq = 7, 8, 10 * qblock + 3
+    q = ref.randn(g, B, H, Lq, D, dtype=dtype)
+    means = torch.randn(B, H, nb, D, device="cuda", generator=g)
+    sel = choose(q, means, keep, qblock)
+    assert np.array_equal(sel, ref.select(f32(ref.block_means(ref.host(q), qblock)), ref.host(means), keep))
+
+
 @pytest.mark.parametrize("nb,keep", [(4096, 100), (4097, 37), (16384, 4000)])
 def test_choice_among_many(nb, keep):
     import torch
