@@ -113,12 +113,21 @@ struct AdapterSet {
 __device__ __forceinline__ AdapterSet adapters_of() { return AdapterSet{}; }
 __device__ __forceinline__ AdapterSet adapters_of(const AdapterSet& a) { return a; }
 
-// Ranks r0 .. r0 + 7 of an adapter's row of R, zeros from R on; rows of whole 16-byte
-// chunks are read as such.
+// Ranks r0 .. r0 + 7 of an adapter's row of R, zeros from R on, in reads of W values (R is
+// a multiple of W).
+template <int W>
 __device__ __forceinline__ u32x4 adapter_chunk(const uint16_t* row, int r0, int R) {
     u32x4 v = {0u, 0u, 0u, 0u};
-    if (R % 8 == 0) {
+    if constexpr (W == 8) {
         if (r0 < R) v = *(const u32x4*)(row + r0);
+    } else if constexpr (W == 4) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (r0 + 4 * e < R) {
+                const u32x2 w = *(const u32x2*)(row + r0 + 4 * e);
+                v[2 * e] = w[0];
+                v[2 * e + 1] = w[1];
+            }
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -127,26 +136,69 @@ __device__ __forceinline__ u32x4 adapter_chunk(const uint16_t* row, int r0, int 
     return v;
 }
 
-// acc[b] += up T^T for the 32 token rows from row0 and the 32 channels from n0 + 32 b,
-// 16 ranks a step.  The rows of one batch item at a time, summed apart and added to its
-// rows alone: other requests' rows see nothing of an adapter, not even its infinities,
-// and a request's bits do not depend on its neighbours in a tile.
-template <int ET, int NB>
-__device__ __forceinline__ void add_adapters(const AdapterSet& ad, int row0, int n0, int M, int N, int L,
-                                             f32x16 (&acc)[NB]) {
-    if (row0 >= M) return;
+// c + the product of 8 pairs of 16-bit values (v_dot2_f32_f16 / v_dot2_f32_bf16)
+template <int ET>
+__device__ __forceinline__ float dot8(u32x4 a, u32x4 b, float c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (ET == kF16) {
+            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+            c = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, (uint32_t)a[i]), __builtin_bit_cast(h2, (uint32_t)b[i]), c, false);
+        } else {
+            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+            c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, (uint32_t)a[i]), __builtin_bit_cast(b2, (uint32_t)b[i]), c, false);
+        }
+    }
+    return c;
+}
+
+// sum[b] = up T^T for the 32 token rows from row0 and the 32 channels from n0 + 32 b, in the
+// accumulators' layout; it is the first addend of those channels' sums.  Every row sees its
+// own request's adapter alone, infinities and all, and a request's bits do not depend on its
+// neighbours in a tile.
+//   Requests of 32 rows and more: 16 ranks a step on the matrix core, one request's rows at
+// a time (at most two in 32 rows), the others' T as zeros and their sums dropped.
+//   Shorter ones: each lane multiplies its row's T with its own channels' rows of up (16
+// tokens of 16 requests, K = N = 1280, R = 8: one request after the other took 9 us more).
+constexpr int kAdapterRows = 32;
+template <int ET, int NB, int W>
+__device__ __forceinline__ void adapter_sums_w(const AdapterSet& ad, int row0, int n0, int M, int N, int L,
+                                               f32x16 (&sum)[NB]) {
     const int l32 = lane_id() & 31, half = lane_id() >> 5;
     const int row = min(row0 + l32, M - 1);
+    if (L < kAdapterRows) {
+        const int id = ad.ids[row / L];
+        if (id < 0 || id >= ad.count) return;
+        const uint16_t* up = ad.up + (size_t)id * N * ad.R;
+        for (int r0 = 0; r0 < ad.R; r0 += 8) {
+            const u32x4 tf = *(const u32x4*)(ad.t + (size_t)row * ad.Rp + r0);
+#pragma unroll
+            for (int t = 0; t < 2 * NB; ++t) {   // 8 channels at a time, two groups of 4
+                u32x4 u[8];
+#pragma unroll
+                for (int r = 0; r < 8; r += 4) {
+                    const uint16_t* p = up + (size_t)min(n0 + 16 * t + 2 * r + 4 * half, N - 4) * ad.R;
+                    asm volatile("" : "+v"(p));   // (kept across steps, the rows' addresses take 64 registers)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[r + e] = adapter_chunk<W>(p + e * ad.R, r0, ad.R);
+                }
+#pragma unroll
+                for (int r = 0; r < 8; ++r) sum[t / 2][8 * (t & 1) + r] = dot8<ET>(u[r], tf, sum[t / 2][8 * (t & 1) + r]);
+                __builtin_amdgcn_sched_barrier(0);   // (all of them at once take 290 registers)
+            }
+        }
+        return;
+    }
     const int last = min(row0 + 31, M - 1) / L;
     for (int b = row0 / L; b <= last; ++b) {
         const int id = __builtin_amdgcn_readfirstlane(ad.ids[b]);
         if (id < 0 || id >= ad.count) continue;
         const bool mine = (long long)row >= (long long)b * L && (long long)row < (long long)(b + 1) * L;
-        f32x16 sum[NB];
+        f32x16 own[NB];
 #pragma unroll
         for (int t = 0; t < NB; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum[t][r] = 0.0f;
+            for (int r = 0; r < 16; ++r) own[t][r] = 0.0f;
         for (int s = 0; s < ad.Rp / 16; ++s) {
             const int r0 = 16 * s + 8 * half;
             u32x4 tf = {0u, 0u, 0u, 0u};
@@ -154,14 +206,26 @@ __device__ __forceinline__ void add_adapters(const AdapterSet& ad, int row0, int
 #pragma unroll
             for (int t = 0; t < NB; ++t) {
                 const int n = min(n0 + 32 * t + l32, N - 1);
-                sum[t] = mfma32x32x16<ET>(adapter_chunk(ad.up + ((size_t)id * N + n) * ad.R, r0, ad.R), tf, sum[t]);
+                own[t] = mfma32x32x16<ET>(adapter_chunk<W>(ad.up + ((size_t)id * N + n) * ad.R, r0, ad.R), tf, own[t]);
             }
         }
 #pragma unroll
         for (int t = 0; t < NB; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[t][r] += mine ? sum[t][r] : 0.0f;
+            for (int r = 0; r < 16; ++r) sum[t][r] = mine ? own[t][r] : sum[t][r];
     }
+}
+template <int ET, int NB>
+__device__ __forceinline__ void adapter_sums(const AdapterSet& ad, int row0, int n0, int M, int N, int L,
+                                             f32x16 (&sum)[NB]) {
+#pragma unroll
+    for (int t = 0; t < NB; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[t][r] = 0.0f;
+    if (row0 >= M) return;
+    if (ad.R % 8 == 0) adapter_sums_w<ET, NB, 8>(ad, row0, n0, M, N, L, sum);
+    else if (ad.R % 4 == 0) adapter_sums_w<ET, NB, 4>(ad, row0, n0, M, N, L, sum);
+    else adapter_sums_w<ET, NB, 1>(ad, row0, n0, M, N, L, sum);
 }
 
 // Wait until at most `ahead` slices of this wave's copies are still in flight.
@@ -318,6 +382,8 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     // 7.2 / 7.5 us (7.9 with them in the loop of every slice), 1024x1280x1280 11.3 /
     // 11.4 (12.0), 2048x2560x640 19.4 / 19.0 (20.0).
     f32x16 acc[2] = {zero, zero}, tot[2] = {zero, zero};
+    // the adapters' part comes first, while the first slices are on their way
+    if constexpr (sizeof...(AD) > 0) adapter_sums<ET>(adapters_of(ad...), m0 + 32 * wave, n0, M, N, L, FOLD ? tot : acc);
     const int run = K > kSplitMinK ? (nk + kRuns - 1) / kRuns : nk;
     if constexpr (!FOLD) {
         // (a loop of its own: as slices opened by a run's first one, products with a
@@ -354,7 +420,7 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     } else
     for (int i0 = 0; i0 < nk; i0 += run) {
         slice(i0, std::true_type{}, acc, [&]() __attribute__((always_inline)) {
-            if (i0 > 0) {
+            if (i0 > 0) {   // (tot is zero, or the adapters' part, before)
                 __builtin_amdgcn_sched_barrier(0);
                 tot[0] += acc[0];
                 tot[1] += acc[1];
@@ -363,8 +429,6 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
         });
         for (int i = i0 + 1; i < min(i0 + run, nk); ++i) slice(i, std::false_type{}, acc, [] {});
     }
-
-    if constexpr (sizeof...(AD) > 0) add_adapters<ET>(adapters_of(ad...), m0 + 32 * wave, n0, M, N, L, acc);
 
     // Stage the 128 x 64 output tile (bias added, rounded) in LDS, rows of
     // kOutStride bytes: lane (l32, half) holds channels 32t + 8g + 4*half + (0..3)
@@ -453,7 +517,7 @@ __device__ __forceinline__ void ks_wait(int n) {
 }
 
 template <int ET, bool YH, int TM, int TN, int ST, typename... AD>
-__global__ __launch_bounds__(256) void linear_ksplit_kernel(const LinGroup grp, const AD... ad) {
+__global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_kernel(const LinGroup grp, const AD... ad) {
     using G = KsGeom<TM, TN, ST>;
     constexpr int MB = TM / 32, NB = TN / 32, KS = kBK / 16;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -522,6 +586,14 @@ __global__ __launch_bounds__(256) void linear_ksplit_kernel(const LinGroup grp, 
     for (int i = 0; i < ST; ++i)
         if (i < count) issue(i);
 
+    [[maybe_unused]] f32x16 more[MB][NB];   // the adapters' part, while the first slices are on their way
+    if constexpr (sizeof...(AD) > 0) {
+        if (wave == 0) {
+#pragma unroll
+            for (int a = 0; a < MB; ++a) adapter_sums<ET>(adapters_of(ad...), m0 + 32 * a, n0, M, N, L, more[a]);
+        }
+    }
+
     for (int i = 0; i < count; ++i) {
         ks_wait<G::kCopies, ST - 1>(count - 1 - i);
         const char* st = ring + (i % ST) * G::kSlice;
@@ -555,12 +627,14 @@ __global__ __launch_bounds__(256) void linear_ksplit_kernel(const LinGroup grp, 
                 for (int b = 0; b < NB; ++b) acc[a][b] = mfma32x32x16<ET>(wf[b][s], xf[a][s], acc[a][b]);
     }
 
-    // the adapters' steps follow the last channels, as in the shared tiles (and so have
-    // the same bits)
+    // the adapters' part is added to the first run, in the order of the shared tiles' sums
+    // (and so with the same bits)
     if constexpr (sizeof...(AD) > 0) {
-        if (wave == (ns - 1) / per) {
+        if (wave == 0) {
 #pragma unroll
-            for (int a = 0; a < MB; ++a) add_adapters<ET>(adapters_of(ad...), m0 + 32 * a, n0, M, N, L, acc[a]);
+            for (int a = 0; a < MB; ++a)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) acc[a][b] = more[a][b] + acc[a][b];
         }
     }
 
