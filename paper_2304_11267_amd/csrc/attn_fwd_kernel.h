@@ -106,6 +106,20 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
     constexpr int kThreads = G::kThreads;
     constexpr int TB = G::kTileBytes;
 
+    // SPARSE: where a tile's rows start in the same LDS banks every 16 / kSw rows (kSw > 1),
+    // their 16-byte chunks lie permuted, chunk c of row r in the place of chunk c ^ chunk_swap(r), so that
+    // 16 rows' equal chunks fall into different banks.  (D = 128's rows all start
+    // in the same banks: 17550 tokens, 40 blocks for 128 queries, 16 heads, bf16 925 us
+    // without, 443 with; D = 64's every second: 16384 tokens, 32 blocks, 8 heads 91 and 80.)
+    constexpr int kSw = SPARSE ? (D / 8) & -(D / 8) & 31 : 1;
+    constexpr int kSwap = kSw > 16 ? 16 : kSw;
+    auto chunk_swap = [](int row) __attribute__((always_inline)) { return kSwap > 1 ? row / (16 / kSwap) & (kSwap - 1) : 0; };
+    // (c + o) ^ x for constants c and chunks o and swaps x of a lane, where c + o has no carry:
+    // what c has above kSwap stays a constant of the address
+    auto swapped_at = [](int c, int o, int x) __attribute__((always_inline)) {
+        return (c & -kSwap) + (((c & (kSwap - 1)) + o) ^ x);
+    };
+
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
     const int tid = threadIdx.x;
@@ -148,23 +162,41 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
         return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)word, i) |
                (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(word >> 32), i) << 32;
     };
-    // bits set in the words of the lanes up to this one
+    // bits set in the words of the lanes up to this one: sums over 1, 2, 4 and 8 lanes of a
+    // row of 16 (row_shr), then row 0 onto 1 and 2 onto 3, and both onto the last two
     [[maybe_unused]] auto bits_upto = [&]() __attribute__((always_inline)) -> int {
         int n = __popcll(word);
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int below = __shfl_up(n, o, 64);
-            n += lane >= o ? below : 0;
-        }
+        n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xf, 0xf, true);
+        n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xf, 0xf, true);
+        n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xf, 0xf, true);
+        n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xf, 0xf, true);
+        n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xa, 0xf, false);
+        n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xc, 0xf, false);
         return n;
     };
+
+    // Q^T operand of block j: lane holds query q0 + 32j + l32, d = 16s + 8*half .. +7.
+    auto q_value = [&](int j, int s) __attribute__((always_inline)) {
+        const int qrow = q0 + 32 * j + l32;
+        const int d0 = 16 * s + 8 * half;
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (qrow < Lq && d0 < D) v = *(const u32x4*)(Q + ((size_t)bh * Lq + qrow) * D + d0);
+        if (neg) v ^= 0x80008000u;   // fold a negative scale into Q (exact)
+        return v;
+    };
+    [[maybe_unused]] u32x4 q_early[QB][DK];
     if constexpr (SPARSE) {
-        ntiles = 0;
-        for (part = 0; part * 64 < mask.nw; ++part) {
+        load_words();
+#pragma unroll
+        for (int j = 0; j < QB; ++j)
+#pragma unroll
+            for (int s = 0; s < DK; ++s) q_early[j][s] = q_value(j, s);   // on their way before the words are looked at
+        ntiles = __builtin_amdgcn_readlane(bits_upto(), 63);
+        while ((part + 1) * 64 < mask.nw) {
+            ++part;
             load_words();
             ntiles += __builtin_amdgcn_readlane(bits_upto(), 63);
         }
-        --part;   // the last words are in the lanes
         ragged = Lk % kTK != 0 && (word_of((mask.nw - 1) % 64) >> (nblocks - 1) % 64 & 1);
         if (ntiles == 0) {   // nothing to attend to
             if (kh == 0)
@@ -184,8 +216,9 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
     // the cursor to bit t_first
     [[maybe_unused]] auto seek = [&]() __attribute__((always_inline)) {
         int before = 0;
+        const bool first = part == 0;   // whose words are in the lanes already
         for (part = 0; part * 64 < mask.nw; ++part) {
-            load_words();
+            if (part > 0 || !first) load_words();
             const int upto = before + bits_upto();
             const uint64_t past = __ballot(upto > t_first);
             if (past) {
@@ -230,12 +263,21 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
             tile_off = lane * 16;
             last = (uint32_t)min(Lk - j * kTK, kTK) * (2 * D) - 16;
         }
+        // the chunk that belongs into this lane's place of piece i of a tile
+        [[maybe_unused]] int l64 = lane;
+        if constexpr (kSwap > 1) asm volatile("" : "+v"(l64));   // (all pieces' places, kept from tile to tile, would be spilled)
+        [[maybe_unused]] auto swapped = [&](int i) __attribute__((always_inline)) -> uint32_t {
+            constexpr uint32_t C = D / 8;
+            const uint32_t q = i * 64 + l64, row = q / C;
+            return (row * C + ((q - row * C) ^ (uint32_t)chunk_swap(row))) * 16;
+        };
 #pragma unroll
         for (int i = 0; i < (2 * G::kChunks + kQW - 1) / kQW; ++i) {
             const int cidx = wq + kQW * i;
             if (cidx < 2 * G::kChunks) {
                 const bool isv = cidx >= G::kChunks;
-                const uint32_t off = tile_off + (isv ? cidx - G::kChunks : cidx) * 1024;
+                const uint32_t off = kSwap > 1 ? swapped(isv ? cidx - G::kChunks : cidx)
+                                               : tile_off + (isv ? cidx - G::kChunks : cidx) * 1024;
                 copy16_to_lds(isv ? Vt : Kt, min(off, last), dst + cidx * 1024);
             }
         }
@@ -275,28 +317,27 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 
-    // Q^T operand of block j: lane holds query q0 + 32j + l32, d = 16s + 8*half .. +7.
     u32x4 qreg[QB][DK];
 #pragma unroll
     for (int j = 0; j < QB; ++j)
 #pragma unroll
-        for (int s = 0; s < DK; ++s) {
-            const int qrow = q0 + 32 * j + l32;
-            const int d0 = 16 * s + 8 * half;
-            u32x4 v = {0u, 0u, 0u, 0u};
-            if (qrow < Lq && d0 < D) v = *(const u32x4*)(Q + ((size_t)bh * Lq + qrow) * D + d0);
-            if (neg) v ^= 0x80008000u;   // fold a negative scale into Q (exact)
-            qreg[j][s] = v;
-        }
-
+        for (int s = 0; s < DK; ++s) qreg[j][s] = SPARSE ? q_early[j][s] : q_value(j, s);
 
     // Per-lane LDS byte offsets inside a buffer.
     // K rows: lane reads key row l32 at d = 8*half (+16 s, +32 sub rows).
     const int k_off = (l32 * D + 8 * half) * 2;
+    [[maybe_unused]] int k_swap[DK];   // SPARSE: for each 16 values
+#pragma unroll
+    for (int s = 0; s < DK; ++s) k_swap[s] = l32 * D * 2 + swapped_at(2 * s, half, chunk_swap(l32)) * 16;
+    // address of keys l32's values 16s + 8*half .. +7 in sub-tile `sub` of the K tile at LDS offset buf
+    auto k_addr = [&](int buf, int sub, int s) __attribute__((always_inline)) -> const char* {
+        return kSwap > 1 ? smem + buf + k_swap[s] + 32 * sub * D * 2 : smem + buf + k_off + (32 * sub * D + 16 * s) * 2;
+    };
     // V^T via transposing reads: 16-lane group g = lane / 16 covers keys
     // 4*(g/2) .. +3 and d = 32n + 16*(g%2) .. +15; its lane i points at key
     // 4*(g/2) + i/4, d = 32n + 16*(g%2) + 4*(i%4) .. +3.
     int v_off[DN];
+    [[maybe_unused]] int v_hi[DN];   // SPARSE: the same for the keys 8 on (the sparse tile's 4 on)
     int v_mask = -1;   // last d tile: 0 in the lanes that read the constant block
     int v_idx = 0;     // places of the sparse tile's values (see step32)
     {
@@ -318,11 +359,26 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
             v_off[n] = ds < D ? TB + (key * D + ds) * 2
                               : G::kOnes ? G::kConst + (key * D + ds - D) * 2 : TB + (key * D + ds - 32) * 2;
             if (G::kOnes && ds >= D) v_mask = 0;
+            if constexpr (kSwap > 1) {   // (no constant block with these widths)
+                const int d = ds < D ? ds : ds - 32, on = G::kSparse && n == DD ? 4 : 8;
+                auto place = [&](int r) __attribute__((always_inline)) {
+                    // (a lane's chunk within 32 values is less than 4: no carry, kSwap 2 aside)
+                    const int c = 32 * n + 32 <= D && kSwap > 2 ? swapped_at(4 * n, d / 8 - 4 * n, chunk_swap(r)) : (d / 8) ^ chunk_swap(r);
+                    return TB + r * D * 2 + c * 16 + d % 8 * 2;
+                };
+                v_off[n] = place(key);
+                v_hi[n] = place(key + on) - on * D * 2;
+            }
         }
     }
     // address of d tile n's values in the V tile of the buffer at LDS offset buf
     auto v_addr = [&](int buf, int n) __attribute__((always_inline)) -> const char* {
         return smem + ((G::kOnes && n == DN - 1 ? buf & v_mask : buf) + v_off[n]);
+    };
+    // and of the second read's, less its keys' distance
+    auto v_addr2 = [&](int buf, int n) __attribute__((always_inline)) -> const char* {
+        if constexpr (kSwap > 1) return smem + buf + v_hi[n];
+        else return v_addr(buf, n);
     };
 
     f32x16 acc[QB][DN];
@@ -384,7 +440,7 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
             for (int r = 0; r < 16; ++r) st[j][r] = 0.0f;
 #pragma unroll
         for (int s = 0; s < DK; ++s) {
-            u32x4 a = *(const u32x4*)(smem + buf + k_off + (32 * sub * D + 16 * s) * 2);
+            u32x4 a = *(const u32x4*)k_addr(buf, sub, s);
 #pragma unroll
             for (int j = 0; j < QB; ++j) st[j] = mfma32x32x16<ET>(a, qreg[j][s], st[j]);
         }
@@ -439,7 +495,7 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
             for (int n = 0; n < DD; ++n) {
                 const char* vb = v_addr(buf, n) + (32 * sub + 16 * u) * D * 2;
                 const u32x2 lo = lds_read_tr(vb);
-                const u32x2 hi = lds_read_tr(vb + 8 * D * 2);
+                const u32x2 hi = lds_read_tr(v_addr2(buf, n) + (32 * sub + 16 * u + 8) * D * 2);
                 const u32x4 a = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
                 for (int j = 0; j < QB; ++j) acc[j][n] = mfma32x32x16<ET>(a, pk[j][u], acc[j][n]);
@@ -452,7 +508,7 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
         if constexpr (G::kSparse) {
             const char* vb = v_addr(buf, DD) + 32 * sub * D * 2;
             const u32x2 lo = lds_read_tr(vb);
-            const u32x2 hi = lds_read_tr(vb + 4 * D * 2);
+            const u32x2 hi = lds_read_tr(v_addr2(buf, DD) + (32 * sub + 4) * D * 2);
             const u32x4 a = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
             for (int j = 0; j < QB; ++j)
@@ -506,7 +562,7 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
                 for (int r = 0; r < 16; ++r) st[sub][j][r] = 0.0f;
 #pragma unroll
             for (int s = 0; s < DK; ++s) {
-                u32x4 a = *(const u32x4*)(smem + buf + k_off + (32 * sub * D + 16 * s) * 2);
+                u32x4 a = *(const u32x4*)k_addr(buf, sub, s);
 #pragma unroll
                 for (int j = 0; j < QB; ++j) st[sub][j] = mfma32x32x16<ET>(a, qreg[j][s], st[sub][j]);
             }
@@ -518,13 +574,13 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
                 for (int n = 0; n < DD; ++n) {
                     const char* vb = v_addr(buf, n) + (32 * sub + 16 * u) * D * 2;
                     const u32x2 lo = lds_read_tr(vb);
-                    const u32x2 hi = lds_read_tr(vb + 8 * D * 2);
+                    const u32x2 hi = lds_read_tr(v_addr2(buf, n) + (32 * sub + 16 * u + 8) * D * 2);
                     vt[sub][u][n] = u32x4{lo[0], lo[1], hi[0], hi[1]};
                 }
             if constexpr (G::kSparse) {
                 const char* vb = v_addr(buf, DD) + 32 * sub * D * 2;
                 const u32x2 lo = lds_read_tr(vb);
-                const u32x2 hi = lds_read_tr(vb + 4 * D * 2);
+                const u32x2 hi = lds_read_tr(v_addr2(buf, DD) + (32 * sub + 4) * D * 2);
                 vs[sub] = u32x4{lo[0], lo[1], hi[0], hi[1]};
             }
         };
@@ -672,20 +728,20 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
         float negm[QB];   // -c m, with statistics
 
         auto read_k = [&](int buf, int sub, int s) __attribute__((always_inline)) {
-            kf[sub][s] = *(const u32x4*)(smem + buf + k_off + (32 * sub * D + 16 * s) * 2);
+            kf[sub][s] = *(const u32x4*)k_addr(buf, sub, s);
         };
         // operand h of the O^T MFMAs (u = h / DD, n = h % DD; last the sparse one)
         auto read_v = [&](int buf, int sub, int h) __attribute__((always_inline)) {
             if (G::kSparse && h == 2 * DD) {
                 const char* vb = v_addr(buf, DD) + 32 * sub * D * 2;
                 const u32x2 lo = lds_read_tr(vb);
-                const u32x2 hi = lds_read_tr(vb + 4 * D * 2);
+                const u32x2 hi = lds_read_tr(v_addr2(buf, DD) + (32 * sub + 4) * D * 2);
                 vsf[sub] = u32x4{lo[0], lo[1], hi[0], hi[1]};
             } else {
                 const int u = h / DD, n = h % DD;
                 const char* vb = v_addr(buf, n) + (32 * sub + 16 * u) * D * 2;
                 const u32x2 lo = lds_read_tr(vb);
-                const u32x2 hi = lds_read_tr(vb + 8 * D * 2);
+                const u32x2 hi = lds_read_tr(v_addr2(buf, n) + (32 * sub + 16 * u + 8) * D * 2);
                 vf[sub][u][n] = u32x4{lo[0], lo[1], hi[0], hi[1]};
             }
         };

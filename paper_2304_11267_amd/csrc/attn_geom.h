@@ -11,6 +11,7 @@ constexpr int kGeoNormal = 1;          // 128 rows, 64-key tiles
 constexpr int kGeoBig = 2;             // 256 rows, 64-key tiles (QB = 2 only)
 constexpr int kGeoQuarter = 3;         // 64 rows, keys split four ways, 64-key tiles
 constexpr int kGeoPair = 4;            // kGeoNormal without the streaming loop's third buffer
+constexpr int kGeoNarrow = 5;          // kGeoSmall with one query block a wave for every D
 constexpr int kMaxLds = 160 * 1024;
 constexpr int kQuarterMinKeys = 512;   // shortest key sequence given to kGeoQuarter
 constexpr int kBigMinKeys = 1024;      // and to kGeoBig
@@ -32,14 +33,16 @@ constexpr int kCus = 256;
 // block (the LDS holds four splits' double buffers), so l comes from v_dot2.
 // kGeoPair is for widths (D = 56, 64) whose streaming ring fills a CU's LDS with
 // one 128-row workgroup, four waves: with two buffers a CU holds two.
+// kGeoNarrow is for attention over selected blocks (attn_sparse.h): 64 rows whose
+// neighbours read other keys, as 32 a wave at every D, so that each SIMD has a wave.
 template <int D, int GEO = kGeoNormal>
 struct Geom {
-    static constexpr int QB = D <= 64 ? 2 : 1;
+    static constexpr int QB = D <= 64 && GEO != kGeoNarrow ? 2 : 1;
     static constexpr bool kBig = GEO == kGeoBig;
     static constexpr bool kQuarter = GEO == kGeoQuarter;
     static constexpr int kKS = kQuarter ? 4 : 2;              // key splits
     static constexpr int kTK = 64;                            // keys per LDS tile
-    static constexpr int kQW = kBig ? 4 : (GEO == kGeoSmall || kQuarter ? 2 : 4) / QB;   // query waves
+    static constexpr int kQW = kBig ? 4 : (GEO == kGeoSmall || GEO == kGeoNarrow || kQuarter ? 2 : 4) / QB;   // query waves
     static constexpr int kBQ = 32 * QB * kQW;                 // query rows per workgroup
     static constexpr int kWaves = kKS * kQW;                  // times the key splits
     static constexpr int kThreads = kWaves * 64;

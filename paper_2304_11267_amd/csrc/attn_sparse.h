@@ -15,14 +15,15 @@ namespace sdattn {
 
 namespace {
 
-// 64 queries: kGeoSmall; 128: kGeoNormal, or kGeoPair past one round over the CUs
-// (attn_geom.h).
+// 64 queries: kGeoNarrow, four waves of 32 of them and half of the blocks (with two waves
+// of all 64 a CU has work for two of its SIMDs: 16384 tokens, 32 blocks, 8 heads, bf16, D = 64
+// 178 us, so 103); 128: kGeoNormal, or kGeoPair past one round over the CUs (attn_geom.h).
 template <int ET, int D>
 hipError_t launch_sparse_d(const SparseArgs& s) {
     const AttnArgs a{s.q, s.k, s.v, s.out, nullptr, s.B, s.H, s.Lq, s.Lk, D, s.scale, s.dtype, s.stream};
     const int nw = ((s.Lk + kSparseBlock - 1) / kSparseBlock + 63) / 64;
     const BlockMask mask{(const unsigned long long*)s.mask, nw};
-    if (s.qblock == 64) return launch_kernel<ET, D, false, false, kGeoSmall>(a, mask);
+    if (s.qblock == 64) return launch_kernel<ET, D, false, false, kGeoNarrow>(a, mask);
     if constexpr (Geom<D, kGeoPair>::kFits) {
         if ((long long)s.B * s.H * ((s.Lq + 127) / 128) > kCus) return launch_kernel<ET, D, false, false, kGeoPair>(a, mask);
     }
@@ -36,7 +37,7 @@ hipError_t dispatch_sparse(const SparseArgs& s, std::integer_sequence<int, I...>
     hipError_t r = hipErrorInvalidValue;
     auto one = [&](auto i_c) {
         constexpr int D = kSparseMinD + 8 * decltype(i_c)::value;
-        static_assert(sparse_width(D) == (Geom<D, kGeoNormal>::kFits && Geom<D, kGeoSmall>::kFits), "");
+        static_assert(sparse_width(D) == (Geom<D, kGeoNormal>::kFits && Geom<D, kGeoNarrow>::kFits), "");
         if constexpr (sparse_width(D)) {
             if (s.D == D) r = launch_sparse_d<ET, D>(s);
         }
