@@ -24,7 +24,7 @@ MARSHAL = os.path.join(HERE, "_marshal.so")
 ARCH = "gfx950"
 
 SOURCES = ["attn_fwd.hip", "attn_fwd_bf16.hip", "attn_fwd_stats.hip", "attn_fwd_short.hip", "attn_fwd_generic.hip",
-           "attn_sparse.hip", "attn_sparse_bf16.hip", "block_select.hip", "softmax_rows.hip",
+           "attn_sparse.hip", "attn_sparse_bf16.hip", "attn_sparse_row.hip", "block_select.hip", "softmax_rows.hip",
            "twopass.hip", "linear.hip", "norm_act.hip", "norm_rotate.hip", "winograd.hip",
            "sdattn_api.hip"]
 

@@ -5,6 +5,7 @@
 namespace sdattn {
 
 hipError_t launch_attn_sparse(const SparseArgs& a) {
+    if (a.Lq == 1) return launch_attn_sparse_row(a);
     return a.dtype == kF16 ? dispatch_sparse<kF16>(a, SparseWidths{}) : launch_attn_sparse_bf16(a);
 }
 

@@ -107,6 +107,22 @@ __device__ __forceinline__ float add_pair(uint32_t w, float acc) {
     }
 }
 
+// c + the product of 8 pairs of 16-bit values (v_dot2_f32_f16 / v_dot2_f32_bf16)
+template <int ET>
+__device__ __forceinline__ float dot8(u32x4 a, u32x4 b, float c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (ET == kF16) {
+            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+            c = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, (uint32_t)a[i]), __builtin_bit_cast(h2, (uint32_t)b[i]), c, false);
+        } else {
+            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+            c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, (uint32_t)a[i]), __builtin_bit_cast(b2, (uint32_t)b[i]), c, false);
+        }
+    }
+    return c;
+}
+
 // s_waitcnt immediate that waits until at most n vector-memory loads are
 // outstanding (gfx9 encoding: vmcnt in bits 3:0 and 15:14; expcnt and
 // lgkmcnt left at their maxima, i.e. not waited on).

@@ -188,6 +188,8 @@ struct SparseArgs {
     void* stream;
 };
 hipError_t launch_attn_sparse(const SparseArgs& a);
+// one query a head (attn_sparse_row.hip)
+hipError_t launch_attn_sparse_row(const SparseArgs& a);
 // the bf16 instantiations (a translation unit of their own)
 hipError_t launch_attn_sparse_bf16(const SparseArgs& a);
 

@@ -136,22 +136,6 @@ __device__ __forceinline__ u32x4 adapter_chunk(const uint16_t* row, int r0, int 
     return v;
 }
 
-// c + the product of 8 pairs of 16-bit values (v_dot2_f32_f16 / v_dot2_f32_bf16)
-template <int ET>
-__device__ __forceinline__ float dot8(u32x4 a, u32x4 b, float c) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (ET == kF16) {
-            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-            c = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, (uint32_t)a[i]), __builtin_bit_cast(h2, (uint32_t)b[i]), c, false);
-        } else {
-            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-            c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, (uint32_t)a[i]), __builtin_bit_cast(b2, (uint32_t)b[i]), c, false);
-        }
-    }
-    return c;
-}
-
 // sum[b] = up T^T for the 32 token rows from row0 and the 32 channels from n0 + 32 b, in the
 // accumulators' layout; it is the first addend of those channels' sums.  Every row sees its
 // own request's adapter alone, infinities and all, and a request's bits do not depend on its
