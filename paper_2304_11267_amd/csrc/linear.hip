@@ -32,9 +32,13 @@
 // LDS so that each lane stores 16 contiguous bytes.
 //
 // Low-rank adapters of many requests ride beside the shared product: row m of batch
-// item b adds s_i up_i (down_i x_m), i = ids[b].  A first launch (adapter_down_kernel)
-// writes T = s_i down_i x_m, and both kernels above then carry T up_i^T as a few more
-// steps of their reduced dimension.
+// item b adds s_i up_i (down_i x_m), i = ids[b], in one of two ways (launch_adapters_e).
+// AdapterFused, ranks up to 16 and requests of 32 rows and more (not of many rows and
+// many channels): tiles of one request
+// each, whose slices carry the 16 rows of down_i beside those of w, so that x is read
+// once and T = s_i down_i x ends in the registers that the last product, up_i T, takes.
+// AdapterSet, all others: a first launch (adapter_down_kernel) writes T, and both kernels
+// above add T up_i^T to the rows of each request.
 #include "device.h"
 #include "launch.h"
 
@@ -110,8 +114,60 @@ struct AdapterSet {
     const int* ids;         // [B]: the adapter of a batch item; none outside [0, count)
     int count, R, Rp;
 };
-__device__ __forceinline__ AdapterSet adapters_of() { return AdapterSet{}; }
-__device__ __forceinline__ AdapterSet adapters_of(const AdapterSet& a) { return a; }
+struct AdapterFused {
+    const uint16_t* down;   // [count, R, K]
+    const uint16_t* up;     // [count, N, R]
+    const int* ids;         // [batch items]
+    const float* scales;    // [count] or null
+    int count, R;
+};
+struct AdapterNone {};
+__device__ __forceinline__ AdapterNone adapters_of() { return AdapterNone{}; }
+template <typename A>
+__device__ __forceinline__ A adapters_of(const A& a) { return a; }
+template <typename A, typename... AD>
+constexpr bool adapters_are = sizeof...(AD) == 1 && (std::is_same<A, AD>::value && ...);
+
+constexpr int kRankRows = 16;   // rows of down beside a slice's rows of w
+constexpr int kFusedMaxN = 768, kFusedMaxRows = 256;   // see launch_adapters_e
+
+// The operands of the last product of AdapterFused, Y^T += up T^T, on one MFMA of 16 ranks:
+// T^T comes as a 32x32 accumulator whose first 8 registers hold ranks 8 (r / 4) + 4 half +
+// r % 4 of token l32 (the others repeat them), so up is read in that order.
+template <int ET>
+__device__ __forceinline__ u32x4 fused_t(const float (&t)[8], float scale, int R, int half) {
+    u32x4 v;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        float f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = 2 * w + e, rank = 8 * (r >> 2) + 4 * half + (r & 3);
+            f[e] = rank < R ? t[r] * scale : 0.0f;   // (rows past R repeat the last one)
+        }
+        v[w] = pack2<ET>(f[0], f[1]);   // rounded to the type that the matrix core multiplies
+    }
+    return v;
+}
+__device__ __forceinline__ u32x4 fused_up(const uint16_t* row, int R, int half) {
+    u32x4 v = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int r0 = 8 * q + 4 * half;
+        if (R % 4 == 0) {
+            if (r0 < R) {
+                const u32x2 w = *(const u32x2*)(row + r0);
+                v[2 * q] = w[0];
+                v[2 * q + 1] = w[1];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (r0 + e < R) v[2 * q + (e >> 1)] |= (uint32_t)row[r0 + e] << (16 * (e & 1));
+        }
+    }
+    return v;
+}
 
 // Ranks r0 .. r0 + 7 of an adapter's row of R, zeros from R on, in reads of W values (R is
 // a multiple of W).
@@ -213,9 +269,10 @@ __device__ __forceinline__ void adapter_sums(const AdapterSet& ad, int row0, int
 }
 
 // Wait until at most `ahead` slices of this wave's copies are still in flight.
+template <int COPIES = kCopies>
 __device__ __forceinline__ void wait_slices(int ahead) {
     static_assert(kStages == 3, "wait_slices covers ahead = 0 and 1");
-    if (ahead >= 1) __builtin_amdgcn_s_waitcnt(vm_wait(kCopies));
+    if (ahead >= 1) __builtin_amdgcn_s_waitcnt(vm_wait(COPIES));
     else __builtin_amdgcn_s_waitcnt(vm_wait(0));
 }
 
@@ -227,9 +284,12 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// AD: nothing, or an AdapterSet (of one product with batch 1)
+// AD: nothing, an AdapterSet (one product with batch 1), or an AdapterFused (one product,
+// a batch item for each request)
 template <int ET, bool XH, bool YH, bool FOLD, typename... AD>
 __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const AD... ad) {
+    constexpr bool FUSED = adapters_are<AdapterFused, AD...>;
+    constexpr int kSlot = kSliceBytes + (FUSED ? kRankRows * kBK * 2 : 0);   // of the ring
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = lane_id();
     const int l32 = lane & 31;
@@ -271,10 +331,34 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     }
     const float inv_xhw = 1.0f / (float)xhw;
 
+    // FUSED: the request's adapter (the first one's addresses where it has none), the four
+    // rows of down that this wave copies with 32 of its lanes, and its operands of up
+    [[maybe_unused]] bool adapted = false;
+    [[maybe_unused]] float t_scale = 1.0f;
+    [[maybe_unused]] const uint16_t* d_row = nullptr;
+    [[maybe_unused]] int d_ch = 0, offd[4];
+    [[maybe_unused]] u32x4 upf[2];
+    [[maybe_unused]] int rank = 0;
+    if constexpr (FUSED) {
+        const AdapterFused a = adapters_of(ad...);
+        const int named = __builtin_amdgcn_readfirstlane(a.ids[bi]);
+        adapted = named >= 0 && named < a.count;
+        const int id = adapted ? named : 0;
+        rank = a.R;
+        if (a.scales) t_scale = a.scales[id];
+        const int r = 4 * wave + ((lane & 31) >> 3);
+        d_ch = 8 * ((lane & 7) ^ swz(r));
+        d_row = a.down + ((size_t)id * a.R + min(r, a.R - 1)) * K;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) upf[t] = fused_up(a.up + ((size_t)id * N + min(n0 + 32 * t + l32, N - 1)) * a.R, a.R, half);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) offd[s] = kSliceBytes + (l32 & 15) * kBK * 2 + ((2 * s + half) ^ swz(l32 & 15)) * 16;
+    }
+
     // slice i (channels 64i .. 64i + 63) into ring slot i % kStages
     auto issue = [&](int i) __attribute__((always_inline)) {
         const int k0 = i * kBK;
-        char* st = smem + (i % kStages) * kSliceBytes;
+        char* st = smem + (i % kStages) * kSlot;
 #pragma unroll
         for (int j = 0; j < kCopies; ++j) {
             const int u0 = (wave * kCopies + j) * 64;
@@ -284,7 +368,13 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
                                   : (const char*)(W + cbase[j] + ch);
             __builtin_amdgcn_global_load_lds(src, (lds_void_t*)(st + u0 * 16), 16, 0, 0);
         }
+        if constexpr (FUSED) {
+            if (lane < 32)
+                __builtin_amdgcn_global_load_lds((const char*)(d_row + min(k0 + d_ch, K - 8)),
+                                                 (lds_void_t*)(st + kSliceBytes + wave * 512), 16, 0, 0);
+        }
     };
+    constexpr int kIssued = kCopies + (FUSED ? 1 : 0);   // copies of a wave and slice
 
     // operand offsets inside a slice: B = x row 32*wave + l32, A_t = w row
     // 32t + l32, chunk 2s + half for k-step s (rows 32t + l32 share swz(l32))
@@ -321,12 +411,19 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     f32x16 zero;
 #pragma unroll
     for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
+    [[maybe_unused]] f32x16 dacc = zero, dtot = zero;   // FUSED: T^T, as acc and tot
+    // the slice's down rows at st, on the x operands of k-step s
+    [[maybe_unused]] auto down_step = [&](const char* st, int s, u32x4 xf, int kval) __attribute__((always_inline)) {
+        u32x4 df = *(const u32x4*)(st + offd[s]);
+        if (8 * (2 * s + half) >= kval) df = u32x4{0u, 0u, 0u, 0u};
+        dacc = mfma32x32x16<ET>(df, xf, dacc);
+    };
     auto slice = [&](int i, auto first_c, f32x16 (&acc)[2], auto before) __attribute__((always_inline)) {
         constexpr bool FIRST = decltype(first_c)::value;
-        wait_slices(min(nk - 1 - i, kStages - 2));
+        wait_slices<kIssued>(min(nk - 1 - i, kStages - 2));
         lds_barrier();   // slice i is in LDS for every wave; slot (i - 1) % kStages is free
         if (i + kStages - 1 < nk) issue(i + kStages - 1);
-        const char* st = smem + (i % kStages) * kSliceBytes;
+        const char* st = smem + (i % kStages) * kSlot;
         const int kval = K - i * kBK;    // channels of this slice inside K (uniform)
         // all twelve operand reads first, so their latencies overlap
         u32x4 bf[4], af[2][4];
@@ -351,6 +448,11 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
             acc[0] = mfma32x32x16<ET>(af[0][s], bf[s], FIRST && s == 0 ? zero : acc[0]);
             acc[1] = mfma32x32x16<ET>(af[1][s], bf[s], FIRST && s == 0 ? zero : acc[1]);
         }
+        if constexpr (FUSED) {
+            if (FIRST) dacc = zero;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) down_step(st, s, bf[s], kval);
+        }
     };
 
 #pragma unroll
@@ -367,16 +469,17 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     // 11.4 (12.0), 2048x2560x640 19.4 / 19.0 (20.0).
     f32x16 acc[2] = {zero, zero}, tot[2] = {zero, zero};
     // the adapters' part comes first, while the first slices are on their way
-    if constexpr (sizeof...(AD) > 0) adapter_sums<ET>(adapters_of(ad...), m0 + 32 * wave, n0, M, N, L, FOLD ? tot : acc);
+    if constexpr (adapters_are<AdapterSet, AD...>)
+        adapter_sums<ET>(adapters_of(ad...), m0 + 32 * wave, n0, M, N, L, FOLD ? tot : acc);
     const int run = K > kSplitMinK ? (nk + kRuns - 1) / kRuns : nk;
     if constexpr (!FOLD) {
         // (a loop of its own: as slices opened by a run's first one, products with a
         // ragged last slice were slower, 8192x328x320 8.7 -> 9.1 us)
         for (int i = 0; i < nk; ++i) {
-            wait_slices(min(nk - 1 - i, kStages - 2));
+            wait_slices<kIssued>(min(nk - 1 - i, kStages - 2));
             lds_barrier();   // slice i is in LDS for every wave; slot (i - 1) % kStages is free
             if (i + kStages - 1 < nk) issue(i + kStages - 1);
-            const char* st = smem + (i % kStages) * kSliceBytes;
+            const char* st = smem + (i % kStages) * kSlot;
             const int kval = K - i * kBK;    // channels of this slice inside K (uniform)
             // all twelve operand reads first, so their latencies overlap
             u32x4 bf[4], af[2][4];
@@ -400,6 +503,10 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
                 acc[0] = mfma32x32x16<ET>(af[0][s], bf[s], acc[0]);
                 acc[1] = mfma32x32x16<ET>(af[1][s], bf[s], acc[1]);
             }
+            if constexpr (FUSED) {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) down_step(st, s, bf[s], kval);
+            }
         }
     } else
     for (int i0 = 0; i0 < nk; i0 += run) {
@@ -408,10 +515,24 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
                 __builtin_amdgcn_sched_barrier(0);
                 tot[0] += acc[0];
                 tot[1] += acc[1];
+                if constexpr (FUSED) dtot += dacc;
                 __builtin_amdgcn_sched_barrier(0);
             }
         });
         for (int i = i0 + 1; i < min(i0 + run, nk); ++i) slice(i, std::false_type{}, acc, [] {});
+    }
+
+    // FUSED: up T^T, added to a row's finished sum
+    [[maybe_unused]] f32x16 more[2] = {zero, zero};
+    if constexpr (FUSED) {
+        if (adapted) {
+            float t[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) t[r] = FOLD ? dtot[r] + dacc[r] : dacc[r];
+            const u32x4 tf = fused_t<ET>(t, t_scale, rank, half);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) more[b] = mfma32x32x16<ET>(upf[b], tf, zero);
+        }
     }
 
     // Stage the 128 x 64 output tile (bias added, rounded) in LDS, rows of
@@ -428,9 +549,11 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
             for (int g = 0; g < 4; ++g) {
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = (FOLD ? tot[t][4 * g + e] + acc[t][4 * g + e] : acc[t][4 * g + e]) +
-                           to_float<ET>((uint16_t)(bias[t][g][e >> 1] >> (16 * (e & 1))));
+                for (int e = 0; e < 4; ++e) {
+                    float f = FOLD ? tot[t][4 * g + e] + acc[t][4 * g + e] : acc[t][4 * g + e];
+                    if constexpr (FUSED) f += more[t][4 * g + e];
+                    v[e] = f + to_float<ET>((uint16_t)(bias[t][g][e >> 1] >> (16 * (e & 1))));
+                }
                 u32x2 w;
                 w[0] = pack2<ET>(v[0], v[1]);
                 w[1] = pack2<ET>(v[2], v[3]);
@@ -476,13 +599,14 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
 // K = 1280 is 328 KB through one CU); with one slice per wave (ST = 1) two or
 // three workgroups share a CU and cover each other's waits, which measured
 // faster than deeper rings (512x1280x1280: 9.1 against 9.4 us with ST = 2).
-template <int TM, int TN, int ST>
+template <int TM, int TN, int ST, int RR = 0>
 struct KsGeom {
-    static constexpr int kSlice = (TM + TN) * kBK * 2;            // bytes
+    static constexpr int kSlice = (TM + TN + RR) * kBK * 2;       // bytes (RR rows of an adapter's down)
     static constexpr int kCopies = kSlice / 1024;                 // copy instructions per slice
     static constexpr int kOutRow = TN * 4 + 16;                   // bytes per row of a partial tile
     static constexpr int kRing = kRuns * ST * kSlice;
-    static constexpr int kPart = kRuns * TM * kOutRow;
+    static constexpr int kTiles = kRuns * TM * kOutRow;           // partial tiles; with RR, T's parts and the adapter's tile
+    static constexpr int kPart = kTiles + (RR > 0 ? kRuns * TM * RR * 4 + TM * kOutRow : 0);
     static constexpr int kLds = kRing > kPart ? kRing : kPart;
     static_assert(kLds <= 160 * 1024 && TM % 32 == 0 && TN % 32 == 0, "geometry");
     static_assert(kCopies * (ST - 1) < 64, "copies in flight fit vmcnt");
@@ -502,7 +626,8 @@ __device__ __forceinline__ void ks_wait(int n) {
 
 template <int ET, bool YH, int TM, int TN, int ST, typename... AD>
 __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_kernel(const LinGroup grp, const AD... ad) {
-    using G = KsGeom<TM, TN, ST>;
+    constexpr bool FUSED = adapters_are<AdapterFused, AD...>;
+    using G = KsGeom<TM, TN, ST, FUSED ? kRankRows : 0>;
     constexpr int MB = TM / 32, NB = TN / 32, KS = kBK / 16;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = lane_id();
@@ -534,6 +659,19 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
     // past M or N repeat the last row (their outputs are never stored).
     const uint16_t* src[G::kCopies];
     int cch[G::kCopies];
+    // FUSED: the request's adapter (the first one's addresses where it has none)
+    [[maybe_unused]] bool adapted = false;
+    [[maybe_unused]] int id = 0;
+    [[maybe_unused]] const uint16_t* down = nullptr;
+    [[maybe_unused]] int rank = 1;
+    if constexpr (FUSED) {
+        const AdapterFused a = adapters_of(ad...);
+        const int named = __builtin_amdgcn_readfirstlane(a.ids[bi]);
+        adapted = named >= 0 && named < a.count;
+        id = adapted ? named : 0;
+        down = a.down + (size_t)id * a.R * K;
+        rank = a.R;
+    }
 #pragma unroll
     for (int j = 0; j < G::kCopies; ++j) {
         const int u = j * 64 + lane;
@@ -541,6 +679,7 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
         cch[j] = 8 * ((u % 8) ^ swz(r)) + first * kBK;
         src[j] = j * 64 < TM * 8 ? X + (size_t)min(m0 + r, M - 1) * K
                                  : W + (size_t)min(n0 + r - TM, N - 1) * K;
+        if (FUSED && j * 64 >= (TM + TN) * 8) src[j] = down + (size_t)min(r - TM - TN, rank - 1) * K;
     }
     auto issue = [&](int i) __attribute__((always_inline)) {
         char* st = ring + (i % ST) * G::kSlice;
@@ -551,11 +690,13 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
     };
 
     int offx[KS], offw[KS];   // row l32, chunk 2s + half; rows 32 apart share the swizzle
+    [[maybe_unused]] int offd[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
         const int cpos = (2 * s + half) ^ swz(l32);
         offx[s] = (l32 * 8 + cpos) * 16;
         offw[s] = ((TM + l32) * 8 + cpos) * 16;
+        offd[s] = ((TM + TN + (l32 & 15)) * 8 + ((2 * s + half) ^ swz(l32 & 15))) * 16;
     }
 
     f32x16 acc[MB][NB];
@@ -570,8 +711,13 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
     for (int i = 0; i < ST; ++i)
         if (i < count) issue(i);
 
+    [[maybe_unused]] f32x16 dacc[MB];       // FUSED: T^T of this run
+#pragma unroll
+    for (int a = 0; a < MB; ++a)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dacc[a][r] = 0.0f;
     [[maybe_unused]] f32x16 more[MB][NB];   // the adapters' part, while the first slices are on their way
-    if constexpr (sizeof...(AD) > 0) {
+    if constexpr (adapters_are<AdapterSet, AD...>) {
         if (wave == 0) {
 #pragma unroll
             for (int a = 0; a < MB; ++a) adapter_sums<ET>(adapters_of(ad...), m0 + 32 * a, n0, M, N, L, more[a]);
@@ -582,8 +728,10 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
         ks_wait<G::kCopies, ST - 1>(count - 1 - i);
         const char* st = ring + (i % ST) * G::kSlice;
         u32x4 xf[MB][KS], wf[NB][KS];
+        [[maybe_unused]] u32x4 df[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
+            if constexpr (FUSED) df[s] = *(const u32x4*)(st + offd[s]);
 #pragma unroll
             for (int a = 0; a < MB; ++a) xf[a][s] = *(const u32x4*)(st + offx[s] + a * 32 * kBK * 2);
 #pragma unroll
@@ -601,7 +749,14 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
                     for (int a = 0; a < MB; ++a) xf[a][s] = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
                     for (int b = 0; b < NB; ++b) wf[b][s] = u32x4{0u, 0u, 0u, 0u};
+                    if constexpr (FUSED) df[s] = u32x4{0u, 0u, 0u, 0u};
                 }
+        }
+        if constexpr (FUSED) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int a = 0; a < MB; ++a) dacc[a] = mfma32x32x16<ET>(df[s], xf[a][s], dacc[a]);
         }
 #pragma unroll
         for (int s = 0; s < KS; ++s)
@@ -613,7 +768,7 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
 
     // the adapters' part is added to the first run, in the order of the shared tiles' sums
     // (and so with the same bits)
-    if constexpr (sizeof...(AD) > 0) {
+    if constexpr (adapters_are<AdapterSet, AD...>) {
         if (wave == 0) {
 #pragma unroll
             for (int a = 0; a < MB; ++a)
@@ -648,6 +803,48 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
                                      acc[a][b][4 * g + 3]};
                     *(f32x4*)(part + (32 * a + l32) * G::kOutRow + (32 * b + 8 * g + 4 * half) * 4) = v;
                 }
+        if constexpr (FUSED) {   // T's part, [TM][16 ranks]
+            char* tp = smem + G::kTiles + wave * (TM * kRankRows * 4);
+#pragma unroll
+            for (int a = 0; a < MB; ++a)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    *(f32x4*)(tp + (32 * a + l32) * kRankRows * 4 + (8 * q + 4 * half) * 4) =
+                        f32x4{dacc[a][4 * q], dacc[a][4 * q + 1], dacc[a][4 * q + 2], dacc[a][4 * q + 3]};
+        }
+    }
+    [[maybe_unused]] constexpr int kMore = G::kTiles + kRuns * TM * kRankRows * 4;   // the adapter's tile
+    if constexpr (FUSED) {
+        // T whole, the runs in the shared tiles' order, then up T^T by a wave for each 32 x 32
+        const AdapterFused f = adapters_of(ad...);
+        static_assert(MB * NB <= kRuns, "a block a wave");
+        const bool mine = wave < MB * NB;
+        const int a = wave / NB, b = wave % NB;
+        u32x4 upf = {0u, 0u, 0u, 0u};
+        if (mine) upf = fused_up(f.up + ((size_t)id * N + min(n0 + 32 * b + l32, N - 1)) * f.R, f.R, half);
+        __syncthreads();
+        if (mine) {
+            float t[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) t[r] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kRuns; ++w)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const f32x4 p = *(const f32x4*)(smem + G::kTiles + w * (TM * kRankRows * 4) +
+                                                    (32 * a + l32) * kRankRows * 4 + (8 * q + 4 * half) * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[4 * q + e] += p[e];
+                }
+            f32x16 sum;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[r] = 0.0f;
+            if (adapted) sum = mfma32x32x16<ET>(upf, fused_t<ET>(t, f.scales ? f.scales[id] : 1.0f, f.R, half), sum);
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(f32x4*)(smem + kMore + (32 * a + l32) * G::kOutRow + (32 * b + 8 * g + 4 * half) * 4) =
+                    f32x4{sum[4 * g], sum[4 * g + 1], sum[4 * g + 2], sum[4 * g + 3]};
+        }
     }
     __syncthreads();
     if (n >= N) return;
@@ -661,6 +858,11 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
 #pragma unroll
             for (int w = 0; w < kRuns; ++w) {
                 const char* p = smem + w * (TM * G::kOutRow) + r * G::kOutRow + c8 * 32;
+                lo += *(const f32x4*)p;
+                hi += *(const f32x4*)(p + 16);
+            }
+            if constexpr (FUSED) {
+                const char* p = smem + kMore + r * G::kOutRow + c8 * 32;
                 lo += *(const f32x4*)p;
                 hi += *(const f32x4*)(p + 16);
             }
@@ -775,10 +977,12 @@ long long tiles_of(const LinearArgs& a, int tm, int tn) {
 template <int ET, bool XH, bool YH, bool FOLD, typename... AD>
 hipError_t launch_t(const LinGroup& g, long long nblk, void* stream, const AD&... ad) {
     auto k = linear_kernel<ET, XH, YH, FOLD, AD...>;
+    constexpr int lds = kLdsBytes + (adapters_are<AdapterFused, AD...> ? kStages * kRankRows * kBK * 2 : 0);
+    static_assert(2 * lds <= 160 * 1024, "two workgroups a CU");
     static const hipError_t attr = hipFuncSetAttribute(
-        reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+        reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL(k, dim3((unsigned)nblk), dim3(256), kLdsBytes, (hipStream_t)stream, g, ad...);
+    hipLaunchKernelGGL(k, dim3((unsigned)nblk), dim3(256), lds, (hipStream_t)stream, g, ad...);
     return hipGetLastError();
 }
 
@@ -804,7 +1008,7 @@ long long number_tiles(LinGroup& g, const LinearArgs* a, int tm, int tn) {
 
 template <int ET, bool YH, int TM, int TN, int ST, typename... AD>
 hipError_t launch_ks(LinGroup& g, const LinearArgs* a, const AD&... ad) {
-    using G = KsGeom<TM, TN, ST>;
+    using G = KsGeom<TM, TN, ST, adapters_are<AdapterFused, AD...> ? kRankRows : 0>;
     const long long nblk = number_tiles(g, a, TM, TN);
     if (nblk > 0x7fffffff) return hipErrorInvalidValue;
     auto k = linear_ksplit_kernel<ET, YH, TM, TN, ST, AD...>;
@@ -829,7 +1033,10 @@ hipError_t launch_ksplit(LinGroup& g, const LinearArgs* a, const AD&... ad) {
         rows = rows > g.p[i].M ? rows : g.p[i].M;
     }
     if (n32 <= 256) return launch_ks<ET, YH, 32, 32, 2>(g, a, ad...);
-    if (rows > 32 && n64 >= 512) return launch_ks<ET, YH, 64, 64, 1>(g, a, ad...);
+    // (with an adapter's tile and T beside the partial tiles one 64 x 64 workgroup fills a CU)
+    if constexpr (!adapters_are<AdapterFused, AD...>) {
+        if (rows > 32 && n64 >= 512) return launch_ks<ET, YH, 64, 64, 1>(g, a, ad...);
+    }
     return launch_ks<ET, YH, 32, 64, 1>(g, a, ad...);
 }
 
@@ -866,25 +1073,6 @@ hipError_t launch_group_e(LinGroup& g, const LinearArgs* a, const AD&... ad) {
     return yh ? launch_f<ET, false, true>(g, nblk, fold, s, ad...) : launch_f<ET, false, false>(g, nblk, fold, s, ad...);
 }
 
-template <int ET, bool XH>
-hipError_t launch_down(const LinearArgs& a, const AdapterArgs& d) {
-    DownKernel k{(const uint16_t*)a.x, (const uint16_t*)d.down, d.ids, d.scales, (uint16_t*)d.t,
-                 a.L, a.K, a.x_heads ? a.K / a.H : 1, d.R, adapter_rank_padded(d.R), d.count, (a.L + 15) / 16};
-    const int rb = d.R <= 16 ? 1 : d.R <= 32 ? 2 : 4;
-    const dim3 grid((unsigned)(a.B * k.tiles), (unsigned)((d.R + 16 * rb - 1) / (16 * rb)));
-    auto f = rb == 1 ? adapter_down_kernel<ET, XH, 1> : rb == 2 ? adapter_down_kernel<ET, XH, 2> : adapter_down_kernel<ET, XH, 4>;
-    hipLaunchKernelGGL(f, grid, dim3(256), 0, (hipStream_t)a.stream, k);
-    return hipGetLastError();
-}
-
-template <int ET>
-hipError_t launch_adapters_e(LinGroup& g, const LinearArgs& a, const AdapterArgs& d) {
-    const hipError_t e = a.x_heads ? launch_down<ET, true>(a, d) : launch_down<ET, false>(a, d);
-    if (e != hipSuccess) return e;
-    const AdapterSet set{(const uint16_t*)d.t, (const uint16_t*)d.up, d.ids, d.count, d.R, adapter_rank_padded(d.R)};
-    return launch_group_e<ET>(g, &a, set);
-}
-
 // The group's products; an error for those that cannot share a launch.
 hipError_t make_group(LinGroup& g, const LinearArgs* a, int n) {
     if (n < 1 || n > kMaxLinearProblems) return hipErrorInvalidValue;
@@ -909,6 +1097,42 @@ hipError_t make_group(LinGroup& g, const LinearArgs* a, int n) {
         p.sy = a[i].sy;
     }
     return hipSuccess;
+}
+
+template <int ET, bool XH>
+hipError_t launch_down(const LinearArgs& a, const AdapterArgs& d) {
+    DownKernel k{(const uint16_t*)a.x, (const uint16_t*)d.down, d.ids, d.scales, (uint16_t*)d.t,
+                 a.L, a.K, a.x_heads ? a.K / a.H : 1, d.R, adapter_rank_padded(d.R), d.count, (a.L + 15) / 16};
+    const int rb = d.R <= 16 ? 1 : d.R <= 32 ? 2 : 4;
+    const dim3 grid((unsigned)(a.B * k.tiles), (unsigned)((d.R + 16 * rb - 1) / (16 * rb)));
+    auto f = rb == 1 ? adapter_down_kernel<ET, XH, 1> : rb == 2 ? adapter_down_kernel<ET, XH, 2> : adapter_down_kernel<ET, XH, 4>;
+    hipLaunchKernelGGL(f, grid, dim3(256), 0, (hipStream_t)a.stream, k);
+    return hipGetLastError();
+}
+
+template <int ET>
+hipError_t launch_adapters_e(LinGroup& g, const LinearArgs& a, const AdapterArgs& d) {
+    // Fused, the down rows cost every tile of 64 channels a third of its time; apart, x is
+    // read once more, and a launch waits for another.  us, plain product / fused / apart: 8
+    // requests of 77 rows, K 768, N 640, R 4 4.7 / 6.0 / 9.9; 8 of 4096, 320, 320, 16 17.8 / 24.2 /
+    // 30.9; 2 of 4096, 320, 1280, 16 16.7 / 22.9 / 25.1; 4 of 1024, 1280, 1280, 16 26.2 / 35.8 /
+    // 33.4, and more requests of these shift to the last.  The choice is by a request's own sizes, so
+    // that its bits do not depend on the others of its batch.
+    if (a.L >= kAdapterRows && d.R <= kRankRows && (a.N <= kFusedMaxN || a.L <= kFusedMaxRows)) {
+        LinearArgs one = a;   // a batch item for each request
+        one.B = 1;
+        one.batch = a.B;
+        one.sx = (long long)a.L * a.K;
+        one.sy = (long long)a.L * a.N;
+        const hipError_t e = make_group(g, &one, 1);
+        if (e != hipSuccess) return e;
+        return launch_group_e<ET>(g, &one, AdapterFused{(const uint16_t*)d.down, (const uint16_t*)d.up, d.ids, d.scales,
+                                                        d.count, d.R});
+    }
+    const hipError_t e = a.x_heads ? launch_down<ET, true>(a, d) : launch_down<ET, false>(a, d);
+    if (e != hipSuccess) return e;
+    const AdapterSet set{(const uint16_t*)d.t, (const uint16_t*)d.up, d.ids, d.count, d.R, adapter_rank_padded(d.R)};
+    return launch_group_e<ET>(g, &a, set);
 }
 
 }  // namespace

@@ -56,6 +56,10 @@ SHAPES = [
     (3, 7, 768, 640, 16, 2), (9, 31, 520, 72, 20, 4), (2, 32, 1288, 136, 33, 3), (4, 77, 768, 320, 64, 4),
     (2, 130, 40, 200, 128, 2), (3, 257, 320, 320, 16, 2), (2, 1100, 648, 640, 8, 3), (1, 33, 64, 96, 300, 1),
     (6, 500, 320, 960, 32, 2), (140, 3, 640, 320, 5, 7),
+    # ranks up to 16 beside the weights' slices: the split kernel's tiles and the shared ones
+    (4, 77, 768, 640, 4, 5), (3, 33, 520, 72, 16, 2), (2, 64, 1288, 136, 1, 2), (1, 500, 1280, 320, 7, 1),
+    (40, 32, 584, 1288, 12, 6), (9, 300, 584, 648, 10, 4), (5, 127, 8, 64, 2, 2), (2, 1000, 72, 8, 16, 3),
+    (64, 65, 56, 72, 13, 9),
 ]
 
 
@@ -90,7 +94,8 @@ def test_layouts(shape, xl, yl, dtype):
     check(ref.heads_to_rows(g) if yl else g, *expected(t, dtype, x), dtype)
 
 
-@pytest.mark.parametrize("shape", [(6, 1, 1280, 320, 8, 2), (3, 90, 320, 320, 16, 2), (2, 600, 640, 640, 4, 2)],
+@pytest.mark.parametrize("shape", [(6, 1, 1280, 320, 8, 2), (3, 90, 320, 320, 16, 2), (2, 600, 640, 640, 4, 2), (8, 600, 640, 640, 4, 2),
+                                   (8, 600, 640, 640, 24, 2)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_no_adapter_gives_the_plain_projections_bits(shape):
     """Requests without an adapter, beside ones that have it, and values of adapters that
@@ -109,14 +114,15 @@ def test_no_adapter_gives_the_plain_projections_bits(shape):
     assert torch.isfinite(y).all() and not torch.equal(y[1], plain[1])
 
 
-def test_large_values_of_one_request_stay_in_it():
+@pytest.mark.parametrize("L,R", [(5, 8), (40, 8), (40, 24)])
+def test_large_values_of_one_request_stay_in_it(L, R):
     """An adapter that overflows its own request's rows leaves the neighbours in a tile alone."""
     import torch
-    t = make(8, 5, 320, 128, 8, 8, "f16", 6)
+    t = make(8, L, 320, 128, R, 8, "f16", 6)
     t["ids"] = torch.arange(8, dtype=torch.int32, device="cuda")
     t["up"][3] = float("inf")
     t["down"][5] = float("nan")
-    y = torch.empty(8, 5, 128, dtype=torch.float16, device="cuda")
+    y = torch.empty(8, L, 128, dtype=torch.float16, device="cuda")
     call(t, y)
     torch.cuda.synchronize()
     ok = [0, 1, 2, 4, 6, 7]
@@ -134,7 +140,8 @@ def test_writes_its_rows_alone_and_the_workspace_it_asked_for():
     assert (buf[3 * 21 * 72:] == 7).all() and (ws[need:] == 9).all()
 
 
-@pytest.mark.parametrize("B,L,K,N", [(4, 40, 640, 320), (90, 40, 584, 640), (300, 1, 1280, 640), (300, 1, 320, 640)],
+@pytest.mark.parametrize("B,L,K,N", [(4, 40, 640, 320), (90, 40, 584, 640), (20, 200, 584, 640), (300, 1, 1280, 640),
+                                     (300, 1, 320, 640)],
                          ids=lambda v: str(v))
 def test_a_requests_bits_do_not_depend_on_the_others(B, L, K, N):
     """One request alone (the split kernel past 512 channels), and among others with other
