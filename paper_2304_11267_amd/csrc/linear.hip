@@ -192,43 +192,93 @@ __device__ __forceinline__ u32x4 adapter_chunk(const uint16_t* row, int r0, int 
     return v;
 }
 
-// sum[b] = up T^T for the 32 token rows from row0 and the 32 channels from n0 + 32 b, in the
-// accumulators' layout; it is the first addend of those channels' sums.  Every row sees its
-// own request's adapter alone, infinities and all, and a request's bits do not depend on its
-// neighbours in a tile.
-//   Requests of 32 rows and more: 16 ranks a step on the matrix core, one request's rows at
-// a time (at most two in 32 rows), the others' T as zeros and their sums dropped.
-//   Shorter ones: each lane multiplies its row's T with its own channels' rows of up (16
-// tokens of 16 requests, K = N = 1280, R = 8: one request after the other took 9 us more).
+// sum[g][e] = the product of T's row t with the rows of up for channels n + dn g + e: 16
+// reads of up in flight.
+template <int ET, int W, int NG>
+__device__ __forceinline__ void adapter_dots(const uint16_t* up, const uint16_t* t, int R, int n, int dn, int N,
+                                             float (&sum)[NG][4]) {
+    constexpr int CH = 4 / NG;   // chunks of 8 ranks at a time
+    const uint16_t* p[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        p[g] = up + (size_t)min(n + dn * g, N - 4) * R;   // (groups of 4 channels end together with N)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[g][e] = 0.0f;
+    }
+    for (int r0 = 0; r0 < R; r0 += 8 * CH) {
+        u32x4 tf[CH], u[CH][NG][4];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            tf[c] = u32x4{0u, 0u, 0u, 0u};
+            if (r0 + 8 * c < R) tf[c] = *(const u32x4*)(t + r0 + 8 * c);
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[c][g][e] = adapter_chunk<W>(p[g] + e * R, r0 + 8 * c, R);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[g][e] = dot8<ET>(u[c][g][e], tf[c], sum[g][e]);
+    }
+}
+// f(W) with the widest reads that R leaves aligned
+template <typename F>
+__device__ __forceinline__ void adapter_width(int R, F f) {
+    if (R % 8 == 0) f(std::integral_constant<int, 8>{});
+    else if (R % 4 == 0) f(std::integral_constant<int, 4>{});
+    else f(std::integral_constant<int, 1>{});
+}
+
+// up T^T for the token rows and channels of a tile, the last addend of their sums.  Every
+// row sees its own request's adapter alone, infinities and all, and a request's bits do not
+// depend on its neighbours in a tile.
+//   Requests of 32 rows and more: adapter_sums, 16 ranks a step on the matrix core, one
+// request's rows at a time (at most two in 32 rows), the others' T as zeros and their sums
+// dropped.
+//   Shorter ones: adapter_dots, each lane multiplies its row's T with its own channels' rows
+// of up (16 tokens of 16 requests, K = N = 1280, R = 8: one request after the other took 9
+// us more).
 constexpr int kAdapterRows = 32;
+constexpr int kUpSteps = 4;   // steps of 16 ranks in flight
+
+// This lane's row's adapter, its up and its T (false: none)
+__device__ __forceinline__ bool adapter_of_row(const AdapterSet& ad, int row, int M, int N, int L, const uint16_t** up,
+                                               const uint16_t** t) {
+    if (row >= M) return false;
+    const int id = ad.ids[row / L];
+    if (id < 0 || id >= ad.count) return false;
+    *up = ad.up + (size_t)id * N * ad.R;
+    *t = ad.t + (size_t)row * ad.Rp;
+    return true;
+}
+
+// sum[b] for the 32 token rows from row0 and the 32 channels from n0 + 32 b, in the
+// accumulators' layout
 template <int ET, int NB, int W>
 __device__ __forceinline__ void adapter_sums_w(const AdapterSet& ad, int row0, int n0, int M, int N, int L,
                                                f32x16 (&sum)[NB]) {
     const int l32 = lane_id() & 31, half = lane_id() >> 5;
-    const int row = min(row0 + l32, M - 1);
     if (L < kAdapterRows) {
-        const int id = ad.ids[row / L];
-        if (id < 0 || id >= ad.count) return;
-        const uint16_t* up = ad.up + (size_t)id * N * ad.R;
-        for (int r0 = 0; r0 < ad.R; r0 += 8) {
-            const u32x4 tf = *(const u32x4*)(ad.t + (size_t)row * ad.Rp + r0);
+        const uint16_t *up, *t;
+        if (!adapter_of_row(ad, row0 + l32, M, N, L, &up, &t)) return;
 #pragma unroll
-            for (int t = 0; t < 2 * NB; ++t) {   // 8 channels at a time, two groups of 4
-                u32x4 u[8];
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int r = 0; r < 8; r += 4) {
-                    const uint16_t* p = up + (size_t)min(n0 + 16 * t + 2 * r + 4 * half, N - 4) * ad.R;
-                    asm volatile("" : "+v"(p));   // (kept across steps, the rows' addresses take 64 registers)
+            for (int q = 0; q < 2; ++q) {
+                float d[2][4];
+                adapter_dots<ET, W, 2>(up, t, ad.R, n0 + 32 * b + 16 * q + 4 * half, 8, N, d);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) u[r + e] = adapter_chunk<W>(p + e * ad.R, r0, ad.R);
-                }
+                for (int g = 0; g < 2; ++g)
 #pragma unroll
-                for (int r = 0; r < 8; ++r) sum[t / 2][8 * (t & 1) + r] = dot8<ET>(u[r], tf, sum[t / 2][8 * (t & 1) + r]);
-                __builtin_amdgcn_sched_barrier(0);   // (all of them at once take 290 registers)
+                    for (int e = 0; e < 4; ++e) sum[b][8 * q + 4 * g + e] = d[g][e];
             }
-        }
         return;
     }
+    const int row = min(row0 + l32, M - 1);
     const int last = min(row0 + 31, M - 1) / L;
     for (int b = row0 / L; b <= last; ++b) {
         const int id = __builtin_amdgcn_readfirstlane(ad.ids[b]);
@@ -239,15 +289,24 @@ __device__ __forceinline__ void adapter_sums_w(const AdapterSet& ad, int row0, i
         for (int t = 0; t < NB; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) own[t][r] = 0.0f;
-        for (int s = 0; s < ad.Rp / 16; ++s) {
-            const int r0 = 16 * s + 8 * half;
-            u32x4 tf = {0u, 0u, 0u, 0u};
-            if (mine) tf = *(const u32x4*)(ad.t + (size_t)row * ad.Rp + r0);
+        const uint16_t* up[NB];
 #pragma unroll
-            for (int t = 0; t < NB; ++t) {
-                const int n = min(n0 + 32 * t + l32, N - 1);
-                own[t] = mfma32x32x16<ET>(adapter_chunk<W>(ad.up + ((size_t)id * N + n) * ad.R, r0, ad.R), tf, own[t]);
+        for (int t = 0; t < NB; ++t) up[t] = ad.up + ((size_t)id * N + min(n0 + 32 * t + l32, N - 1)) * ad.R;
+        for (int s0 = 0; s0 < ad.Rp / 16; s0 += kUpSteps) {
+            u32x4 tf[kUpSteps], uf[kUpSteps][NB];
+#pragma unroll
+            for (int s = 0; s < kUpSteps; ++s) {
+                const int r0 = 16 * (s0 + s) + 8 * half;   // from R on: zeros
+                tf[s] = u32x4{0u, 0u, 0u, 0u};
+                if (mine && r0 < ad.Rp) tf[s] = *(const u32x4*)(ad.t + (size_t)row * ad.Rp + r0);
+#pragma unroll
+                for (int t = 0; t < NB; ++t) uf[s][t] = adapter_chunk<W>(up[t], r0, ad.R);
             }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < kUpSteps; ++s)
+#pragma unroll
+                for (int t = 0; t < NB; ++t) own[t] = mfma32x32x16<ET>(uf[s][t], tf[s], own[t]);
         }
 #pragma unroll
         for (int t = 0; t < NB; ++t)
@@ -263,9 +322,9 @@ __device__ __forceinline__ void adapter_sums(const AdapterSet& ad, int row0, int
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum[t][r] = 0.0f;
     if (row0 >= M) return;
-    if (ad.R % 8 == 0) adapter_sums_w<ET, NB, 8>(ad, row0, n0, M, N, L, sum);
-    else if (ad.R % 4 == 0) adapter_sums_w<ET, NB, 4>(ad, row0, n0, M, N, L, sum);
-    else adapter_sums_w<ET, NB, 1>(ad, row0, n0, M, N, L, sum);
+    adapter_width(ad.R, [&](auto w) __attribute__((always_inline)) {
+        adapter_sums_w<ET, NB, decltype(w)::value>(ad, row0, n0, M, N, L, sum);
+    });
 }
 
 // Wait until at most `ahead` slices of this wave's copies are still in flight.
@@ -468,9 +527,10 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     // 7.2 / 7.5 us (7.9 with them in the loop of every slice), 1024x1280x1280 11.3 /
     // 11.4 (12.0), 2048x2560x640 19.4 / 19.0 (20.0).
     f32x16 acc[2] = {zero, zero}, tot[2] = {zero, zero};
-    // the adapters' part comes first, while the first slices are on their way
+    // the adapters' part, the last addend: AdapterSet's while the first slices are on their way
+    [[maybe_unused]] f32x16 more[2] = {zero, zero};
     if constexpr (adapters_are<AdapterSet, AD...>)
-        adapter_sums<ET>(adapters_of(ad...), m0 + 32 * wave, n0, M, N, L, FOLD ? tot : acc);
+        adapter_sums<ET>(adapters_of(ad...), m0 + 32 * wave, n0, M, N, L, more);
     const int run = K > kSplitMinK ? (nk + kRuns - 1) / kRuns : nk;
     if constexpr (!FOLD) {
         // (a loop of its own: as slices opened by a run's first one, products with a
@@ -511,7 +571,7 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     } else
     for (int i0 = 0; i0 < nk; i0 += run) {
         slice(i0, std::true_type{}, acc, [&]() __attribute__((always_inline)) {
-            if (i0 > 0) {   // (tot is zero, or the adapters' part, before)
+            if (i0 > 0) {
                 __builtin_amdgcn_sched_barrier(0);
                 tot[0] += acc[0];
                 tot[1] += acc[1];
@@ -522,8 +582,7 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
         for (int i = i0 + 1; i < min(i0 + run, nk); ++i) slice(i, std::false_type{}, acc, [] {});
     }
 
-    // FUSED: up T^T, added to a row's finished sum
-    [[maybe_unused]] f32x16 more[2] = {zero, zero};
+    // FUSED: up T^T
     if constexpr (FUSED) {
         if (adapted) {
             float t[8];
@@ -551,7 +610,7 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float f = FOLD ? tot[t][4 * g + e] + acc[t][4 * g + e] : acc[t][4 * g + e];
-                    if constexpr (FUSED) f += more[t][4 * g + e];
+                    if constexpr (sizeof...(AD) > 0) f += more[t][4 * g + e];
                     v[e] = f + to_float<ET>((uint16_t)(bias[t][g][e >> 1] >> (16 * (e & 1))));
                 }
                 u32x2 w;
@@ -599,14 +658,16 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
 // K = 1280 is 328 KB through one CU); with one slice per wave (ST = 1) two or
 // three workgroups share a CU and cover each other's waits, which measured
 // faster than deeper rings (512x1280x1280: 9.1 against 9.4 us with ST = 2).
-template <int TM, int TN, int ST, int RR = 0>
+template <int TM, int TN, int ST, typename... AD>
 struct KsGeom {
-    static constexpr int kSlice = (TM + TN + RR) * kBK * 2;       // bytes (RR rows of an adapter's down)
+    static constexpr int RR = adapters_are<AdapterFused, AD...> ? kRankRows : 0;   // rows of down in a slice
+    static constexpr int kSlice = (TM + TN + RR) * kBK * 2;       // bytes
     static constexpr int kCopies = kSlice / 1024;                 // copy instructions per slice
     static constexpr int kOutRow = TN * 4 + 16;                   // bytes per row of a partial tile
     static constexpr int kRing = kRuns * ST * kSlice;
-    static constexpr int kTiles = kRuns * TM * kOutRow;           // partial tiles; with RR, T's parts and the adapter's tile
-    static constexpr int kPart = kTiles + (RR > 0 ? kRuns * TM * RR * 4 + TM * kOutRow : 0);
+    static constexpr int kMore = kRuns * TM * kOutRow;            // partial tiles, then the adapters' tile, then T's parts
+    static constexpr int kT = kMore + (sizeof...(AD) > 0 ? TM * kOutRow : 0);
+    static constexpr int kPart = kT + kRuns * TM * RR * 4;
     static constexpr int kLds = kRing > kPart ? kRing : kPart;
     static_assert(kLds <= 160 * 1024 && TM % 32 == 0 && TN % 32 == 0, "geometry");
     static_assert(kCopies * (ST - 1) < 64, "copies in flight fit vmcnt");
@@ -627,7 +688,7 @@ __device__ __forceinline__ void ks_wait(int n) {
 template <int ET, bool YH, int TM, int TN, int ST, typename... AD>
 __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_kernel(const LinGroup grp, const AD... ad) {
     constexpr bool FUSED = adapters_are<AdapterFused, AD...>;
-    using G = KsGeom<TM, TN, ST, FUSED ? kRankRows : 0>;
+    using G = KsGeom<TM, TN, ST, AD...>;
     constexpr int MB = TM / 32, NB = TN / 32, KS = kBK / 16;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = lane_id();
@@ -716,11 +777,29 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
     for (int a = 0; a < MB; ++a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dacc[a][r] = 0.0f;
-    [[maybe_unused]] f32x16 more[MB][NB];   // the adapters' part, while the first slices are on their way
-    if constexpr (adapters_are<AdapterSet, AD...>) {
-        if (wave == 0) {
+    // AdapterSet: the adapters' part while the first slices are on their way; a wave takes a
+    // quarter of the channels, or a block of 32 x 32
+    constexpr bool APART = adapters_are<AdapterSet, AD...>;
+    constexpr int kWaveN = TN / kRuns, NG = kWaveN / 8;
+    [[maybe_unused]] float dots[MB][NG][4];
+    [[maybe_unused]] f32x16 block[1];
+    if constexpr (APART) {
+        const AdapterSet set = adapters_of(ad...);
+        if (L < kAdapterRows) {
 #pragma unroll
-            for (int a = 0; a < MB; ++a) adapter_sums<ET>(adapters_of(ad...), m0 + 32 * a, n0, M, N, L, more[a]);
+            for (int a = 0; a < MB; ++a) {
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dots[a][g][e] = 0.0f;
+                const uint16_t *up, *t;
+                if (adapter_of_row(set, m0 + 32 * a + l32, M, N, L, &up, &t))
+                    adapter_width(set.R, [&](auto w) __attribute__((always_inline)) {
+                        adapter_dots<ET, decltype(w)::value, NG>(up, t, set.R, n0 + kWaveN * wave + 4 * half, 8, N, dots[a]);
+                    });
+            }
+        } else if (wave < MB * NB) {
+            adapter_sums<ET>(set, m0 + 32 * (wave / NB), n0 + 32 * (wave % NB), M, N, L, block);
         }
     }
 
@@ -766,17 +845,6 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
                 for (int b = 0; b < NB; ++b) acc[a][b] = mfma32x32x16<ET>(wf[b][s], xf[a][s], acc[a][b]);
     }
 
-    // the adapters' part is added to the first run, in the order of the shared tiles' sums
-    // (and so with the same bits)
-    if constexpr (adapters_are<AdapterSet, AD...>) {
-        if (wave == 0) {
-#pragma unroll
-            for (int a = 0; a < MB; ++a)
-#pragma unroll
-                for (int b = 0; b < NB; ++b) acc[a][b] = more[a][b] + acc[a][b];
-        }
-    }
-
     // 16 bytes per lane: chunk q = tid + 256j is tile row q / (TN / 8), channels
     // n = n0 + 8 (q % (TN / 8)) .. + 7, the same n for every j
     constexpr int kCols = TN / 8;
@@ -804,7 +872,7 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
                     *(f32x4*)(part + (32 * a + l32) * G::kOutRow + (32 * b + 8 * g + 4 * half) * 4) = v;
                 }
         if constexpr (FUSED) {   // T's part, [TM][16 ranks]
-            char* tp = smem + G::kTiles + wave * (TM * kRankRows * 4);
+            char* tp = smem + G::kT + wave * (TM * kRankRows * 4);
 #pragma unroll
             for (int a = 0; a < MB; ++a)
 #pragma unroll
@@ -813,7 +881,21 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
                         f32x4{dacc[a][4 * q], dacc[a][4 * q + 1], dacc[a][4 * q + 2], dacc[a][4 * q + 3]};
         }
     }
-    [[maybe_unused]] constexpr int kMore = G::kTiles + kRuns * TM * kRankRows * 4;   // the adapter's tile
+    if constexpr (APART) {
+        if (L < kAdapterRows) {
+#pragma unroll
+            for (int a = 0; a < MB; ++a)
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+                    *(f32x4*)(smem + G::kMore + (32 * a + l32) * G::kOutRow + (kWaveN * wave + 8 * g + 4 * half) * 4) =
+                        f32x4{dots[a][g][0], dots[a][g][1], dots[a][g][2], dots[a][g][3]};
+        } else if (wave < MB * NB) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(f32x4*)(smem + G::kMore + (32 * (wave / NB) + l32) * G::kOutRow + (32 * (wave % NB) + 8 * g + 4 * half) * 4) =
+                    f32x4{block[0][4 * g], block[0][4 * g + 1], block[0][4 * g + 2], block[0][4 * g + 3]};
+        }
+    }
     if constexpr (FUSED) {
         // T whole, the runs in the shared tiles' order, then up T^T by a wave for each 32 x 32
         const AdapterFused f = adapters_of(ad...);
@@ -831,7 +913,7 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
             for (int w = 0; w < kRuns; ++w)
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    const f32x4 p = *(const f32x4*)(smem + G::kTiles + w * (TM * kRankRows * 4) +
+                    const f32x4 p = *(const f32x4*)(smem + G::kT + w * (TM * kRankRows * 4) +
                                                     (32 * a + l32) * kRankRows * 4 + (8 * q + 4 * half) * 4);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) t[4 * q + e] += p[e];
@@ -842,7 +924,7 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
             if (adapted) sum = mfma32x32x16<ET>(upf, fused_t<ET>(t, f.scales ? f.scales[id] : 1.0f, f.R, half), sum);
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *(f32x4*)(smem + kMore + (32 * a + l32) * G::kOutRow + (32 * b + 8 * g + 4 * half) * 4) =
+                *(f32x4*)(smem + G::kMore + (32 * a + l32) * G::kOutRow + (32 * b + 8 * g + 4 * half) * 4) =
                     f32x4{sum[4 * g], sum[4 * g + 1], sum[4 * g + 2], sum[4 * g + 3]};
         }
     }
@@ -861,8 +943,8 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
                 lo += *(const f32x4*)p;
                 hi += *(const f32x4*)(p + 16);
             }
-            if constexpr (FUSED) {
-                const char* p = smem + kMore + r * G::kOutRow + c8 * 32;
+            if constexpr (sizeof...(AD) > 0) {
+                const char* p = smem + G::kMore + r * G::kOutRow + c8 * 32;
                 lo += *(const f32x4*)p;
                 hi += *(const f32x4*)(p + 16);
             }
@@ -881,11 +963,12 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
 }
 
 // T = s_i down_i x for the rows of the batch items that have an adapter: a workgroup
-// takes 16 rows of one item and 16 RB ranks, its four waves a quarter of the channels
+// takes 16 TB rows of one item and 16 RB ranks, its four waves a quarter of the channels
 // each.  T^T = down x^T on 16x16x32 MFMAs, whose operands come straight from memory, 16
 // bytes a lane: a row's 64 bytes meet in one instruction, and the next one takes the
-// other half of its cache lines.  Bound by reading x once (rows of other items, and the
-// adapters, are read from the cache).  T is rounded to the tensors' type, the type that
+// other half of its cache lines.  Bound by reading x once where there are few ranks, by the
+// caches' reads of down where there are many (4 requests of 1024 rows, K = N = 1280, R 128:
+// 51.3 us in all with TB = 1, 49.4 with 2).  T is rounded to the tensors' type, the type that
 // the second product's matrix instructions take; the scale goes in before, in fp32.
 constexpr int kDownSteps = 4;   // steps of 32 channels in flight
 struct DownKernel {
@@ -906,35 +989,39 @@ __device__ __forceinline__ f32x4 mfma16x16x32(u32x4 a, u32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-template <int ET, bool XH, int RB>
+template <int ET, bool XH, int RB, int TB>
 __global__ __launch_bounds__(256) void adapter_down_kernel(const DownKernel a) {
-    __shared__ f32x4 part[kRuns - 1][RB][64];
+    __shared__ f32x4 part[kRuns - 1][RB * TB][64];
     const int lane = lane_id();
     const int l16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int b = blockIdx.x / a.tiles, l0 = (blockIdx.x - b * a.tiles) * 16;
+    const int b = blockIdx.x / a.tiles, l0 = (blockIdx.x - b * a.tiles) * 16 * TB;
     const int r0 = blockIdx.y * 16 * RB;
     const int id = a.ids[b];
     if (id < 0 || id >= a.count) return;
     const float inv_xhw = 1.0f / (float)a.xhw;
-    const int l = min(l0 + l16, a.L - 1);
-    const uint16_t* x = a.x + row_base<XH>(b * a.L + l, a.L, a.K, a.xhw);
+    const uint16_t* x[TB];
     const uint16_t* d[RB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) x[t] = a.x + row_base<XH>(b * a.L + min(l0 + 16 * t + l16, a.L - 1), a.L, a.K, a.xhw);
 #pragma unroll
     for (int j = 0; j < RB; ++j) d[j] = a.down + ((size_t)id * a.R + min(r0 + 16 * j + l16, a.R - 1)) * a.K;
 
-    f32x4 acc[RB];
+    f32x4 acc[RB][TB];
 #pragma unroll
-    for (int j = 0; j < RB; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < RB; ++j)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) acc[j][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int steps = (a.K + 31) / 32;
     const int per = (steps + kRuns - 1) / kRuns;
     const int first = wave * per, end = min(first + per, steps);
     for (int s0 = first; s0 < end; s0 += kDownSteps) {
-        u32x4 xv[kDownSteps], dv[kDownSteps][RB];
+        u32x4 xv[kDownSteps][TB], dv[kDownSteps][RB];
 #pragma unroll
         for (int u = 0; u < kDownSteps; ++u) {
             const int c = 32 * (s0 + u) + 8 * quad, cc = min(c, a.K - 8);
-            xv[u] = *(const u32x4*)(x + chan_offset<XH>(cc, a.L, a.xhw, inv_xhw));
+#pragma unroll
+            for (int t = 0; t < TB; ++t) xv[u][t] = *(const u32x4*)(x[t] + chan_offset<XH>(cc, a.L, a.xhw, inv_xhw));
 #pragma unroll
             for (int j = 0; j < RB; ++j) dv[u][j] = *(const u32x4*)(d[j] + cc);
         }
@@ -942,31 +1029,38 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(const DownKernel a) {
         for (int u = 0; u < kDownSteps; ++u) {
             // past this wave's channels both factors are zeros (a zero and a NaN are no zero)
             const bool out = s0 + u >= end || 32 * (s0 + u) + 8 * quad >= a.K;
-            if (out) xv[u] = u32x4{0u, 0u, 0u, 0u};
+            const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
-            for (int j = 0; j < RB; ++j) acc[j] = mfma16x16x32<ET>(out ? xv[u] : dv[u][j], xv[u], acc[j]);
+            for (int j = 0; j < RB; ++j)
+#pragma unroll
+                for (int t = 0; t < TB; ++t)
+                    acc[j][t] = mfma16x16x32<ET>(out ? zero : dv[u][j], out ? zero : xv[u][t], acc[j][t]);
         }
     }
     if (wave > 0) {
 #pragma unroll
-        for (int j = 0; j < RB; ++j) part[wave - 1][j][lane] = acc[j];
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int t = 0; t < TB; ++t) part[wave - 1][j * TB + t][lane] = acc[j][t];
     }
     __syncthreads();
     if (wave > 0) return;
     const float scale = a.scales ? a.scales[id] : 1.0f;
 #pragma unroll
-    for (int j = 0; j < RB; ++j) {
+    for (int j = 0; j < RB; ++j)
 #pragma unroll
-        for (int w = 0; w < kRuns - 1; ++w) acc[j] += part[w][j][lane];
-        // this lane's 4 ranks of its row; ranks from R on are zeros
-        const int r = r0 + 16 * j + 4 * quad;
-        if (l0 + l16 < a.L && r < a.Rp) {
-            float v[4];
+        for (int t = 0; t < TB; ++t) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = r + e < a.R ? acc[j][e] * scale : 0.0f;
-            *(u32x2*)(a.t + (size_t)(b * a.L + l) * a.Rp + r) = u32x2{pack2<ET>(v[0], v[1]), pack2<ET>(v[2], v[3])};
+            for (int w = 0; w < kRuns - 1; ++w) acc[j][t] += part[w][j * TB + t][lane];
+            // this lane's 4 ranks of its row; ranks from R on are zeros
+            const int r = r0 + 16 * j + 4 * quad, l = l0 + 16 * t + l16;
+            if (l < a.L && r < a.Rp) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = r + e < a.R ? acc[j][t][e] * scale : 0.0f;
+                *(u32x2*)(a.t + (size_t)(b * a.L + l) * a.Rp + r) = u32x2{pack2<ET>(v[0], v[1]), pack2<ET>(v[2], v[3])};
+            }
         }
-    }
 }
 
 // tm x tn tiles of one batch item
@@ -1008,7 +1102,7 @@ long long number_tiles(LinGroup& g, const LinearArgs* a, int tm, int tn) {
 
 template <int ET, bool YH, int TM, int TN, int ST, typename... AD>
 hipError_t launch_ks(LinGroup& g, const LinearArgs* a, const AD&... ad) {
-    using G = KsGeom<TM, TN, ST, adapters_are<AdapterFused, AD...> ? kRankRows : 0>;
+    using G = KsGeom<TM, TN, ST, AD...>;
     const long long nblk = number_tiles(g, a, TM, TN);
     if (nblk > 0x7fffffff) return hipErrorInvalidValue;
     auto k = linear_ksplit_kernel<ET, YH, TM, TN, ST, AD...>;
@@ -1102,10 +1196,15 @@ hipError_t make_group(LinGroup& g, const LinearArgs* a, int n) {
 template <int ET, bool XH>
 hipError_t launch_down(const LinearArgs& a, const AdapterArgs& d) {
     DownKernel k{(const uint16_t*)a.x, (const uint16_t*)d.down, d.ids, d.scales, (uint16_t*)d.t,
-                 a.L, a.K, a.x_heads ? a.K / a.H : 1, d.R, adapter_rank_padded(d.R), d.count, (a.L + 15) / 16};
+                 a.L, a.K, a.x_heads ? a.K / a.H : 1, d.R, adapter_rank_padded(d.R), d.count, 0};
     const int rb = d.R <= 16 ? 1 : d.R <= 32 ? 2 : 4;
+    const bool two = rb > 1 && a.L >= 32;
+    const int rows = two ? 32 : 16;
+    k.tiles = (a.L + rows - 1) / rows;
     const dim3 grid((unsigned)(a.B * k.tiles), (unsigned)((d.R + 16 * rb - 1) / (16 * rb)));
-    auto f = rb == 1 ? adapter_down_kernel<ET, XH, 1> : rb == 2 ? adapter_down_kernel<ET, XH, 2> : adapter_down_kernel<ET, XH, 4>;
+    auto f = rb == 1   ? adapter_down_kernel<ET, XH, 1, 1>
+             : rb == 2 ? (two ? adapter_down_kernel<ET, XH, 2, 2> : adapter_down_kernel<ET, XH, 2, 1>)
+                       : (two ? adapter_down_kernel<ET, XH, 4, 2> : adapter_down_kernel<ET, XH, 4, 1>);
     hipLaunchKernelGGL(f, grid, dim3(256), 0, (hipStream_t)a.stream, k);
     return hipGetLastError();
 }
