@@ -8,11 +8,11 @@
 //
 // The angles depend on the token and the pair alone, so a workgroup takes a few
 // tokens with all of their heads, of q and k both, and has each angle's cosine and
-// sine once, in LDS, beside the tokens' places.  t is reduced to a part of a turn in 64
+// sine once, from LDS, times the gammas in registers of the lanes that turn with it.  t is reduced to a part of a turn in 64
 // bits (at a million positions a product in 32 bits would be off by 0.06), its sine and
 // cosine are taken in 32.  A row belongs to G lanes, G the power of two that holds its
 // items of V pairs: the sum of squares goes through them in DPP moves, and the row stays
-// in registers between its read and its write, four rows of a lane in flight.
+// in registers between its read and its write.
 #include "device.h"
 #include "launch.h"
 
@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kNrThreads = 256;
 constexpr int kNrTokens = 8;     // most tokens of a workgroup (2^3)
-constexpr int kNrRows = 4;       // rows in flight of a group of lanes
+constexpr int kNrRows = 2;       // rows of 4 pairs a lane in flight (of 8 pairs: half as many)
 
 struct NrKernel {
     const uint16_t* x[2];
@@ -64,16 +64,16 @@ __device__ __forceinline__ float nr_sum(float v) {
     return v;
 }
 
-// V consecutive values at p, to fp32
+// V consecutive values as they lie in memory
+template <int V>
+using NrRaw = typename std::conditional<V == 1, uint16_t, typename std::conditional<V == 4, u32x2, u32x4>::type>::type;
 template <int ET, int V>
-__device__ __forceinline__ void nr_load(const uint16_t* p, float* f) {
+__device__ __forceinline__ void nr_widen(NrRaw<V> w, float* f) {
     if constexpr (V == 1) {
-        f[0] = to_float<ET>(p[0]);
+        f[0] = to_float<ET>(w);
     } else {
-        static_assert(V == 4, "");
-        const u32x2 w = *(const u32x2*)p;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < V / 2; ++i) {
             f[2 * i] = to_float<ET>((uint16_t)(w[i] & 0xffffu));
             f[2 * i + 1] = to_float<ET>((uint16_t)(w[i] >> 16));
         }
@@ -81,136 +81,182 @@ __device__ __forceinline__ void nr_load(const uint16_t* p, float* f) {
 }
 template <int ET, int V>
 __device__ __forceinline__ void nr_store(uint16_t* p, const float* f) {
-    if constexpr (V == 1) p[0] = from_float<ET>(f[0]);
-    else *(u32x2*)p = u32x2{pack2<ET>(f[0], f[1]), pack2<ET>(f[2], f[3])};
+    if constexpr (V == 1) {
+        p[0] = from_float<ET>(f[0]);
+    } else {
+        NrRaw<V> w;
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) w[i] = pack2<ET>(f[2 * i], f[2 * i + 1]);
+        *(NrRaw<V>*)p = w;
+    }
 }
 
-// IPL items of V pairs a lane, G lanes a row
-template <int ET, int V, int IPL, int G, bool HALVES>
+// IPL items of V pairs a lane, G lanes a row, IDX the type of places in the tensors.  With
+// q and k, two waves each: what differs between them is the same for a whole wave.
+template <int ET, int V, int IPL, int G, bool HALVES, typename IDX>
 __global__ __launch_bounds__(kNrThreads) void norm_rotate_kernel(const NrKernel a) {
+    using Raw = NrRaw<V>;
+    constexpr int kRows = V == 8 ? kNrRows / 2 : kNrRows;
     extern __shared__ __attribute__((aligned(16))) float2 turn[];   // [tokens][D / 2]
-    __shared__ size_t xplace[kNrTokens], yplace[kNrTokens];         // of a token's head 0
+    __shared__ IDX xplace[kNrTokens], yplace[kNrTokens];            // of a token's head 0
     const int D = a.D, H = a.H, L = a.L, pairs = D / 2;
     const int m0 = blockIdx.x << a.log_tokens;
     const int tokens = min(a.tokens, a.M - m0);
 
     if (threadIdx.x < tokens) {
         const int m = m0 + threadIdx.x, b = m / L, l = m - b * L;
-        const size_t heads = ((size_t)b * H * L + l) * D, rows = (size_t)m * H * D;
+        const IDX heads = ((IDX)b * H * L + l) * D, rows = (IDX)m * H * D;
         xplace[threadIdx.x] = a.x_heads ? heads : rows;
         yplace[threadIdx.x] = a.y_heads ? heads : rows;
     }
+    // an angle's position and frequency (its pair among the turned ones)
     const float inv_pairs = 1.0f / (float)pairs;
-    for (int i = threadIdx.x; i < tokens * pairs; i += kNrThreads) {
+    auto place_of = [&](int i, int* at, float* freq) __attribute__((always_inline)) {
         const int t = nr_div(i, pairs, inv_pairs), p = i - t * pairs;
-        float s = 0.0f, c = 1.0f;
-        if (p < a.P) {
+        *at = 0;
+        *freq = 0.0f;   // an angle of 0 for the pairs that are not turned
+        if (i < tokens * pairs && p < a.P) {
             const int axis = (p >= a.end[0]) + (p >= a.end[1]) + (p >= a.end[2]);
             const int m = m0 + t, b = m / L, l = m - b * L;
-            const int at = a.pos[((size_t)b * a.pos_batch + l) * a.A + axis];
-            double r = (double)at * ((double)a.freqs[p] * 0.15915494309189535);   // turns
-            r -= rint(r);
-            sincospif(2.0f * (float)r, &s, &c);
+            *at = a.pos[((size_t)b * a.pos_batch + l) * a.A + axis];
+            *freq = a.freqs[p];
         }
+    };
+    int at;
+    float freq;
+    place_of(threadIdx.x, &at, &freq);
+    __syncthreads();
+
+    const int lane = threadIdx.x % G;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int w = a.n > 1 ? wave >> 1 : 0;                       // this wave's tensor
+    const int team = (threadIdx.x - (w << 7)) / G, teams = (a.n > 1 ? 128 : 256) / G;
+    // this team's token, and its heads h0, h0 + hstep, ...
+    const int t = team & (a.tokens - 1), h0 = team >> a.log_tokens, hstep = teams >> a.log_tokens;
+    const bool in = t < tokens;
+    const IDX xstep = a.x_heads ? (IDX)L * D : D, ystep = a.y_heads ? (IDX)L * D : D;
+    const uint16_t* X = a.x[w];
+    uint16_t* Y = a.y[w];
+    const IDX from = in ? xplace[t] : 0, to = in ? yplace[t] : 0;
+    const float inv_d = 1.0f / (float)D;
+    // the first and second values of item i's pairs
+    auto first = [&](int i) { return !HALVES ? 2 * V * i : V * i < a.P ? V * i : V * i + a.P; };
+    auto second = [&](int i) { return !HALVES ? 2 * V * i + V : V * i < a.P ? V * i + a.P : V * i + pairs; };
+    Raw raw[kRows][IPL][2];
+    auto load = [&](int h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)
+#pragma unroll
+            for (int k = 0; k < IPL; ++k) {
+                const int i = lane + G * k;
+                raw[u][k][0] = raw[u][k][1] = Raw{};
+                if (in && h + u * hstep < H && V * i < pairs) {
+                    const IDX row = from + (h + u * hstep) * xstep;
+                    raw[u][k][0] = *(const Raw*)(X + (IDX)(row + first(i)));
+                    raw[u][k][1] = *(const Raw*)(X + (IDX)(row + second(i)));
+                }
+            }
+    };
+    load(h0);   // on its way beside the angles
+    float g[IPL][2 * V];
+    const uint16_t* Gamma = a.norm ? a.gamma[w] : nullptr;
+#pragma unroll
+    for (int k = 0; k < IPL; ++k) {
+        const int i = lane + G * k;
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) g[k][e] = 1.0f;
+        if (Gamma && V * i < pairs) {
+            nr_widen<ET, V>(*(const Raw*)(Gamma + first(i)), g[k]);
+            nr_widen<ET, V>(*(const Raw*)(Gamma + second(i)), g[k] + V);
+        }
+    }
+
+    for (int i = threadIdx.x; i < tokens * pairs; i += kNrThreads) {
+        if (i != threadIdx.x) place_of(i, &at, &freq);
+        double r = (double)at * ((double)freq * 0.15915494309189535);   // turns
+        r -= rint(r);
+        float s, c;
+        sincospif(2.0f * (float)r, &s, &c);
         turn[i] = make_float2(c, s);
     }
     __syncthreads();
 
-    const int lane = threadIdx.x % G;
-    const int nrows = H << a.log_tokens;
-    const float inv_h = 1.0f / (float)H, inv_d = 1.0f / (float)D;
-    const size_t xstep = a.x_heads ? (size_t)L * D : D, ystep = a.y_heads ? (size_t)L * D : D;
-    // the first and second values of item i's pairs
-    auto first = [&](int i) { return !HALVES ? 2 * V * i : V * i < a.P ? V * i : V * i + a.P; };
-    auto second = [&](int i) { return !HALVES ? 2 * V * i + V : V * i < a.P ? V * i + a.P : V * i + pairs; };
-
-    for (int w = 0; w < a.n; ++w) {
-        const uint16_t* X = a.x[w];
-        uint16_t* Y = a.y[w];
-        float g[IPL][2 * V];
+    // pair e of item k: (p0, p1) -> (p0 own[0] - p1 other[1], p1 own[1] + p0 other[0]), the
+    // gammas in the sine and cosine
+    float own[IPL][V][2], other[IPL][V][2];
 #pragma unroll
-        for (int k = 0; k < IPL; ++k) {
-            const int i = lane + G * k;
+    for (int k = 0; k < IPL; ++k)
 #pragma unroll
-            for (int e = 0; e < 2 * V; ++e) g[k][e] = 1.0f;
-            if (a.norm && a.gamma[w] && V * i < pairs) {
-                nr_load<ET, V>(a.gamma[w] + first(i), g[k]);
-                nr_load<ET, V>(a.gamma[w] + second(i), g[k] + V);
+        for (int e = 0; e < V; ++e) {
+            const int p = V * (lane + G * k) + e;
+            float2 cs = make_float2(1.0f, 0.0f);
+            if (in && p < pairs) cs = turn[t * pairs + p];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const float ga = g[k][HALVES ? V * q + e : 2 * e + q];
+                own[k][e][q] = ga * cs.x;
+                other[k][e][q] = ga * cs.y;
             }
         }
-        for (int r0 = threadIdx.x / G; r0 < nrows; r0 += kNrThreads / G * kNrRows) {
-            float f[kNrRows][IPL][2 * V];
-            size_t out[kNrRows];
-            int tok[kNrRows];
+
+    for (int h = h0; h < H; h += hstep * kRows) {
+        if (h != h0) load(h);
 #pragma unroll
-            for (int u = 0; u < kNrRows; ++u) {
-                const int r = r0 + u * (kNrThreads / G);
-                // neighbouring rows of x: a head's tokens, or a token's heads
-                int t, h;
-                if (a.x_heads) {
-                    h = r >> a.log_tokens;
-                    t = r & (a.tokens - 1);
-                } else {
-                    t = nr_div(r, H, inv_h);
-                    h = r - t * H;
-                }
-                const bool in = r < nrows && t < tokens;
-                tok[u] = in ? t : -1;
-                const size_t from = in ? xplace[t] + h * xstep : 0;
-                out[u] = in ? yplace[t] + h * ystep : 0;
+        for (int u = 0; u < kRows; ++u) {
+            float f[IPL][2 * V];
 #pragma unroll
-                for (int k = 0; k < IPL; ++k) {
-                    const int i = lane + G * k;
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) f[u][k][e] = 0.0f;
-                    if (in && V * i < pairs) {
-                        nr_load<ET, V>(X + from + first(i), f[u][k]);
-                        nr_load<ET, V>(X + from + second(i), f[u][k] + V);
-                    }
-                }
+            for (int k = 0; k < IPL; ++k) {
+                nr_widen<ET, V>(raw[u][k][0], f[k]);
+                nr_widen<ET, V>(raw[u][k][1], f[k] + V);
             }
+            float rstd = 1.0f;
+            if (a.norm) {
+                float s = 0.0f;
 #pragma unroll
-            for (int u = 0; u < kNrRows; ++u) {
-                float rstd = 1.0f;
-                if (a.norm) {
-                    float s = 0.0f;
+                for (int k = 0; k < IPL; ++k)
 #pragma unroll
-                    for (int k = 0; k < IPL; ++k)
+                    for (int e = 0; e < 2 * V; ++e) s = fmaf(f[k][e], f[k][e], s);
+                rstd = rsqrtf(fmaf(nr_sum<G>(s), inv_d, a.eps));
+            }
+            if (!in || h + u * hstep >= H) continue;
+            const IDX row = to + (h + u * hstep) * ystep;
 #pragma unroll
-                        for (int e = 0; e < 2 * V; ++e) s = fmaf(f[u][k][e], f[u][k][e], s);
-                    rstd = rsqrtf(fmaf(nr_sum<G>(s), inv_d, a.eps));
+            for (int k = 0; k < IPL; ++k) {
+                const int i = lane + G * k;
+                if (V * i >= pairs) continue;
+                float* v = f[k];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float& p0 = HALVES ? v[e] : v[2 * e];
+                    float& p1 = HALVES ? v[V + e] : v[2 * e + 1];
+                    const float q0 = p0 * own[k][e][0] - p1 * other[k][e][1];
+                    const float q1 = p1 * own[k][e][1] + p0 * other[k][e][0];
+                    p0 = q0 * rstd;
+                    p1 = q1 * rstd;
                 }
-                if (tok[u] < 0) continue;
-#pragma unroll
-                for (int k = 0; k < IPL; ++k) {
-                    const int i = lane + G * k;
-                    if (V * i >= pairs) continue;
-                    float* v = f[u][k];
-                    if (a.norm) {
-#pragma unroll
-                        for (int e = 0; e < 2 * V; ++e) v[e] = v[e] * rstd * g[k][e];
-                    }
-                    const float2* tn = turn + tok[u] * pairs + V * i;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float c = tn[e].x, s = tn[e].y;
-                        float& p0 = HALVES ? v[e] : v[2 * e];
-                        float& p1 = HALVES ? v[V + e] : v[2 * e + 1];
-                        const float q0 = p0 * c - p1 * s, q1 = p1 * c + p0 * s;
-                        p0 = q0;
-                        p1 = q1;
-                    }
-                    nr_store<ET, V>(Y + out[u] + first(i), v);
-                    nr_store<ET, V>(Y + out[u] + second(i), v + V);
-                }
+                nr_store<ET, V>(Y + (IDX)(row + first(i)), v);
+                nr_store<ET, V>(Y + (IDX)(row + second(i)), v + V);
             }
         }
     }
 }
 
 template <int ET, int V, int IPL, int G>
-hipError_t launch_nr_g(const NrKernel& k, bool halves, void* stream) {
-    auto f = halves ? norm_rotate_kernel<ET, V, IPL, G, true> : norm_rotate_kernel<ET, V, IPL, G, false>;
+hipError_t launch_nr_g(NrKernel k, bool halves, void* stream) {
+    // places in 32 bits where the tensors have fewer than 2^32 bytes
+    const bool far = (long long)k.M * k.H * k.D * 2 >= (1LL << 32);
+    auto f = halves ? (far ? norm_rotate_kernel<ET, V, IPL, G, true, size_t> : norm_rotate_kernel<ET, V, IPL, G, true, uint32_t>)
+                    : (far ? norm_rotate_kernel<ET, V, IPL, G, false, size_t> : norm_rotate_kernel<ET, V, IPL, G, false, uint32_t>);
+    // Tokens of a workgroup: at most a team each (a team's heads then share its angles) and 8;
+    // more of them while teams would have no head, or while that leaves each CU four workgroups and
+    // a team fewer than four rounds of heads.  8 tokens / 4, us: 2 x 4096 tokens, 8 heads, D = 64
+    // (2 rounds / 1) 9.1 / 10.9; 17550, 16 heads, D = 128 (8 / 4) 60.8 / 58.7.
+    const int teams = (k.n > 1 ? 128 : 256) / G, rows = V == 8 ? kNrRows / 2 : kNrRows;
+    while ((1 << k.log_tokens) < kNrTokens && (1 << k.log_tokens) < teams &&
+           ((teams >> k.log_tokens) > k.H ||
+            ((1024 << (k.log_tokens + 1)) <= k.M && ((long long)k.H << k.log_tokens) < 4LL * teams * rows)))
+        ++k.log_tokens;
+    k.tokens = 1 << k.log_tokens;
     const int grid = (k.M + k.tokens - 1) / k.tokens;
     hipLaunchKernelGGL(f, dim3((unsigned)grid), dim3(kNrThreads), (size_t)k.tokens * (k.D / 2) * sizeof(float2),
                        (hipStream_t)stream, k);
@@ -221,8 +267,16 @@ template <int ET>
 hipError_t launch_nr_e(const NrKernel& k, bool halves, void* stream) {
     // Pairs whose halves do not start on 8 bytes (P not a multiple of 4) go one by one.
     if (halves && k.P % 4 != 0) return launch_nr_g<ET, 1, 2, 64>(k, halves, stream);
+    // Eight pairs a lane where both halves and their rest are whole 16-byte chunks, else four
+    // (the work for a row beside its values' own is then twice as much).
+    if (k.D % 16 == 0 && (!halves || k.P % 8 == 0)) {
+        const int items = k.D / 16;
+        if (items <= 2) return launch_nr_g<ET, 8, 1, 2>(k, halves, stream);
+        if (items <= 4) return launch_nr_g<ET, 8, 1, 4>(k, halves, stream);
+        if (items <= 8) return launch_nr_g<ET, 8, 1, 8>(k, halves, stream);
+        return launch_nr_g<ET, 8, 1, 16>(k, halves, stream);
+    }
     const int items = k.D / 8;
-    if (items <= 1) return launch_nr_g<ET, 4, 1, 1>(k, halves, stream);
     if (items <= 2) return launch_nr_g<ET, 4, 1, 2>(k, halves, stream);
     if (items <= 4) return launch_nr_g<ET, 4, 1, 4>(k, halves, stream);
     if (items <= 8) return launch_nr_g<ET, 4, 1, 8>(k, halves, stream);
@@ -259,9 +313,6 @@ hipError_t launch_norm_rotate(const NormRotateArgs& a) {
     k.norm = a.norm;
     k.eps = a.eps;
     k.M = a.B * a.L;
-    // a workgroup's tokens: as many as leave each CU four workgroups
-    while (k.log_tokens < 3 && (1024 << (k.log_tokens + 1)) <= k.M) ++k.log_tokens;
-    k.tokens = 1 << k.log_tokens;
     const bool halves = a.halves;
     return a.dtype == kF16 ? launch_nr_e<kF16>(k, halves, a.stream) : launch_nr_e<kBF16>(k, halves, a.stream);
 }
