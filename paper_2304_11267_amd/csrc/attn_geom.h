@@ -34,7 +34,9 @@ constexpr int kCus = 256;
 // kGeoPair is for widths (D = 56, 64) whose streaming ring fills a CU's LDS with
 // one 128-row workgroup, four waves: with two buffers a CU holds two.
 // kGeoNarrow is for attention over selected blocks (attn_sparse.h): 64 rows whose
-// neighbours read other keys, as 32 a wave at every D, so that each SIMD has a wave.
+// neighbours read other keys, as 32 a wave at every D, so that each SIMD has a wave; and
+// without the block of ones, so that at D = 40 a CU holds four workgroups, the 1024 of a 64x64
+// latent's 16 heads at once (16 of 64 blocks 22.9 -> 22.2 us, 4 of 64 11.2 -> 9.5).
 template <int D, int GEO = kGeoNormal>
 struct Geom {
     static constexpr int QB = D <= 64 && GEO != kGeoNarrow ? 2 : 1;
@@ -52,7 +54,7 @@ struct Geom {
     // one sparse MFMA per 32 keys instead of two dense ones (step32's O^T).
     static constexpr bool kSparse = D % 32 == 8 || D % 32 == 16;
     static constexpr int DD = kSparse ? DN - 1 : DN;          // dense d tiles
-    static constexpr bool kOnes = (D % 32 == 8 || D % 32 == 24) && !kQuarter;   // padding rows carry the row sum
+    static constexpr bool kOnes = (D % 32 == 8 || D % 32 == 24) && !kQuarter && GEO != kGeoNarrow;   // padding rows carry the row sum
     static constexpr int kTileBytes = kTK * D * 2;            // one K or V tile
     static constexpr int kChunks = kTileBytes / 1024;         // 1 KiB wave copies per tile
     static constexpr int kBufBytes = 2 * kTileBytes;          // K, V
@@ -90,7 +92,8 @@ struct Geom {
     // what would otherwise spill to scratch) at no cost in occupancy.  (The
     // streaming loop keeps 256 also for the odd waves of three workgroups a CU.)
     static constexpr int kWgPerCu = kLdsBytes <= kMaxLds ? kMaxLds / kLdsBytes : 1;
-    static constexpr int kWavesPerSimd = kWgPerCu * kWaves >= (kStream ? 5 : 8) ? 2 : 1;
+    static constexpr int kWavesPerSimd = GEO == kGeoNarrow && kWgPerCu > 2 ? (kWgPerCu > 3 ? 4 : 3)
+                                         : kWgPerCu * kWaves >= (kStream ? 5 : 8) ? 2 : 1;
 };
 
 // The geometry of a call over `heads` (batch, head) pairs.  What counts is how

@@ -28,7 +28,7 @@ template <int ET, bool AHEAD>
 __device__ __forceinline__ int bs_sums(const uint16_t* __restrict__ x, int r0, int r1, int D, int id, int size,
                                        double* part) {
     const int cols = D / 8;
-    const int groups = min(size / cols, r1 - r0);
+    const int groups = min(min(size / cols, 16), r1 - r0);   // (more of them only add up longer)
     const int g = id / cols, c = id - g * cols;
     if (g < groups) {
         double s[8];
