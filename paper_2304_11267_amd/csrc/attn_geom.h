@@ -12,6 +12,8 @@ constexpr int kGeoBig = 2;             // 256 rows, 64-key tiles (QB = 2 only)
 constexpr int kGeoQuarter = 3;         // 64 rows, keys split four ways, 64-key tiles
 constexpr int kGeoPair = 4;            // kGeoNormal without the streaming loop's third buffer
 constexpr int kGeoNarrow = 5;          // kGeoSmall with one query block a wave for every D
+constexpr int kGeoSolo = 6;            // kGeoNormal without the key split
+constexpr int kGeoNarrowSolo = 7;      // kGeoNarrow without it
 constexpr int kMaxLds = 160 * 1024;
 constexpr int kQuarterMinKeys = 512;   // shortest key sequence given to kGeoQuarter
 constexpr int kBigMinKeys = 1024;      // and to kGeoBig
@@ -37,14 +39,18 @@ constexpr int kCus = 256;
 // neighbours read other keys, as 32 a wave at every D, so that each SIMD has a wave; and
 // without the block of ones, so that at D = 40 a CU holds four workgroups, the 1024 of a 64x64
 // latent's 16 heads at once (16 of 64 blocks 22.9 -> 22.2 us, 4 of 64 11.2 -> 9.5).
+// kGeoSolo and kGeoNarrowSolo are for selected blocks and D > 64 and 80: waves that go
+// through all keys, two or three workgroups a CU where the split's LDS leaves room for one, so
+// that one's first tile and last rows have the other's products beside them.
 template <int D, int GEO = kGeoNormal>
 struct Geom {
-    static constexpr int QB = D <= 64 && GEO != kGeoNarrow ? 2 : 1;
+    static constexpr bool kNarrow = GEO == kGeoNarrow || GEO == kGeoNarrowSolo;
+    static constexpr int QB = D <= 64 && !kNarrow ? 2 : 1;
     static constexpr bool kBig = GEO == kGeoBig;
     static constexpr bool kQuarter = GEO == kGeoQuarter;
-    static constexpr int kKS = kQuarter ? 4 : 2;              // key splits
+    static constexpr int kKS = kQuarter ? 4 : GEO == kGeoSolo || GEO == kGeoNarrowSolo ? 1 : 2;   // key splits
     static constexpr int kTK = 64;                            // keys per LDS tile
-    static constexpr int kQW = kBig ? 4 : (GEO == kGeoSmall || GEO == kGeoNarrow || kQuarter ? 2 : 4) / QB;   // query waves
+    static constexpr int kQW = kBig ? 4 : (GEO == kGeoSmall || kNarrow || kQuarter ? 2 : 4) / QB;   // query waves
     static constexpr int kBQ = 32 * QB * kQW;                 // query rows per workgroup
     static constexpr int kWaves = kKS * kQW;                  // times the key splits
     static constexpr int kThreads = kWaves * 64;
@@ -54,7 +60,7 @@ struct Geom {
     // one sparse MFMA per 32 keys instead of two dense ones (step32's O^T).
     static constexpr bool kSparse = D % 32 == 8 || D % 32 == 16;
     static constexpr int DD = kSparse ? DN - 1 : DN;          // dense d tiles
-    static constexpr bool kOnes = (D % 32 == 8 || D % 32 == 24) && !kQuarter && GEO != kGeoNarrow;   // padding rows carry the row sum
+    static constexpr bool kOnes = (D % 32 == 8 || D % 32 == 24) && !kQuarter && !kNarrow;   // padding rows carry the row sum
     static constexpr int kTileBytes = kTK * D * 2;            // one K or V tile
     static constexpr int kChunks = kTileBytes / 1024;         // 1 KiB wave copies per tile
     static constexpr int kBufBytes = 2 * kTileBytes;          // K, V

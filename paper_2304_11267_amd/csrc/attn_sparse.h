@@ -17,15 +17,29 @@ namespace {
 
 // 64 queries: kGeoNarrow, four waves of 32 of them and half of the blocks (with two waves
 // of all 64 a CU has work for two of its SIMDs: 16384 tokens, 32 blocks, 8 heads, bf16, D = 64
-// 178 us, so 103); 128: kGeoNormal, or kGeoPair past one round over the CUs (attn_geom.h).
+// 178 us, so 103), for D > 80 and more than one round over the CUs kGeoNarrowSolo
+// (kGeoNarrow / kGeoNarrowSolo, us: those tokens D = 80 129 / 169, D = 128 241 / 207, D = 160 275 /
+// 258; 1024 tokens, 4 blocks, 16 heads D = 128 9.7 / 10.7); 128: kGeoNormal, or past one round over the CUs kGeoPair (D = 56, 64) or
+// kGeoSolo (D > 64).  kGeoNormal / kGeoSolo, us: 16384 tokens, 32 blocks, 8 heads, bf16 D = 80 125
+// / 112, D = 128 179 / 151, D = 160 216 / 184; 1024 tokens, 4 blocks, 8 heads D = 80 7.9 / 8.9.
 template <int ET, int D>
 hipError_t launch_sparse_d(const SparseArgs& s) {
     const AttnArgs a{s.q, s.k, s.v, s.out, nullptr, s.B, s.H, s.Lq, s.Lk, D, s.scale, s.dtype, s.stream};
     const int nw = ((s.Lk + kSparseBlock - 1) / kSparseBlock + 63) / 64;
     const BlockMask mask{(const unsigned long long*)s.mask, nw};
-    if (s.qblock == 64) return launch_kernel<ET, D, false, false, kGeoNarrow>(a, mask);
+    if (s.qblock == 64) {
+        if constexpr (D > 80) {
+            if ((long long)s.B * s.H * ((s.Lq + 63) / 64) > kCus)
+                return launch_kernel<ET, D, false, false, kGeoNarrowSolo>(a, mask);
+        }
+        return launch_kernel<ET, D, false, false, kGeoNarrow>(a, mask);
+    }
+    [[maybe_unused]] const bool rounds = (long long)s.B * s.H * ((s.Lq + 127) / 128) > kCus;   // more than one
     if constexpr (Geom<D, kGeoPair>::kFits) {
-        if ((long long)s.B * s.H * ((s.Lq + 127) / 128) > kCus) return launch_kernel<ET, D, false, false, kGeoPair>(a, mask);
+        if (rounds) return launch_kernel<ET, D, false, false, kGeoPair>(a, mask);
+    }
+    if constexpr (D > 64) {
+        if (rounds) return launch_kernel<ET, D, false, false, kGeoSolo>(a, mask);
     }
     return launch_kernel<ET, D, false, false, kGeoNormal>(a, mask);
 }

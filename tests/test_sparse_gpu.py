@@ -99,7 +99,8 @@ def test_one_token_over_half_of_the_blocks(D, Lk):
     run(2, 3, 1, Lk, D, 64, sel, dtype="bf16")
 
 
-@pytest.mark.parametrize("D,qblock", [(40, 128), (64, 64), (64, 128), (96, 64)])
+@pytest.mark.parametrize("D,qblock", [(40, 128), (64, 64), (64, 128), (96, 64)] +
+                         [(d, q) for d in WIDTHS if d > 64 for q in ((64, 128) if d > 80 else (128,)) if (d, q) != (96, 64)])
 def test_full_grid(D, qblock):
     """More query blocks than CUs (the geometry of two workgroups a CU at D = 64)."""
     run(4, 8, 1300, 640, D, qblock, "few", seed=5)
