@@ -343,12 +343,20 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// The slices of linear_kernel's ring.  With an adapter's rows in them and few channels, two: three workgroups
+// then share a CU (8 requests of 4096 rows, K = N = 320, R 16: 24.2 -> 21.4 us; past
+// kSplitMinK channels their registers leave room for two either way).
+template <bool FOLD, typename... AD>
+constexpr int linear_stages = adapters_are<AdapterFused, AD...> && !FOLD ? 2 : kStages;
+template <bool FOLD, typename... AD>
+constexpr int linear_lds = linear_stages<FOLD, AD...> * (kSliceBytes + (adapters_are<AdapterFused, AD...> ? kRankRows * kBK * 2 : 0));
 // AD: nothing, an AdapterSet (one product with batch 1), or an AdapterFused (one product,
 // a batch item for each request)
 template <int ET, bool XH, bool YH, bool FOLD, typename... AD>
 __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const AD... ad) {
     constexpr bool FUSED = adapters_are<AdapterFused, AD...>;
     constexpr int kSlot = kSliceBytes + (FUSED ? kRankRows * kBK * 2 : 0);   // of the ring
+    constexpr int ST = linear_stages<FOLD, AD...>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = lane_id();
     const int l32 = lane & 31;
@@ -414,10 +422,10 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
         for (int s = 0; s < 4; ++s) offd[s] = kSliceBytes + (l32 & 15) * kBK * 2 + ((2 * s + half) ^ swz(l32 & 15)) * 16;
     }
 
-    // slice i (channels 64i .. 64i + 63) into ring slot i % kStages
+    // slice i (channels 64i .. 64i + 63) into ring slot i % ST
     auto issue = [&](int i) __attribute__((always_inline)) {
         const int k0 = i * kBK;
-        char* st = smem + (i % kStages) * kSlot;
+        char* st = smem + (i % ST) * kSlot;
 #pragma unroll
         for (int j = 0; j < kCopies; ++j) {
             const int u0 = (wave * kCopies + j) * 64;
@@ -479,10 +487,10 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     };
     auto slice = [&](int i, auto first_c, f32x16 (&acc)[2], auto before) __attribute__((always_inline)) {
         constexpr bool FIRST = decltype(first_c)::value;
-        wait_slices<kIssued>(min(nk - 1 - i, kStages - 2));
-        lds_barrier();   // slice i is in LDS for every wave; slot (i - 1) % kStages is free
-        if (i + kStages - 1 < nk) issue(i + kStages - 1);
-        const char* st = smem + (i % kStages) * kSlot;
+        wait_slices<kIssued>(min(nk - 1 - i, ST - 2));
+        lds_barrier();   // slice i is in LDS for every wave; slot (i - 1) % ST is free
+        if (i + ST - 1 < nk) issue(i + ST - 1);
+        const char* st = smem + (i % ST) * kSlot;
         const int kval = K - i * kBK;    // channels of this slice inside K (uniform)
         // all twelve operand reads first, so their latencies overlap
         u32x4 bf[4], af[2][4];
@@ -515,7 +523,7 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     };
 
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i)
+    for (int i = 0; i < ST - 1; ++i)
         if (i < nk) issue(i);
 
     // With FOLD, acc sums a run of slices and tot the runs before it.  Past
@@ -536,10 +544,10 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
         // (a loop of its own: as slices opened by a run's first one, products with a
         // ragged last slice were slower, 8192x328x320 8.7 -> 9.1 us)
         for (int i = 0; i < nk; ++i) {
-            wait_slices<kIssued>(min(nk - 1 - i, kStages - 2));
-            lds_barrier();   // slice i is in LDS for every wave; slot (i - 1) % kStages is free
-            if (i + kStages - 1 < nk) issue(i + kStages - 1);
-            const char* st = smem + (i % kStages) * kSlot;
+            wait_slices<kIssued>(min(nk - 1 - i, ST - 2));
+            lds_barrier();   // slice i is in LDS for every wave; slot (i - 1) % ST is free
+            if (i + ST - 1 < nk) issue(i + ST - 1);
+            const char* st = smem + (i % ST) * kSlot;
             const int kval = K - i * kBK;    // channels of this slice inside K (uniform)
             // all twelve operand reads first, so their latencies overlap
             u32x4 bf[4], af[2][4];
@@ -1071,7 +1079,7 @@ long long tiles_of(const LinearArgs& a, int tm, int tn) {
 template <int ET, bool XH, bool YH, bool FOLD, typename... AD>
 hipError_t launch_t(const LinGroup& g, long long nblk, void* stream, const AD&... ad) {
     auto k = linear_kernel<ET, XH, YH, FOLD, AD...>;
-    constexpr int lds = kLdsBytes + (adapters_are<AdapterFused, AD...> ? kStages * kRankRows * kBK * 2 : 0);
+    constexpr int lds = linear_lds<FOLD, AD...>;
     static_assert(2 * lds <= 160 * 1024, "two workgroups a CU");
     static const hipError_t attr = hipFuncSetAttribute(
         reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -1211,13 +1219,13 @@ hipError_t launch_down(const LinearArgs& a, const AdapterArgs& d) {
 
 template <int ET>
 hipError_t launch_adapters_e(LinGroup& g, const LinearArgs& a, const AdapterArgs& d) {
-    // Fused, the down rows cost every tile of 64 channels a third of its time; apart, x is
-    // read once more, and a launch waits for another.  us, plain product / fused / apart: 8
-    // requests of 77 rows, K 768, N 640, R 4 4.7 / 6.0 / 9.9; 8 of 4096, 320, 320, 16 17.8 / 24.2 /
-    // 30.9; 2 of 4096, 320, 1280, 16 16.7 / 22.9 / 25.1; 4 of 1024, 1280, 1280, 16 26.2 / 35.8 /
-    // 33.4, and more requests of these shift to the last.  The choice is by a request's own sizes, so
-    // that its bits do not depend on the others of its batch.
-    if (a.L >= kAdapterRows && d.R <= kRankRows && (a.N <= kFusedMaxN || a.L <= kFusedMaxRows)) {
+    // Fused, the down rows cost every tile of 64 channels a fifth of its time (up to kSplitMinK input
+    // channels) or a third; apart, x is read once more, and a launch waits for another.  us, plain product /
+    // fused / apart: 8 requests of 77 rows, K 768, N 640, R 4 4.7 / 6.0 / 9.9; 8 of 4096, 320, 320, 16
+    // 17.8 / 21.4 / 30.9; 8 of 4096, 320, 1280, 16 60 / 73 / 72; 4 of 1024, 1280, 1280, 16 26.2 / 35.8 / 33.4.
+    // The choice is by a request's own sizes, so that its bits do not depend on the others of its batch.
+    if (a.L >= kAdapterRows && d.R <= kRankRows &&
+        (a.K <= kSplitMinK || a.N <= kFusedMaxN || a.L <= kFusedMaxRows)) {
         LinearArgs one = a;   // a batch item for each request
         one.B = 1;
         one.batch = a.B;
