@@ -33,9 +33,9 @@
 //
 // Low-rank adapters of many requests ride beside the shared product: row m of batch
 // item b adds s_i up_i (down_i x_m), i = ids[b], in one of two ways (launch_adapters_e).
-// AdapterFused, ranks up to 16 and requests of 32 rows and more (not of many rows and
+// AdapterFused, ranks up to 32 and requests of 32 rows and more (not of many rows and
 // many channels): tiles of one request
-// each, whose slices carry the 16 rows of down_i beside those of w, so that x is read
+// each, whose slices carry the 16 or 32 rows of down_i beside those of w, so that x is read
 // once and T = s_i down_i x ends in the registers that the last product, up_i T, takes.
 // AdapterSet, all others: a first launch (adapter_down_kernel) writes T, and both kernels
 // above add T up_i^T to the rows of each request.
@@ -114,7 +114,9 @@ struct AdapterSet {
     const int* ids;         // [B]: the adapter of a batch item; none outside [0, count)
     int count, R, Rp;
 };
+template <int RR>           // rows of down beside a slice's rows of w: 16 or 32, at least R
 struct AdapterFused {
+    static constexpr int kRows = RR;
     const uint16_t* down;   // [count, R, K]
     const uint16_t* up;     // [count, N, R]
     const int* ids;         // [batch items]
@@ -127,33 +129,42 @@ template <typename A>
 __device__ __forceinline__ A adapters_of(const A& a) { return a; }
 template <typename A, typename... AD>
 constexpr bool adapters_are = sizeof...(AD) == 1 && (std::is_same<A, AD>::value && ...);
+template <typename... AD>
+struct FusedRows {
+    static constexpr int value = 0;
+};
+template <int RR>
+struct FusedRows<AdapterFused<RR>> {
+    static constexpr int value = RR;
+};
+template <typename... AD>
+constexpr int fused_rows = FusedRows<AD...>::value;   // 0: no AdapterFused
 
-constexpr int kRankRows = 16;   // rows of down beside a slice's rows of w
 constexpr int kFusedMaxN = 768, kFusedMaxRows = 256;   // see launch_adapters_e
 
-// The operands of the last product of AdapterFused, Y^T += up T^T, on one MFMA of 16 ranks:
-// T^T comes as a 32x32 accumulator whose first 8 registers hold ranks 8 (r / 4) + 4 half +
-// r % 4 of token l32 (the others repeat them), so up is read in that order.
+// The operands of the last product of AdapterFused, Y^T += up T^T, on an MFMA of 16 ranks from
+// `base` on: T^T comes as a 32x32 accumulator whose registers hold ranks 8 (r / 4) + 4 half +
+// r % 4 of token l32 (with 16 rows the last 8 repeat them), so up is read in that order.
 template <int ET>
-__device__ __forceinline__ u32x4 fused_t(const float (&t)[8], float scale, int R, int half) {
+__device__ __forceinline__ u32x4 fused_t(const float* t, float scale, int base, int R, int half) {
     u32x4 v;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         float f[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int r = 2 * w + e, rank = 8 * (r >> 2) + 4 * half + (r & 3);
+            const int r = 2 * w + e, rank = base + 8 * (r >> 2) + 4 * half + (r & 3);
             f[e] = rank < R ? t[r] * scale : 0.0f;   // (rows past R repeat the last one)
         }
         v[w] = pack2<ET>(f[0], f[1]);   // rounded to the type that the matrix core multiplies
     }
     return v;
 }
-__device__ __forceinline__ u32x4 fused_up(const uint16_t* row, int R, int half) {
+__device__ __forceinline__ u32x4 fused_up(const uint16_t* row, int base, int R, int half) {
     u32x4 v = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const int r0 = 8 * q + 4 * half;
+        const int r0 = base + 8 * q + 4 * half;
         if (R % 4 == 0) {
             if (r0 < R) {
                 const u32x2 w = *(const u32x2*)(row + r0);
@@ -343,19 +354,20 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// The slices of linear_kernel's ring.  With an adapter's rows in them and few channels, two: three workgroups
-// then share a CU (8 requests of 4096 rows, K = N = 320, R 16: 24.2 -> 21.4 us; past
-// kSplitMinK channels their registers leave room for two either way).
+// The slices of linear_kernel's ring.  With an adapter's rows in them and few channels, two: three
+// workgroups then share a CU (8 requests of 4096 rows, K = N = 320, R 16: 24.2 -> 21.4 us; past
+// kSplitMinK channels their registers leave room for two either way), or two with 32 such rows.
 template <bool FOLD, typename... AD>
-constexpr int linear_stages = adapters_are<AdapterFused, AD...> && !FOLD ? 2 : kStages;
+constexpr int linear_stages = (fused_rows<AD...> > 0 && !FOLD) || fused_rows<AD...> > 16 ? 2 : kStages;
 template <bool FOLD, typename... AD>
-constexpr int linear_lds = linear_stages<FOLD, AD...> * (kSliceBytes + (adapters_are<AdapterFused, AD...> ? kRankRows * kBK * 2 : 0));
+constexpr int linear_lds = linear_stages<FOLD, AD...> * (kSliceBytes + fused_rows<AD...> * kBK * 2);
 // AD: nothing, an AdapterSet (one product with batch 1), or an AdapterFused (one product,
 // a batch item for each request)
 template <int ET, bool XH, bool YH, bool FOLD, typename... AD>
 __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const AD... ad) {
-    constexpr bool FUSED = adapters_are<AdapterFused, AD...>;
-    constexpr int kSlot = kSliceBytes + (FUSED ? kRankRows * kBK * 2 : 0);   // of the ring
+    constexpr int RR = fused_rows<AD...>;
+    constexpr bool FUSED = RR > 0;
+    constexpr int kSlot = kSliceBytes + RR * kBK * 2;   // of the ring
     constexpr int ST = linear_stages<FOLD, AD...>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = lane_id();
@@ -398,28 +410,32 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     }
     const float inv_xhw = 1.0f / (float)xhw;
 
-    // FUSED: the request's adapter (the first one's addresses where it has none), the four
-    // rows of down that this wave copies with 32 of its lanes, and its operands of up
+    // FUSED: the request's adapter (the first one's addresses where it has none), the quarter
+    // of down's rows that this wave copies with 8 lanes each, and its operands of up
     [[maybe_unused]] bool adapted = false;
     [[maybe_unused]] float t_scale = 1.0f;
     [[maybe_unused]] const uint16_t* d_row = nullptr;
     [[maybe_unused]] int d_ch = 0, offd[4];
-    [[maybe_unused]] u32x4 upf[2];
+    [[maybe_unused]] u32x4 upf[RR > 0 ? RR / 16 : 1][2];
     [[maybe_unused]] int rank = 0;
     if constexpr (FUSED) {
-        const AdapterFused a = adapters_of(ad...);
+        const auto a = adapters_of(ad...);
         const int named = __builtin_amdgcn_readfirstlane(a.ids[bi]);
         adapted = named >= 0 && named < a.count;
         const int id = adapted ? named : 0;
         rank = a.R;
         if (a.scales) t_scale = a.scales[id];
-        const int r = 4 * wave + ((lane & 31) >> 3);
+        const int r = RR / 4 * wave + (lane % (2 * RR) >> 3);
         d_ch = 8 * ((lane & 7) ^ swz(r));
         d_row = a.down + ((size_t)id * a.R + min(r, a.R - 1)) * K;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) upf[t] = fused_up(a.up + ((size_t)id * N + min(n0 + 32 * t + l32, N - 1)) * a.R, a.R, half);
+        for (int q = 0; q < RR / 16; ++q)
 #pragma unroll
-        for (int s = 0; s < 4; ++s) offd[s] = kSliceBytes + (l32 & 15) * kBK * 2 + ((2 * s + half) ^ swz(l32 & 15)) * 16;
+            for (int t = 0; t < 2; ++t)
+                upf[q][t] = fused_up(a.up + ((size_t)id * N + min(n0 + 32 * t + l32, N - 1)) * a.R, 16 * q, a.R, half);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            offd[s] = kSliceBytes + (l32 & (RR - 1)) * kBK * 2 + ((2 * s + half) ^ swz(l32 & (RR - 1))) * 16;
     }
 
     // slice i (channels 64i .. 64i + 63) into ring slot i % ST
@@ -436,9 +452,9 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
             __builtin_amdgcn_global_load_lds(src, (lds_void_t*)(st + u0 * 16), 16, 0, 0);
         }
         if constexpr (FUSED) {
-            if (lane < 32)
+            if (lane < 2 * RR)
                 __builtin_amdgcn_global_load_lds((const char*)(d_row + min(k0 + d_ch, K - 8)),
-                                                 (lds_void_t*)(st + kSliceBytes + wave * 512), 16, 0, 0);
+                                                 (lds_void_t*)(st + kSliceBytes + wave * (RR * 32)), 16, 0, 0);
         }
     };
     constexpr int kIssued = kCopies + (FUSED ? 1 : 0);   // copies of a wave and slice
@@ -593,12 +609,15 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
     // FUSED: up T^T
     if constexpr (FUSED) {
         if (adapted) {
-            float t[8];
+            float t[16];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) t[r] = FOLD ? dtot[r] + dacc[r] : dacc[r];
-            const u32x4 tf = fused_t<ET>(t, t_scale, rank, half);
+            for (int r = 0; r < 16; ++r) t[r] = FOLD ? dtot[r] + dacc[r] : dacc[r];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) more[b] = mfma32x32x16<ET>(upf[b], tf, zero);
+            for (int q = 0; q < RR / 16; ++q) {
+                const u32x4 tf = fused_t<ET>(t + 8 * q, t_scale, 16 * q, rank, half);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) more[b] = mfma32x32x16<ET>(upf[q][b], tf, more[b]);
+            }
         }
     }
 
@@ -668,7 +687,7 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinGroup grp, const A
 // faster than deeper rings (512x1280x1280: 9.1 against 9.4 us with ST = 2).
 template <int TM, int TN, int ST, typename... AD>
 struct KsGeom {
-    static constexpr int RR = adapters_are<AdapterFused, AD...> ? kRankRows : 0;   // rows of down in a slice
+    static constexpr int RR = fused_rows<AD...>;                  // rows of down in a slice
     static constexpr int kSlice = (TM + TN + RR) * kBK * 2;       // bytes
     static constexpr int kCopies = kSlice / 1024;                 // copy instructions per slice
     static constexpr int kOutRow = TN * 4 + 16;                   // bytes per row of a partial tile
@@ -695,7 +714,8 @@ __device__ __forceinline__ void ks_wait(int n) {
 
 template <int ET, bool YH, int TM, int TN, int ST, typename... AD>
 __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_kernel(const LinGroup grp, const AD... ad) {
-    constexpr bool FUSED = adapters_are<AdapterFused, AD...>;
+    constexpr int RR = fused_rows<AD...>;
+    constexpr bool FUSED = RR > 0;
     using G = KsGeom<TM, TN, ST, AD...>;
     constexpr int MB = TM / 32, NB = TN / 32, KS = kBK / 16;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -734,7 +754,7 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
     [[maybe_unused]] const uint16_t* down = nullptr;
     [[maybe_unused]] int rank = 1;
     if constexpr (FUSED) {
-        const AdapterFused a = adapters_of(ad...);
+        const auto a = adapters_of(ad...);
         const int named = __builtin_amdgcn_readfirstlane(a.ids[bi]);
         adapted = named >= 0 && named < a.count;
         id = adapted ? named : 0;
@@ -765,7 +785,7 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
         const int cpos = (2 * s + half) ^ swz(l32);
         offx[s] = (l32 * 8 + cpos) * 16;
         offw[s] = ((TM + l32) * 8 + cpos) * 16;
-        offd[s] = ((TM + TN + (l32 & 15)) * 8 + ((2 * s + half) ^ swz(l32 & 15))) * 16;
+        if constexpr (FUSED) offd[s] = ((TM + TN + (l32 & (RR - 1))) * 8 + ((2 * s + half) ^ swz(l32 & (RR - 1)))) * 16;
     }
 
     f32x16 acc[MB][NB];
@@ -879,13 +899,13 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
                                      acc[a][b][4 * g + 3]};
                     *(f32x4*)(part + (32 * a + l32) * G::kOutRow + (32 * b + 8 * g + 4 * half) * 4) = v;
                 }
-        if constexpr (FUSED) {   // T's part, [TM][16 ranks]
-            char* tp = smem + G::kT + wave * (TM * kRankRows * 4);
+        if constexpr (FUSED) {   // T's part, [TM][RR ranks]
+            char* tp = smem + G::kT + wave * (TM * RR * 4);
 #pragma unroll
             for (int a = 0; a < MB; ++a)
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
-                    *(f32x4*)(tp + (32 * a + l32) * kRankRows * 4 + (8 * q + 4 * half) * 4) =
+                for (int q = 0; q < RR / 8; ++q)
+                    *(f32x4*)(tp + (32 * a + l32) * RR * 4 + (8 * q + 4 * half) * 4) =
                         f32x4{dacc[a][4 * q], dacc[a][4 * q + 1], dacc[a][4 * q + 2], dacc[a][4 * q + 3]};
         }
     }
@@ -906,30 +926,37 @@ __global__ __launch_bounds__(256, sizeof...(AD) > 0 ? 2 : 1) void linear_ksplit_
     }
     if constexpr (FUSED) {
         // T whole, the runs in the shared tiles' order, then up T^T by a wave for each 32 x 32
-        const AdapterFused f = adapters_of(ad...);
+        const auto f = adapters_of(ad...);
         static_assert(MB * NB <= kRuns, "a block a wave");
         const bool mine = wave < MB * NB;
         const int a = wave / NB, b = wave % NB;
-        u32x4 upf = {0u, 0u, 0u, 0u};
-        if (mine) upf = fused_up(f.up + ((size_t)id * N + min(n0 + 32 * b + l32, N - 1)) * f.R, f.R, half);
+        u32x4 upf[RR / 16];
+#pragma unroll
+        for (int q = 0; q < RR / 16; ++q)
+            upf[q] = fused_up(f.up + ((size_t)id * N + min(n0 + 32 * b + l32, N - 1)) * f.R, 16 * q, f.R, half);
         __syncthreads();
         if (mine) {
-            float t[8];
+            float t[RR / 2];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) t[r] = 0.0f;
+            for (int r = 0; r < RR / 2; ++r) t[r] = 0.0f;
 #pragma unroll
             for (int w = 0; w < kRuns; ++w)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const f32x4 p = *(const f32x4*)(smem + G::kT + w * (TM * kRankRows * 4) +
-                                                    (32 * a + l32) * kRankRows * 4 + (8 * q + 4 * half) * 4);
+                for (int q = 0; q < RR / 8; ++q) {
+                    const f32x4 p = *(const f32x4*)(smem + G::kT + w * (TM * RR * 4) + (32 * a + l32) * RR * 4 +
+                                                    (8 * q + 4 * half) * 4);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) t[4 * q + e] += p[e];
                 }
             f32x16 sum;
 #pragma unroll
             for (int r = 0; r < 16; ++r) sum[r] = 0.0f;
-            if (adapted) sum = mfma32x32x16<ET>(upf, fused_t<ET>(t, f.scales ? f.scales[id] : 1.0f, f.R, half), sum);
+            if (adapted) {
+                const float scale = f.scales ? f.scales[id] : 1.0f;
+#pragma unroll
+                for (int q = 0; q < RR / 16; ++q)
+                    sum = mfma32x32x16<ET>(upf[q], fused_t<ET>(t + 8 * q, scale, 16 * q, f.R, half), sum);
+            }
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *(f32x4*)(smem + G::kMore + (32 * a + l32) * G::kOutRow + (32 * b + 8 * g + 4 * half) * 4) =
@@ -1136,7 +1163,7 @@ hipError_t launch_ksplit(LinGroup& g, const LinearArgs* a, const AD&... ad) {
     }
     if (n32 <= 256) return launch_ks<ET, YH, 32, 32, 2>(g, a, ad...);
     // (with an adapter's tile and T beside the partial tiles one 64 x 64 workgroup fills a CU)
-    if constexpr (!adapters_are<AdapterFused, AD...>) {
+    if constexpr (fused_rows<AD...> == 0) {
         if (rows > 32 && n64 >= 512) return launch_ks<ET, YH, 64, 64, 1>(g, a, ad...);
     }
     return launch_ks<ET, YH, 32, 64, 1>(g, a, ad...);
@@ -1223,8 +1250,11 @@ hipError_t launch_adapters_e(LinGroup& g, const LinearArgs& a, const AdapterArgs
     // channels) or a third; apart, x is read once more, and a launch waits for another.  us, plain product /
     // fused / apart: 8 requests of 77 rows, K 768, N 640, R 4 4.7 / 6.0 / 9.9; 8 of 4096, 320, 320, 16
     // 17.8 / 21.4 / 30.9; 8 of 4096, 320, 1280, 16 60 / 73 / 72; 4 of 1024, 1280, 1280, 16 26.2 / 35.8 / 33.4.
+    // With 17 to 32 ranks: 2 of 64, 1280, 1280, 32 4.5 / 7.0 / 12.8; 8 of 77, 768, 640, 24 4.6 / 6.9 / 11.8; 2 of
+    // 4096, 320, 320, 32 7.4 / 9.7 / 13.4; 8 of 1024, 640, 640, 32 16.3 / 22.7 / 26.3; 8 of 4096, 320, 1280, 32
+    // 62 / 82 / 80; worst where many requests' rows end early in a tile, 64 of 40, 640, 640, 32 7.6 / 19.9 / 16.0.
     // The choice is by a request's own sizes, so that its bits do not depend on the others of its batch.
-    if (a.L >= kAdapterRows && d.R <= kRankRows &&
+    if (a.L >= kAdapterRows && d.R <= 32 &&
         (a.K <= kSplitMinK || a.N <= kFusedMaxN || a.L <= kFusedMaxRows)) {
         LinearArgs one = a;   // a batch item for each request
         one.B = 1;
@@ -1233,8 +1263,11 @@ hipError_t launch_adapters_e(LinGroup& g, const LinearArgs& a, const AdapterArgs
         one.sy = (long long)a.L * a.N;
         const hipError_t e = make_group(g, &one, 1);
         if (e != hipSuccess) return e;
-        return launch_group_e<ET>(g, &one, AdapterFused{(const uint16_t*)d.down, (const uint16_t*)d.up, d.ids, d.scales,
-                                                        d.count, d.R});
+        auto with = [&](auto rows) {
+            return launch_group_e<ET>(g, &one, AdapterFused<decltype(rows)::value>{
+                (const uint16_t*)d.down, (const uint16_t*)d.up, d.ids, d.scales, d.count, d.R});
+        };
+        return d.R <= 16 ? with(std::integral_constant<int, 16>{}) : with(std::integral_constant<int, 32>{});
     }
     const hipError_t e = a.x_heads ? launch_down<ET, true>(a, d) : launch_down<ET, false>(a, d);
     if (e != hipSuccess) return e;

@@ -56,10 +56,11 @@ SHAPES = [
     (3, 7, 768, 640, 16, 2), (9, 31, 520, 72, 20, 4), (2, 32, 1288, 136, 33, 3), (4, 77, 768, 320, 64, 4),
     (2, 130, 40, 200, 128, 2), (3, 257, 320, 320, 16, 2), (2, 1100, 648, 640, 8, 3), (1, 33, 64, 96, 300, 1),
     (6, 500, 320, 960, 32, 2), (140, 3, 640, 320, 5, 7),
-    # ranks up to 16 beside the weights' slices: the split kernel's tiles and the shared ones
+    # ranks up to 32 beside the weights' slices: the split kernel's tiles and the shared ones
     (4, 77, 768, 640, 4, 5), (3, 33, 520, 72, 16, 2), (2, 64, 1288, 136, 1, 2), (1, 500, 1280, 320, 7, 1),
     (40, 32, 584, 1288, 12, 6), (9, 300, 584, 648, 10, 4), (5, 127, 8, 64, 2, 2), (2, 1000, 72, 8, 16, 3),
-    (64, 65, 56, 72, 13, 9),
+    (64, 65, 56, 72, 13, 9), (4, 77, 768, 640, 20, 5), (3, 33, 520, 72, 32, 2), (9, 300, 584, 648, 17, 4),
+    (2, 1000, 72, 8, 31, 3), (1, 500, 1280, 320, 24, 1), (2, 300, 1288, 1280, 32, 2), (2, 300, 1288, 1280, 16, 2),
 ]
 
 
@@ -95,7 +96,7 @@ def test_layouts(shape, xl, yl, dtype):
 
 
 @pytest.mark.parametrize("shape", [(6, 1, 1280, 320, 8, 2), (3, 90, 320, 320, 16, 2), (2, 600, 640, 640, 4, 2), (8, 600, 640, 640, 4, 2),
-                                   (8, 600, 640, 640, 24, 2)],
+                                   (8, 600, 640, 640, 24, 2), (8, 600, 640, 640, 40, 2)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_no_adapter_gives_the_plain_projections_bits(shape):
     """Requests without an adapter, beside ones that have it, and values of adapters that
@@ -114,7 +115,7 @@ def test_no_adapter_gives_the_plain_projections_bits(shape):
     assert torch.isfinite(y).all() and not torch.equal(y[1], plain[1])
 
 
-@pytest.mark.parametrize("L,R", [(5, 8), (40, 8), (40, 24)])
+@pytest.mark.parametrize("L,R", [(5, 8), (40, 8), (40, 24), (40, 40)])
 def test_large_values_of_one_request_stay_in_it(L, R):
     """An adapter that overflows its own request's rows leaves the neighbours in a tile alone."""
     import torch
@@ -140,14 +141,15 @@ def test_writes_its_rows_alone_and_the_workspace_it_asked_for():
     assert (buf[3 * 21 * 72:] == 7).all() and (ws[need:] == 9).all()
 
 
+@pytest.mark.parametrize("R", [16, 32, 48])
 @pytest.mark.parametrize("B,L,K,N", [(4, 40, 640, 320), (90, 40, 584, 640), (20, 200, 584, 640), (300, 1, 1280, 640),
                                      (300, 1, 320, 640)],
                          ids=lambda v: str(v))
-def test_a_requests_bits_do_not_depend_on_the_others(B, L, K, N):
+def test_a_requests_bits_do_not_depend_on_the_others(B, L, K, N, R):
     """One request alone (the split kernel past 512 channels), and among others with other
     adapters (the shared tiles where they are many)."""
     import torch
-    t = make(B, L, K, N, 16, 3, "bf16", 9)
+    t = make(B, L, K, N, R, 3, "bf16", 9)
     t["ids"] = (torch.arange(B, dtype=torch.int32, device="cuda") + 2) % 3
     y = torch.empty(B, L, N, dtype=torch.bfloat16, device="cuda")
     call(t, y)
