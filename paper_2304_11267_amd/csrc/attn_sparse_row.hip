@@ -73,6 +73,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void sparse_row_kernel(
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
 
+    bool any = false;   // block named
     for (int w0 = 0; w0 < nw; w0 += 64) {
         if (w0 > 0) __syncthreads();   // every wave is done with the last words' blocks
         if (wave == 0) {
@@ -89,6 +90,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void sparse_row_kernel(
         }
         __syncthreads();
         const int steps = named * kSteps;
+        any = any || steps > 0;
         auto first_key = [&](int s) __attribute__((always_inline)) {
             const int j = 64 * w0 + __builtin_amdgcn_readfirstlane(blocks[s / kSteps]);
             return j * kSparseBlock + s % kSteps * kKeys;
@@ -147,6 +149,8 @@ __global__ __launch_bounds__(kRowWaves * 64) void sparse_row_kernel(
                     for (int e = 0; e < 8; ++e)
                         acc[e] = fmaf(p, to_float<ET>((uint16_t)(vv[i][e >> 1] >> (16 * (e & 1)))), acc[e]);
                 }
+            } else if (__any(mine != mine)) {   // products that are no number are no weight 0
+                l = __builtin_nanf("");
             }
             __builtin_amdgcn_wave_barrier();
             if (more) load_v(key0);
@@ -182,6 +186,8 @@ __global__ __launch_bounds__(kRowWaves * 64) void sparse_row_kernel(
             o = fmaf(part[w][d], a, o);
         }
         o /= sum;
+    } else if (any) {
+        o = __builtin_nanf("");   // no product of a named block is a number, or all are minus infinity
     }
     O[(size_t)bh * D + col0 + d] = from_float<ET>(o);   // 0 where no block is named
 }

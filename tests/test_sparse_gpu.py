@@ -288,3 +288,24 @@ def test_infinite_and_missing_scores_end():
     assert int(choose(q, means, 20, 64).sum()) == 20
     means[:] = float("nan")
     assert int(choose(q, means, 20, 64).sum()) == 20
+
+
+@pytest.mark.parametrize("Lq,qblock", [(1, 64), (130, 64), (130, 128)])
+@pytest.mark.parametrize("D", [32, 64, 128, 160])
+def test_a_named_block_without_numbers_shows(D, Lq, qblock):
+    """Keys that are NaN all over one named block, or over all of them: no finite output of
+    their head, and the other head's as before."""
+    import torch
+    g = ref.generator(21)
+    q, k, v = (ref.randn(g, 1, 2, n, D, dtype="bf16") for n in (Lq, 700, 700))
+    sel = np.ones((1, 2, -(-Lq // qblock), 11), bool)
+    mask = torch.from_numpy(ref.pack(sel)).cuda()
+    clean, out = torch.empty_like(q), torch.empty_like(q)
+    sd.sparse_forward(q, k, v, mask, clean, 0.125, qblock=qblock)
+    for spoilt in (slice(128, 192), slice(640, 700), slice(None)):
+        bad = k.clone()
+        bad[:, 1, spoilt] = float("nan")
+        sd.sparse_forward(q, bad, v, mask, out, 0.125, qblock=qblock)
+        torch.cuda.synchronize()
+        assert torch.equal(out[:, 0], clean[:, 0])
+        assert not torch.isfinite(out[:, 1].float()).any(), spoilt
