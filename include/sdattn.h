@@ -180,16 +180,20 @@ int sdattn_linear(const void *x, const void *w, const void *bias, void *y, int B
  *   down   [A, R, K] of `dtype`; up [A, N, R] of `dtype`
  *   ids    [B] 32-bit integers; scales [A] fp32, or NULL (for 1)
  *   workspace: at least sdattn_linear_adapters_workspace(B, L, R) bytes, owned by
- *   the caller; it receives scales[i] * down_i x, rounded to `dtype`
+ *   the caller, for calls that may run at the same time one each; long or low-rank
+ *   requests leave it as it is, others write scales[i] * down_i x to it
+ *
+ * scales[i] * down_i x is rounded to `dtype`, all other sums are fp32, rounded once.
  *
  * The other arguments are sdattn_linear's.  Adapters of different ranks share a
  * call with the smaller ones' missing ranks as zeros in down (rows) and up
- * (columns).  An adapter's values reach the rows of its own requests alone.  Two
- * launches on `stream`.
+ * (columns).  An adapter's values reach the rows of its own requests alone.  One
+ * launch on `stream`, or two.
  *
  * Requirements: sdattn_linear's; 1 <= R <= 65536; A >= 1; down, up and workspace
  * 16-byte aligned, ids and scales 4-byte; y and the workspace must not overlap each
- * other or an input.  Fastest when R % 8 == 0.
+ * other or an input; no launch of 2^32 threads or more (SDATTN_ERR_UNSUPPORTED, here and
+ * for the calls up to sdattn_sparse_forward).  Fastest when R % 8 == 0.
  */
 long long sdattn_linear_adapters_workspace(int B, int L, int R);
 int sdattn_linear_adapters(const void *x, const void *w, const void *bias, const void *down,
@@ -255,6 +259,8 @@ int sdattn_norm_rotate(const void *q, const void *k, const void *gamma_q, const 
  *
  * sdattn_sparse_forward: out = softmax(scale q k^T) v over the keys of the named
  * blocks; zeros where none is named.  Keys and values of other blocks are not read.
+ * Weights are rounded to `dtype` before they meet v, as in sdattn_forward; with Lq = 1
+ * they stay fp32.
  *
  * Requirements: x, q, k, v, out and means 16-byte aligned, mask 8-byte; sizes >= 1,
  * L, Lq and Lk at most 2^30; 8 <= D <= 256 with D % 8 == 0 for the first two (at most

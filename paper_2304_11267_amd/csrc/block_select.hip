@@ -317,7 +317,8 @@ __global__ __launch_bounds__(1024) void select_one_kernel(const uint16_t* __rest
 }
 
 template <typename K>
-hipError_t launch_select_with(K k, const SelectArgs& a, int nq, int grid, int threads, size_t lds) {
+hipError_t launch_select_with(K k, const SelectArgs& a, int nq, long long grid, int threads, size_t lds) {
+    if (!grid_fits(grid, threads)) return hipErrorInvalidConfiguration;
     const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(k),
                                                 hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (attr != hipSuccess) return attr;
@@ -335,7 +336,7 @@ hipError_t launch_select_e(const SelectArgs& a) {
     if (heads * nq <= 512 || select_tile_lds(4, a.D, a.NB) > 160 * 1024) {
         const size_t lds = 8 * ((size_t)a.D + (a.NB > 512 ? a.NB : 512));
         auto k = a.D <= 64 ? select_one_kernel<ET, 1> : a.D <= 128 ? select_one_kernel<ET, 2> : select_one_kernel<ET, 4>;
-        return launch_select_with(k, a, nq, (int)(heads * nq), 1024, lds);
+        return launch_select_with(k, a, nq, heads * nq, 1024, lds);
     }
     // Else as many query blocks a workgroup as leave the fullest CU the fewest, of two
     // such numbers the larger.
@@ -348,7 +349,7 @@ hipError_t launch_select_e(const SelectArgs& a) {
             load = fullest;
         }
     }
-    return launch_select_with(select_tile_kernel<ET>, a, nq, (int)(heads * ((nq + best - 1) / best)), 64 * best,
+    return launch_select_with(select_tile_kernel<ET>, a, nq, heads * ((nq + best - 1) / best), 64 * best,
                               select_tile_lds(best, a.D, a.NB));
 }
 
@@ -357,7 +358,7 @@ hipError_t launch_select_e(const SelectArgs& a) {
 hipError_t launch_block_means(const BlockMeansArgs& a) {
     const int nb = (a.L + kSparseBlock - 1) / kSparseBlock;
     const long long grid = (long long)a.B * a.H * nb;
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    if (!grid_fits(grid, kBsThreads)) return hipErrorInvalidConfiguration;
     auto k = a.dtype == kF16 ? block_means_kernel<kF16> : block_means_kernel<kBF16>;
     hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(kBsThreads), 0, (hipStream_t)a.stream, (const uint16_t*)a.x,
                        a.means, a.L, a.D, nb);

@@ -20,6 +20,9 @@ struct AttnArgs {
 
 // Number of workgroups the attention kernels launch for these sizes.
 long long attn_fwd_grid(int B, int H, int Lq);
+// A launch's threads are counted in 32 bits.  (The adapters, the norms with rotation and
+// the selected blocks' launchers give hipErrorInvalidConfiguration past that, before any HIP call.)
+constexpr bool grid_fits(long long workgroups, int threads) { return workgroups * threads < (1LL << 32); }
 // Picks the kernel for (D, Lk) and launches it.
 hipError_t launch_attn_fwd(const AttnArgs& a);
 // the bf16 instantiations of the tiled kernel (a translation unit of their own)

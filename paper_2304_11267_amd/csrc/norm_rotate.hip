@@ -220,23 +220,29 @@ __global__ __launch_bounds__(kNrThreads) void norm_rotate_kernel(const NrKernel 
             }
             if (!in || h + u * hstep >= H) continue;
             const IDX row = to + (h + u * hstep) * ystep;
+            auto turned = [&](auto all) __attribute__((always_inline)) {
 #pragma unroll
-            for (int k = 0; k < IPL; ++k) {
-                const int i = lane + G * k;
-                if (V * i >= pairs) continue;
-                float* v = f[k];
+                for (int k = 0; k < IPL; ++k) {
+                    const int i = lane + G * k;
+                    if (V * i >= pairs) continue;
+                    float* v = f[k];
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float& p0 = HALVES ? v[e] : v[2 * e];
-                    float& p1 = HALVES ? v[V + e] : v[2 * e + 1];
-                    const float q0 = p0 * own[k][e][0] - p1 * other[k][e][1];
-                    const float q1 = p1 * own[k][e][1] + p0 * other[k][e][0];
-                    p0 = q0 * rstd;
-                    p1 = q1 * rstd;
+                    for (int e = 0; e < V; ++e) {
+                        float& p0 = HALVES ? v[e] : v[2 * e];
+                        float& p1 = HALVES ? v[V + e] : v[2 * e + 1];
+                        // (a value that is not turned never meets its neighbour, which may be no number)
+                        const bool turns = decltype(all)::value || V * i + e < a.P;
+                        const float q0 = turns ? p0 * own[k][e][0] - p1 * other[k][e][1] : p0 * own[k][e][0];
+                        const float q1 = turns ? p1 * own[k][e][1] + p0 * other[k][e][0] : p1 * own[k][e][1];
+                        p0 = q0 * rstd;
+                        p1 = q1 * rstd;
+                    }
+                    nr_store<ET, V>(Y + (IDX)(row + first(i)), v);
+                    nr_store<ET, V>(Y + (IDX)(row + second(i)), v + V);
                 }
-                nr_store<ET, V>(Y + (IDX)(row + first(i)), v);
-                nr_store<ET, V>(Y + (IDX)(row + second(i)), v + V);
-            }
+            };
+            if (a.P == pairs) turned(std::true_type{});
+            else turned(std::false_type{});
         }
     }
 }
@@ -258,6 +264,7 @@ hipError_t launch_nr_g(NrKernel k, bool halves, void* stream) {
         ++k.log_tokens;
     k.tokens = 1 << k.log_tokens;
     const int grid = (k.M + k.tokens - 1) / k.tokens;
+    if (!grid_fits(grid, kNrThreads)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(f, dim3((unsigned)grid), dim3(kNrThreads), (size_t)k.tokens * (k.D / 2) * sizeof(float2),
                        (hipStream_t)stream, k);
     return hipGetLastError();

@@ -76,6 +76,9 @@ int finish(hipError_t e) {
     return SDATTN_OK;
 }
 
+// of launchers that look at their grid first
+int finish_grid(hipError_t e) { return e == hipErrorInvalidConfiguration ? SDATTN_ERR_UNSUPPORTED : finish(e); }
+
 int check_attention(const void* q, const void* k, const void* v, const void* out, const float* ls,
                     int B, int H, int Lq, int Lk, int D, float scale, int dtype) {
     if (!q || !k || !v || !out) return SDATTN_ERR_INVALID_ARG;
@@ -307,7 +310,7 @@ int sdattn_linear_adapters(const void* x, const void* w, const void* bias, const
         meets(workspace, (unsigned long long)need, {{x, xb}, {w, wb}, {bias, 2ULL * N}, {y, yb}}))
         return SDATTN_ERR_INVALID_ARG;
     (void)hipGetLastError();
-    return finish(sdattn::launch_linear_adapters(args, {down, up, ids, scales, workspace, R, A}));
+    return finish_grid(sdattn::launch_linear_adapters(args, {down, up, ids, scales, workspace, R, A}));
 }
 
 int sdattn_norm_rotate(const void* q, const void* k, const void* gamma_q, const void* gamma_k,
@@ -358,7 +361,7 @@ int sdattn_norm_rotate(const void* q, const void* k, const void* gamma_q, const 
         if (meets(ko, nb, small) || overlap(ko, nb, q, nb)) return SDATTN_ERR_INVALID_ARG;
     }
     (void)hipGetLastError();
-    return finish(sdattn::launch_norm_rotate(a));
+    return finish_grid(sdattn::launch_norm_rotate(a));
 }
 
 int sdattn_block_means(const void* x, float* means, int B, int H, int L, int D, sdattn_dtype dtype,
@@ -374,7 +377,7 @@ int sdattn_block_means(const void* x, float* means, int B, int H, int L, int D, 
     if (!aligned(x, 16) || !aligned(means, 16)) return SDATTN_ERR_MISALIGNED;
     if (overlap(means, 4ULL * nm, x, 2ULL * nx)) return SDATTN_ERR_INVALID_ARG;
     (void)hipGetLastError();
-    return finish(sdattn::launch_block_means({x, means, B, H, L, D, (int)dtype, stream}));
+    return finish_grid(sdattn::launch_block_means({x, means, B, H, L, D, (int)dtype, stream}));
 }
 
 int sdattn_select_blocks(const void* q, const float* means, void* mask, int B, int H, int Lq, int NB,
@@ -391,7 +394,7 @@ int sdattn_select_blocks(const void* q, const float* means, void* mask, int B, i
     if (!aligned(q, 16) || !aligned(means, 16) || !aligned(mask, 8)) return SDATTN_ERR_MISALIGNED;
     if (meets(mask, 8ULL * nk, {{q, 2ULL * nx}, {means, 4ULL * nm}})) return SDATTN_ERR_INVALID_ARG;
     (void)hipGetLastError();
-    return finish(sdattn::launch_select_blocks({q, means, mask, B, H, Lq, NB, D, qblock, keep, (int)dtype, stream}));
+    return finish_grid(sdattn::launch_select_blocks({q, means, mask, B, H, Lq, NB, D, qblock, keep, (int)dtype, stream}));
 }
 
 int sdattn_sparse_forward(const void* q, const void* k, const void* v, const void* mask, void* out,
@@ -407,7 +410,7 @@ int sdattn_sparse_forward(const void* q, const void* k, const void* v, const voi
     if (!aligned(mask, 8)) return SDATTN_ERR_MISALIGNED;
     if (overlap(out, 2ULL * B * H * Lq * D, mask, 8ULL * nk)) return SDATTN_ERR_INVALID_ARG;
     (void)hipGetLastError();
-    return finish(sdattn::launch_attn_sparse({q, k, v, mask, out, B, H, Lq, Lk, D, qblock, scale, (int)dtype, stream}));
+    return finish_grid(sdattn::launch_attn_sparse({q, k, v, mask, out, B, H, Lq, Lk, D, qblock, scale, (int)dtype, stream}));
 }
 
 long long sdattn_attention_block_workspace(int B, int Lq, int Lk, int C) {

@@ -108,3 +108,22 @@ def test_not_a_number_stays_in_its_row():
     torch.cuda.synchronize()
     bad = torch.isnan(out).any(-1)
     assert bad[0, 1, 7] and int(bad.sum()) == 1
+
+
+@pytest.mark.parametrize("halves", [False, True], ids=["adjacent", "halves"])
+@pytest.mark.parametrize("D,P", [(64, 16), (64, 6), (40, 12), (128, 40), (128, 0)])
+def test_values_that_are_not_turned_never_meet_their_neighbours(D, P, halves):
+    import torch
+    g = ref.generator(6)
+    q = ref.randn(g, 1, 2, 9, D, dtype="bf16")
+    q[0, 1, 4, 2 * P] = float("inf")
+    q[0, 0, 2, D - 1] = float("nan")
+    q[0, 0, 5, 2 * P:] = -0.0
+    pos = torch.arange(9, device="cuda", dtype=torch.int32).view(1, 9, 1) if P else None
+    freqs = torch.ones(P, device="cuda") if P else None
+    out = torch.empty_like(q)
+    sd.norm_rotate(q, out, 2, pos=pos, freqs=freqs, pairs=(P,) if P else (), norm=sd.NORM_NONE,
+                   pairing=sd.PAIR_HALVES if halves else sd.PAIR_ADJACENT)
+    torch.cuda.synchronize()
+    assert torch.equal(out[..., 2 * P:].view(torch.int16), q[..., 2 * P:].view(torch.int16))
+    assert torch.isfinite(out[..., :2 * P].float()).all()

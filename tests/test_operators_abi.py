@@ -132,6 +132,25 @@ def test_sparse_forward(lib):
     refused(lib.sdattn_sparse_forward, good, cases, lib)
 
 
+def test_launches_of_more_threads_than_32_bits(lib):
+    far = [at(i << 42) for i in range(1, 10)]
+    names = "x w bias down up ids scales y ws".split()
+    adapters = dict(zip(names, far), wsb=1 << 40, B=4, L=70, K=520, N=640, R=20, A=3, H=1, xl=ROWS, yl=ROWS, dtype=F16)
+    refused(lib.sdattn_linear_adapters, adapters, [
+        (UNSUPPORTED, dict(B=1 << 24, L=1, K=8, N=8)), (UNSUPPORTED, dict(B=1 << 18, L=33, N=65536)),
+        (UNSUPPORTED, dict(B=1 << 18, L=65, N=65536)), (UNSUPPORTED, dict(B=1 << 20, L=16, N=65536, R=40))], lib)
+    rotate = dict(q=far[0], k=None, gq=None, gk=None, pos=None, freqs=None, qo=far[1], ko=None, B=1, H=1, L=1 << 28, D=8,
+                  axes=0, pairs=None, batches=1, norm=1, eps=f32(1e-6), pairing=0, xl=ROWS, yl=HEADS, dtype=BF16)
+    refused(lib.sdattn_norm_rotate, rotate, [(UNSUPPORTED, {})], lib)
+    means = dict(x=far[0], means=far[1], B=1 << 12, H=1 << 12, L=1, D=8, dtype=F16)
+    refused(lib.sdattn_block_means, means, [(UNSUPPORTED, {})], lib)
+    select = dict(q=far[0], means=far[1], mask=far[2], B=1 << 12, H=1 << 12, Lq=1, NB=1, D=8, qblock=64, keep=1, dtype=F16)
+    refused(lib.sdattn_select_blocks, select, [(UNSUPPORTED, {}), (UNSUPPORTED, dict(B=1 << 10, NB=16384))], lib)
+    sparse = dict(zip("q k v mask out".split(), far), B=1 << 12, H=1 << 10, Lq=1, Lk=1, D=32, qblock=64, scale=f32(0.125),
+                  dtype=F16)
+    refused(lib.sdattn_sparse_forward, sparse, [(UNSUPPORTED, {}), (UNSUPPORTED, dict(B=1 << 13, Lq=2))], lib)
+
+
 def test_python_refuses_shapes_types_and_places(lib):
     import torch
     h, f, i32, i64 = torch.float16, torch.float32, torch.int32, torch.int64
