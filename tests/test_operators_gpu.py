@@ -194,3 +194,39 @@ def test_refusals_leave_the_outputs(native, monkeypatch):
     assert e.value.status == sd.STATUS_INVALID_ARG
     torch.cuda.synchronize()
     assert (b.out == 7).all() and (o == 7).all()
+
+
+@pytest.mark.parametrize("halves", [0, 1])
+@pytest.mark.parametrize("D", [40, 128, 256])
+def test_small_arguments_at_their_smallest_alignment(D, halves):
+    """Gammas and biases on 8 bytes, positions, frequencies, adapter numbers and scales on 4:
+    the bits of the aligned call."""
+    import torch
+    g = ref.generator(31)
+
+    def moved(t, bytes_):
+        room = torch.empty(t.numel() * t.element_size() + 16, dtype=torch.uint8, device="cuda")
+        at = room[bytes_:bytes_ + t.numel() * t.element_size()].view(t.dtype).view(t.shape)
+        at.copy_(t)
+        assert at.data_ptr() % 16 == bytes_
+        return at
+
+    q = ref.randn(g, 2, 3, 50, D, dtype="bf16")
+    gamma, pos = ref.randn(g, D, dtype="bf16"), torch.randint(0, 99, (2, 50, 1), generator=g, device="cuda", dtype=torch.int32)
+    freqs = torch.rand(16, generator=g, device="cuda")
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    sd.norm_rotate(q, a, 3, gamma_q=gamma, pos=pos, freqs=freqs, pairs=(16,), pairing=halves)
+    sd.norm_rotate(q, b, 3, gamma_q=moved(gamma, 8), pos=moved(pos, 4), freqs=moved(freqs, 12), pairs=(16,), pairing=halves)
+    torch.cuda.synchronize()
+    assert torch.equal(a, b)
+    for L, R in ((40, 16), (3, 24)):
+        x, w = ref.randn(g, 2, L, D, dtype="bf16"), ref.randn(g, 64, D, dtype="bf16")
+        down, up, bias = (ref.randn(g, *s, dtype="bf16") for s in ((3, R, D), (3, 64, R), (64,)))
+        ids = torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+        scales = torch.tensor([0.5, 1.0, 2.0], device="cuda")
+        ws = torch.empty(sd.linear_adapters_workspace(2, L, R), dtype=torch.uint8, device="cuda")
+        y, z = (torch.empty(2, L, 64, dtype=x.dtype, device="cuda") for _ in range(2))
+        sd.linear_adapters(x, w, y, down, up, ids, ws, scales=scales, bias=bias)
+        sd.linear_adapters(x, w, z, down, up, moved(ids, 4), ws, scales=moved(scales, 12), bias=moved(bias, 8))
+        torch.cuda.synchronize()
+        assert torch.equal(y, z)

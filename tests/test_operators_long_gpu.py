@@ -1,0 +1,113 @@
+"""Places past 2^31 values and 2^32 bytes in one tensor: the far end of a long sequence, of a
+head and of a batch gives what the same rows give in a short call, or the 64-bit form's."""
+import numpy as np
+import pytest
+
+import operators_ref as ref
+import paper_2304_11267_amd as sd
+from parity_util import assert_close
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _needs_gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    sd.load_library()
+    yield
+    torch.cuda.empty_cache()
+
+
+def fill(*shape, seed, dtype="bf16"):
+    import torch
+    return torch.empty(shape, device="cuda", dtype=ref.t_type(dtype)).normal_(generator=ref.generator(seed))
+
+
+def same(a, b):
+    import torch
+    return torch.equal(a.contiguous().view(torch.int16), b.contiguous().view(torch.int16))
+
+
+@pytest.mark.parametrize("Lq,qblock", [(1, 64), (100, 64), (100, 128)])
+def test_selected_blocks_of_a_far_sequence(Lq, qblock):
+    import torch
+    D, Lk = 128, (1 << 24) + 100
+    nb = -(-Lk // 64)
+    q, k, v = fill(1, 1, Lq, D, seed=1), fill(1, 1, Lk, D, seed=2), fill(1, 1, Lk, D, seed=3)
+    blocks = [0, 63, 64, 4095, 4096, nb // 2, 200000, nb - 2, nb - 1]
+    words = np.zeros((1, 1, -(-Lq // qblock), -(-nb // 64)), np.int64)
+    for j in blocks:
+        words[..., j // 64] |= np.int64(np.uint64(1 << j % 64).astype(np.int64))
+    out = torch.empty_like(q)
+    sd.sparse_forward(q, k, v, torch.from_numpy(words).cuda(), out, D ** -0.5, qblock=qblock)
+    rows = torch.cat([torch.arange(64 * j, min(64 * j + 64, Lk)) for j in blocks]).cuda()
+    few = np.ones((1, 1, words.shape[2], len(blocks)), bool)
+    k, v = k[:, :, rows], v[:, :, rows]
+    r, dev = ref.sparse(ref.host(q), ref.host(k), ref.host(v), few, D ** -0.5, qblock)
+    assert_close(ref.host(out), r, dtype="bf16", what="far blocks", dev=dev)
+
+
+def test_means_and_choice_of_a_far_sequence():
+    import torch
+    D, L = 128, (1 << 24) + 70
+    x = fill(1, 1, L, D, seed=4)
+    nb = -(-L // 64)
+    means = torch.empty(1, 1, nb, D, device="cuda")
+    sd.block_means(x, means)
+    for j in (0, nb // 2, nb - 2, nb - 1):
+        want = ref.host(x[0, 0, 64 * j:64 * j + 64]).astype(np.float64).mean(0)
+        assert np.all(np.abs(ref.host(means[0, 0, j]) - want) <= 2.0 ** -24 * np.abs(want) * (1 + 2.0 ** -20) + 1e-40)
+    few = means[:, :, -300:].contiguous()
+    mask = torch.empty(1, 1, nb, 5, dtype=torch.int64, device="cuda")
+    sd.select_blocks(x, few, mask, 7)
+    tail = x[:, :, 64 * (nb - 3):].contiguous()
+    short = torch.empty(1, 1, 3, 5, dtype=torch.int64, device="cuda")
+    sd.select_blocks(tail, few, short, 7)
+    assert torch.equal(mask[:, :, -3:], short)
+
+
+@pytest.mark.parametrize("xl,yl", [(sd.LAYOUT_HEADS, sd.LAYOUT_HEADS), (sd.LAYOUT_ROWS, sd.LAYOUT_HEADS), (sd.LAYOUT_HEADS, sd.LAYOUT_ROWS)])
+def test_norms_and_rotation_of_far_tokens(xl, yl):
+    import torch
+    H, D, L = 16, 128, (1 << 20) + 9
+    q = fill(*((1, H, L, D) if xl == sd.LAYOUT_HEADS else (1, L, H * D)), seed=5)
+    out = torch.empty((1, H, L, D) if yl == sd.LAYOUT_HEADS else (1, L, H * D), device="cuda", dtype=q.dtype)
+    gamma = fill(D, seed=6)
+    pos = torch.arange(L, device="cuda", dtype=torch.int32).view(1, L, 1)
+    freqs = torch.logspace(0, -4, 48, device="cuda")
+    args = dict(gamma_q=gamma, freqs=freqs, pairs=(48,), x_layout=xl, y_layout=yl)
+    sd.norm_rotate(q, out, H, pos=pos, **args)
+    for l0 in (0, L // 2, L - 21):
+        cut = lambda t, layout: (t[:, :, l0:l0 + 21] if layout == sd.LAYOUT_HEADS else t[:, l0:l0 + 21]).contiguous()
+        qs, want = cut(q, xl), cut(out, yl)
+        got = torch.empty_like(want)
+        sd.norm_rotate(qs, got, H, pos=pos[:, l0:l0 + 21].contiguous(), **args)
+        assert same(got, want), l0
+
+
+@pytest.mark.parametrize("R", [16, 40])
+@pytest.mark.parametrize("K,N,yl", [(320, 64, sd.LAYOUT_ROWS), (64, 320, sd.LAYOUT_HEADS)])
+def test_adapters_of_far_requests(K, N, yl, R):
+    """The last of three requests, whose rows lie past 2^31 values, has the bits it has alone."""
+    import torch
+    B, L, H = 3, 2400000, 8
+    x, w = fill(B, L, K, seed=7), fill(N, K, seed=8)
+    down, up = fill(4, R, K, seed=9), fill(4, N, R, seed=10)
+    ids = torch.tensor([3, 9, 1], dtype=torch.int32, device="cuda")
+    assert B * L * max(K, N) > 1 << 31
+
+    def run(x, ids):
+        y = torch.empty((len(ids), L, N) if yl == sd.LAYOUT_ROWS else (len(ids), H, L, N // H), device="cuda", dtype=x.dtype)
+        ws = torch.empty(sd.linear_adapters_workspace(len(ids), L, R), dtype=torch.uint8, device="cuda")
+        sd.linear_adapters(x, w, y, down, up, ids, ws, heads=H, y_layout=yl)
+        return y
+
+    y = run(x, ids)
+    alone = run(x[2:].contiguous(), ids[2:].contiguous())
+    assert same(y[2:], alone)
+    rows = torch.tensor([0, 1, 127, 128, L // 2, L - 2, L - 1], device="cuda")
+    got = ref.host(alone[0, rows] if yl == sd.LAYOUT_ROWS else alone[0][:, rows].transpose(0, 1).reshape(len(rows), N))
+    r, off = ref.adapters(ref.host(x[2:, rows]), ref.host(w), None, ref.host(down), ref.host(up), np.array([1]), None, "bf16")
+    assert np.all(np.abs(got - r[0]) <= off[0] + ref.half_step(got, r[0], "bf16") * (1 + 2.0 ** -10))
