@@ -1232,9 +1232,20 @@ template <int ET, bool XH>
 hipError_t launch_down(const LinearArgs& a, const AdapterArgs& d) {
     DownKernel k{(const uint16_t*)a.x, (const uint16_t*)d.down, d.ids, d.scales, (uint16_t*)d.t,
                  a.L, a.K, a.x_heads ? a.K / a.H : 1, d.R, adapter_rank_padded(d.R), d.count, 0};
-    const int rb = d.R <= 16 ? 1 : d.R <= 32 ? 2 : 4;
-    const bool two = rb > 1 && a.L >= 32;
-    const int rows = two ? 32 : 16;
+    auto rows_of = [&](int rb) { return rb > 1 && a.L >= 32 ? 32 : 16; };
+    auto groups = [&](int rb) {
+        return (long long)a.B * ((a.L + rows_of(rb) - 1) / rows_of(rb)) * ((d.R + 16 * rb - 1) / (16 * rb));
+    };
+    // 64 ranks a workgroup read x least often; fewer while the workgroups are too few to have enough of
+    // down in flight (a T's sum is the same either way).  The whole call with 64 / 32 / 16 ranks, us: 64
+    // tokens of 64 requests, K = N = 1280, R 64 (64 / 128 / 256 workgroups) 18.3 / 15.3 / 13.9; 8 of 77, 768,
+    // 640, R 64 (24 / 48 / 160) 15.0 / 12.7 / 10.7; 4 of 1024, 1280, 1280, R 64 (128 / 256 / 1024) 43.1 / 39.6 /
+    // 43.1; 4096 rows, 640, 640, R 128 (256 / 512 / 2048) 24.5 / 25.6 / 32.2.
+    int rb = d.R <= 16 ? 1 : d.R <= 32 ? 2 : 4;
+    if (groups(1) <= 512) rb = 1;
+    else if (rb > 2 && groups(2) < 512) rb = 2;
+    const int rows = rows_of(rb);
+    const bool two = rows == 32;
     k.tiles = (a.L + rows - 1) / rows;
     const dim3 grid((unsigned)(a.B * k.tiles), (unsigned)((d.R + 16 * rb - 1) / (16 * rb)));
     auto f = rb == 1   ? adapter_down_kernel<ET, XH, 1, 1>
