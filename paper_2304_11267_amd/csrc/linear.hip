@@ -1261,9 +1261,9 @@ hipError_t launch_adapters_e(LinGroup& g, const LinearArgs& a, const AdapterArgs
     // channels) or a third; apart, x is read once more, and a launch waits for another.  us, plain product /
     // fused / apart: 8 requests of 77 rows, K 768, N 640, R 4 4.7 / 6.0 / 9.9; 8 of 4096, 320, 320, 16
     // 17.8 / 21.4 / 30.9; 8 of 4096, 320, 1280, 16 60 / 73 / 72; 4 of 1024, 1280, 1280, 16 26.2 / 35.8 / 33.4.
-    // With 17 to 32 ranks: 2 of 64, 1280, 1280, 32 4.5 / 7.0 / 12.8; 8 of 77, 768, 640, 24 4.6 / 6.9 / 11.8; 2 of
-    // 4096, 320, 320, 32 7.4 / 9.7 / 13.4; 8 of 1024, 640, 640, 32 16.3 / 22.7 / 26.3; 8 of 4096, 320, 1280, 32
-    // 62 / 82 / 80; worst where many requests' rows end early in a tile, 64 of 40, 640, 640, 32 7.6 / 19.9 / 16.0.
+    // With 17 to 32 ranks: 2 of 64, 1280, 1280, 32 4.5 / 7.0 / 9.8; 8 of 77, 768, 640, 24 4.6 / 6.9 / 10.0; 2 of
+    // 4096, 320, 320, 32 7.7 / 10.0 / 13.6; 8 of 1024, 640, 640, 32 16.7 / 22.9 / 26.9; 8 of 4096, 320, 1280, 32
+    // 60 / 79 / 81; worst where many requests' rows end early in a tile, 64 of 40, 640, 640, 32 7.6 / 19.6 / 15.5.
     // The choice is by a request's own sizes, so that its bits do not depend on the others of its batch.
     if (a.L >= kAdapterRows && d.R <= 32 &&
         (a.K <= kSplitMinK || a.N <= kFusedMaxN || a.L <= kFusedMaxRows)) {
