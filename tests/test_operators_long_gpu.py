@@ -111,3 +111,21 @@ def test_adapters_of_far_requests(K, N, yl, R):
     got = ref.host(alone[0, rows] if yl == sd.LAYOUT_ROWS else alone[0][:, rows].transpose(0, 1).reshape(len(rows), N))
     r, off = ref.adapters(ref.host(x[2:, rows]), ref.host(w), None, ref.host(down), ref.host(up), np.array([1]), None, "bf16")
     assert np.all(np.abs(got - r[0]) <= off[0] + ref.half_step(got, r[0], "bf16") * (1 + 2.0 ** -10))
+
+
+@pytest.mark.parametrize("B,L,K,N,R", [(70000, 1, 64, 72, 8), (5000, 33, 64, 72, 16), (3000, 40, 520, 64, 24)])
+def test_adapters_of_very_many_requests(B, L, K, N, R):
+    """Every request against the 64-bit form, a third of them without an adapter and with sdattn_linear's bits."""
+    import torch
+    x, w = fill(B, L, K, seed=11), fill(N, K, seed=12)
+    down, up = fill(100, R, K, seed=13), fill(100, N, R, seed=14)
+    ids = torch.randint(-50, 100, (B,), generator=ref.generator(15), device="cuda", dtype=torch.int32)
+    y, plain = (torch.empty(B, L, N, device="cuda", dtype=x.dtype) for _ in range(2))
+    ws = torch.empty(sd.linear_adapters_workspace(B, L, R), dtype=torch.uint8, device="cuda")
+    sd.linear_adapters(x, w, y, down, up, ids, ws)
+    sd.linear(x, w, plain)
+    assert same(y[ids < 0], plain[ids < 0])
+    some = torch.cat([torch.arange(50), torch.arange(B - 50, B)]).cuda()
+    got = ref.host(y[some])
+    r, off = ref.adapters(ref.host(x[some]), ref.host(w), None, ref.host(down), ref.host(up), ids[some].cpu().numpy(), None, "bf16")
+    assert np.all(np.abs(got - r) <= off + ref.half_step(got, r, "bf16") * (1 + 2.0 ** -10))
