@@ -945,7 +945,7 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
             overflow = overflow || (__float_as_uint(l_check) & 0x7f800000u) == 0x7f800000u;   // inf or NaN
         }
         // workgroup-wide OR through LDS
-        int* vote = (int*)(smem + G::kVote);
+        int* vote = (int*)(smem + G::vote_at(nh));
         const int wave_overflow = __any(overflow) ? 1 : 0;   // ballot with every lane active
         if (lane == 0) vote[wave] = wave_overflow;
         __syncthreads();

@@ -88,7 +88,13 @@ struct Geom {
     static constexpr int kMergeBytes = (kKS - 1) * kQW * kMergeFloats * 4;
     static constexpr int kTiles = kConst + kConstBytes;
     static constexpr int kUsed = kTiles > kMergeBytes ? kTiles : kMergeBytes;
-    static constexpr int kVote = kStream ? kUsed : 0;         // overflow votes: their own words, or the idle first tile
+    // Overflow votes of a pass over n tiles (the most of a key split): words of their own, or an
+    // idle buffer.  A ragged last tile is read past the last barrier (run_tiles), beside the
+    // first waves' votes: with a key split it is a later split's, without one it lies in buffer
+    // (n - 1) % 2, and the votes go into the other (64 bytes more would cost D = 80 and 160, whose
+    // buffers fill a CU to the last byte, a workgroup there).
+    static constexpr int vote_at(int n) { return kStream ? kUsed : kKS > 1 ? 0 : (n & 1) * kBufBytes; }
+    static_assert(kStream || kSlots == 2, "the votes' buffer is the other of two");
     static constexpr int kLdsBytes = kUsed + (kStream ? 64 : 0);
     static constexpr bool kFits = D >= 32 && D % 8 == 0 && kLdsBytes <= kMaxLds && (!kBig || QB == 2) &&
                                   (GEO != kGeoPair || D == 56 || D == 64);
