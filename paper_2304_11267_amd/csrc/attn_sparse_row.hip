@@ -7,7 +7,8 @@
 // with the parts of a head next to each other on one XCD, whose L2 gives K to the later
 // ones (a split of the keys would have to be joined through memory).  Nothing is staged in
 // LDS: a row of D values lies over a team of T lanes, 16 bytes each, and a wave takes 32
-// keys (16 where T = 32) at a time, K of the next ones asked for when these scores are
+// keys at a time (16 where T = 32; 64 where a lane holds a whole row of V's part, so that a load
+// of V never leaves its block), K of the next ones asked for when these scores are
 // done and V when their sums are.  A key's score is its team's sum of products (v_dot2,
 // fp32) over DPP moves; the scores pass through LDS to the lanes that hold V, whose rows lie
 // over T / N lanes.  Each wave keeps its own running maximum, sum and O in fp32 (the weights
@@ -44,12 +45,13 @@ __global__ __launch_bounds__(kRowWaves * 64) void sparse_row_kernel(
     const unsigned long long* __restrict__ Mask, uint16_t* __restrict__ O, int heads, int Lk, int D, int nblocks, int nw,
     float c) {
     constexpr int kTeams = 64 / T;                  // keys of one load of K
-    constexpr int kKeys = T == 32 ? 16 : 32;        // of a step
+    constexpr int TV = T / N;                       // lanes of a row of V
+    constexpr int kKeys = T == 32 ? 16 : TV == 1 ? 64 : 32;   // of a step: whole loads of V
     constexpr int kLoads = kKeys / kTeams;
     constexpr int kSteps = kSparseBlock / kKeys;    // of a block
-    constexpr int TV = T / N;                       // lanes of a row of V
-    constexpr int kLoadsV = kKeys * TV / 64 > 0 ? kKeys * TV / 64 : 1;
+    constexpr int kLoadsV = kKeys * TV / 64;
     static_assert(kLoads <= T, "a lane of each team for every load");
+    static_assert(kLoadsV * 64 == kKeys * TV, "a load of V ends with the step: what follows may be a block that is not named");
     __shared__ uint16_t blocks[64 * 64];            // the named blocks among 64 words'
     __shared__ int named;
     __shared__ float score[kRowWaves][kKeys];
@@ -142,8 +144,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void sparse_row_kernel(
                 for (int e = 0; e < 8; ++e) acc[e] *= alpha;
 #pragma unroll
                 for (int i = 0; i < kLoadsV; ++i) {
-                    const int at = 64 / TV * i + vkey;
-                    const float p = at < kKeys ? fast_exp2(score[wave][at] - m_new) : 0.0f;
+                    const float p = fast_exp2(score[wave][64 / TV * i + vkey] - m_new);
                     l += p;
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
