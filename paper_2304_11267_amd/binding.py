@@ -226,6 +226,13 @@ def _here(t, name):
     return p
 
 
+def _ints(**named):
+    """Raises for what does not fit a C int, which ctypes would cut to some other number."""
+    for name, n in named.items():
+        if not -1 << 31 <= n < 1 << 31:
+            raise ValueError(f"{name} is {n}, past 32 bits")
+
+
 def forward(q, k, v, out, scale: float, stream=None):
     """out = softmax(scale * q k^T) v for q/out [B,H,Lq,D], k/v [B,H,Lk,D], fp16."""
     if _native and _done("sdattn_forward", _native.forward(_fn["sdattn_forward"], q, k, v, out, scale, stream)):
@@ -500,6 +507,7 @@ def conv3x3(x, u, y, workspace, bias=None, stream=None):
 
 def linear_adapters_workspace(B, L, R):
     """Bytes of workspace sdattn_linear_adapters needs."""
+    _ints(B=B, L=L, R=R)
     return int(load_library().sdattn_linear_adapters_workspace(B, L, R))
 
 
@@ -514,6 +522,7 @@ def linear_adapters(x, w, y, down, up, ids, workspace, scales=None, bias=None, h
             stream)):
         return y
     import torch
+    _ints(heads=heads, x_layout=x_layout, y_layout=y_layout)
     if x_layout == LAYOUT_HEADS:
         B, H, L, hw = x.shape
         K = H * hw
@@ -523,6 +532,7 @@ def linear_adapters(x, w, y, down, up, ids, workspace, scales=None, bias=None, h
         B, L, K = x.shape
     N = w.shape[0]
     A, R = down.shape[:2]
+    _ints(B=B, L=L, K=K, N=N, A=A, R=R)
     _expect(w, (N, K), x, "w")
     _expect(down, (A, R, K), x, "down")
     _expect(up, (A, N, R), x, "up")
@@ -563,6 +573,7 @@ def norm_rotate(q, qo, heads, k=None, ko=None, gamma_q=None, gamma_k=None, pos=N
             x_layout, y_layout, stream)):
         return result
     import torch
+    _ints(heads=heads, norm=norm, pairing=pairing, x_layout=x_layout, y_layout=y_layout)
     if x_layout == LAYOUT_HEADS:
         B, H, L, D = q.shape
         if H != heads:
@@ -572,6 +583,7 @@ def norm_rotate(q, qo, heads, k=None, ko=None, gamma_q=None, gamma_k=None, pos=N
         if heads < 1 or C % heads:
             raise ValueError("heads must divide the channels")
         H, D = heads, C // heads
+    _ints(B=B, H=H, L=L, D=D)
     into = (B, H, L, D) if y_layout == LAYOUT_HEADS else (B, L, H * D)
     _expect(qo, into, q, "qo")
     if (k is None) != (ko is None):
@@ -583,6 +595,7 @@ def norm_rotate(q, qo, heads, k=None, ko=None, gamma_q=None, gamma_k=None, pos=N
         if t is not None:
             _expect(t, (D,), q, name)
     pairs = tuple(pairs)
+    _ints(**{f"pairs[{i}]": n for i, n in enumerate(pairs)})
     batches = 1
     if pairs:
         if pos is None or freqs is None:
@@ -617,6 +630,7 @@ def block_means(x, means, stream=None):
     if _native and _done("sdattn_block_means", _native.block_means(_fn["sdattn_block_means"], x, means, stream)):
         return means
     B, H, L, D = x.shape
+    _ints(B=B, H=H, L=L, D=D)
     _expect_means(means, (B, H, _blocks(L), D))
     status = load_library().sdattn_block_means(_here(x, "x"), _here(means, "means"), B, H, L, D, _dtype_code(x),
                                                _stream(stream))
@@ -633,6 +647,7 @@ def _expect_means(means, shape):
 
 def _expect_mask(mask, B, H, Lq, qblock, nb):
     import torch
+    _ints(qblock=qblock)
     if qblock < 1:
         raise ValueError("qblock must be 64 or 128")
     _expect(mask, (B, H, _blocks(Lq, qblock), _blocks(nb)), None, "mask")
@@ -648,8 +663,10 @@ def select_blocks(q, means, mask, keep, qblock=64, stream=None):
         return mask
     B, H, Lq, D = q.shape
     NB = means.shape[2]
+    _ints(B=B, H=H, Lq=Lq, NB=NB, D=D)
     _expect_means(means, (B, H, NB, D))
     _expect_mask(mask, B, H, Lq, qblock, NB)
+    keep = max(0, min(keep, NB))   # the same choice, or refusal, in a C int
     status = load_library().sdattn_select_blocks(_here(q, "q"), _here(means, "means"), _here(mask, "mask"), B, H, Lq, NB,
                                                  D, qblock, keep, _dtype_code(q), _stream(stream))
     _check("sdattn_select_blocks", status)
@@ -667,6 +684,7 @@ def sparse_forward(q, k, v, mask, out, scale: float, qblock=64, stream=None):
     _expect(k, (B, H, Lk, D), q, "k")
     _expect(v, (B, H, Lk, D), q, "v")
     _expect(out, q.shape, q, "out")
+    _ints(B=B, H=H, Lq=Lq, Lk=Lk, D=D)
     _expect_mask(mask, B, H, Lq, qblock, _blocks(Lk))
     status = load_library().sdattn_sparse_forward(
         _here(q, "q"), _here(k, "k"), _here(v, "v"), _here(mask, "mask"), _here(out, "out"), B, H, Lq, Lk, D, qblock,
