@@ -30,7 +30,7 @@ hipError_t launch_sparse_d(const SparseArgs& s) {
     const int nw = ((s.Lk + kSparseBlock - 1) / kSparseBlock + 63) / 64;
     const BlockMask mask{(const unsigned long long*)s.mask, nw};
     // (of the geometries with as many rows the one with the most waves: eight)
-    if (!grid_fits((long long)s.B * s.H * ((s.Lq + s.qblock - 1) / s.qblock), 512)) return hipErrorInvalidConfiguration;
+    if (!grid_fits((long long)s.B * s.H * ((s.Lq + s.qblock - 1) / s.qblock), 512)) return kGridTooLarge;
     if (s.qblock == 64) {
         if constexpr (D > 80) {
             if ((long long)s.B * s.H * ((s.Lq + 63) / 64) > kCus)

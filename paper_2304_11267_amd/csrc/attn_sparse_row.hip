@@ -197,7 +197,7 @@ template <int ET, int N>
 hipError_t launch_row_n(const SparseArgs& s) {
     const int nb = (s.Lk + kSparseBlock - 1) / kSparseBlock, nw = (nb + 63) / 64;
     const int heads = s.B * s.H;   // (check_attention has seen that these fit)
-    if (!grid_fits(((long long)heads + 7) / 8 * 8 * N, kRowWaves * 64)) return hipErrorInvalidConfiguration;
+    if (!grid_fits(((long long)heads + 7) / 8 * 8 * N, kRowWaves * 64)) return kGridTooLarge;
     auto k = s.D <= 32 ? sparse_row_kernel<ET, 4, N> : s.D <= 64 ? sparse_row_kernel<ET, 8, N>
            : s.D <= 128 ? sparse_row_kernel<ET, 16, N> : sparse_row_kernel<ET, 32, N>;
     hipLaunchKernelGGL(k, dim3((unsigned)((heads + 7) / 8 * 8 * N)), dim3(kRowWaves * 64), 0, (hipStream_t)s.stream,

@@ -318,7 +318,7 @@ __global__ __launch_bounds__(1024) void select_one_kernel(const uint16_t* __rest
 
 template <typename K>
 hipError_t launch_select_with(K k, const SelectArgs& a, int nq, long long grid, int threads, size_t lds) {
-    if (!grid_fits(grid, threads)) return hipErrorInvalidConfiguration;
+    if (!grid_fits(grid, threads)) return kGridTooLarge;
     const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(k),
                                                 hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (attr != hipSuccess) return attr;
@@ -358,7 +358,7 @@ hipError_t launch_select_e(const SelectArgs& a) {
 hipError_t launch_block_means(const BlockMeansArgs& a) {
     const int nb = (a.L + kSparseBlock - 1) / kSparseBlock;
     const long long grid = (long long)a.B * a.H * nb;
-    if (!grid_fits(grid, kBsThreads)) return hipErrorInvalidConfiguration;
+    if (!grid_fits(grid, kBsThreads)) return kGridTooLarge;
     auto k = a.dtype == kF16 ? block_means_kernel<kF16> : block_means_kernel<kBF16>;
     hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(kBsThreads), 0, (hipStream_t)a.stream, (const uint16_t*)a.x,
                        a.means, a.L, a.D, nb);

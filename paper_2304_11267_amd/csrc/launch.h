@@ -20,8 +20,10 @@ struct AttnArgs {
 
 // Number of workgroups the attention kernels launch for these sizes.
 long long attn_fwd_grid(int B, int H, int Lq);
-// A launch's threads are counted in 32 bits.  (The adapters, the norms with rotation and
-// the selected blocks' launchers give hipErrorInvalidConfiguration past that, before any HIP call.)
+// A launch's threads are counted in 32 bits.  The adapters, the norms with rotation and
+// the selected blocks' launchers give kGridTooLarge past that, before any HIP call: a value that
+// is no error of HIP's, whose own errors keep their numbers.
+constexpr hipError_t kGridTooLarge = (hipError_t)2047;
 constexpr bool grid_fits(long long workgroups, int threads) { return workgroups * threads < (1LL << 32); }
 // Picks the kernel for (D, Lk) and launches it.
 hipError_t launch_attn_fwd(const AttnArgs& a);

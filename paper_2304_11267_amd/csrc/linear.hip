@@ -1269,7 +1269,7 @@ hipError_t launch_adapters_e(LinGroup& g, const LinearArgs& a, const AdapterArgs
         (a.K <= kSplitMinK || a.N <= kFusedMaxN || a.L <= kFusedMaxRows)) {
         // tiles of launch_group_e at most
         const int rows = a.L <= 64 && a.K > kSplitMinK ? 32 : kBM;
-        if (!grid_fits(a.B * (((long long)a.L + rows - 1) / rows) * ((a.N + kBN - 1) / kBN), 256)) return hipErrorInvalidConfiguration;
+        if (!grid_fits(a.B * (((long long)a.L + rows - 1) / rows) * ((a.N + kBN - 1) / kBN), 256)) return kGridTooLarge;
         LinearArgs one = a;   // a batch item for each request
         one.B = 1;
         one.batch = a.B;
@@ -1284,7 +1284,7 @@ hipError_t launch_adapters_e(LinGroup& g, const LinearArgs& a, const AdapterArgs
         return d.R <= 16 ? with(std::integral_constant<int, 16>{}) : with(std::integral_constant<int, 32>{});
     }
     if (!grid_fits(a.B * (((long long)a.L + 15) / 16), 256) || !grid_fits(tiles_of(a, kBM, kBN), 256))
-        return hipErrorInvalidConfiguration;
+        return kGridTooLarge;
     const hipError_t e = a.x_heads ? launch_down<ET, true>(a, d) : launch_down<ET, false>(a, d);
     if (e != hipSuccess) return e;
     const AdapterSet set{(const uint16_t*)d.t, (const uint16_t*)d.up, d.ids, d.count, d.R, adapter_rank_padded(d.R)};

@@ -264,7 +264,7 @@ hipError_t launch_nr_g(NrKernel k, bool halves, void* stream) {
         ++k.log_tokens;
     k.tokens = 1 << k.log_tokens;
     const int grid = (k.M + k.tokens - 1) / k.tokens;
-    if (!grid_fits(grid, kNrThreads)) return hipErrorInvalidConfiguration;
+    if (!grid_fits(grid, kNrThreads)) return kGridTooLarge;
     hipLaunchKernelGGL(f, dim3((unsigned)grid), dim3(kNrThreads), (size_t)k.tokens * (k.D / 2) * sizeof(float2),
                        (hipStream_t)stream, k);
     return hipGetLastError();

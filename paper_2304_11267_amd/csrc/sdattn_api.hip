@@ -77,7 +77,7 @@ int finish(hipError_t e) {
 }
 
 // of launchers that look at their grid first
-int finish_grid(hipError_t e) { return e == hipErrorInvalidConfiguration ? SDATTN_ERR_UNSUPPORTED : finish(e); }
+int finish_grid(hipError_t e) { return e == sdattn::kGridTooLarge ? SDATTN_ERR_UNSUPPORTED : finish(e); }
 
 int check_attention(const void* q, const void* k, const void* v, const void* out, const float* ls,
                     int B, int H, int Lq, int Lk, int D, float scale, int dtype) {
