@@ -254,7 +254,8 @@ int sdattn_norm_rotate(const void *q, const void *k, const void *gamma_q, const 
  * sdattn_select_blocks: sets for every query block i the bits of the `keep` key
  * blocks j with the largest scores s_ij = mq_i . means_j, where mq_i is the mean of the
  * block's queries, rounded to fp32 like the keys'; of equal scores the lower j, and
- * all blocks where keep >= NB.  Sums and products are held in 64 bits.  means is what
+ * all blocks where keep >= NB.  A score that is NaN counts as larger than any number,
+ * all such scores as equal.  Sums and products are held in 64 bits.  means is what
  * sdattn_block_means gives for the keys, once for keys that stay.
  *
  * sdattn_sparse_forward: out = softmax(scale q k^T) v over the keys of the named

@@ -74,8 +74,9 @@ __global__ __launch_bounds__(kBsThreads) void block_means_kernel(const uint16_t*
     }
 }
 
-// Scores as 64-bit integers of the same order (-0 as 0).
+// Scores as 64-bit integers of the same order (-0 as 0; no number, of either sign, past all).
 __device__ __forceinline__ uint64_t bs_key(double s) {
+    if (s != s) return ~0ull;
     const uint64_t u = (uint64_t)__double_as_longlong(s + 0.0);
     return u >> 63 ? ~u : u | (1ull << 63);
 }
