@@ -79,6 +79,16 @@ __device__ __forceinline__ void nr_widen(NrRaw<V> w, float* f) {
         }
     }
 }
+// and from an address of 8 bytes' alignment (the gammas')
+template <int V>
+__device__ __forceinline__ NrRaw<V> nr_read8(const uint16_t* p) {
+    if constexpr (V == 8) {
+        const u32x2 lo = *(const u32x2*)p, hi = *(const u32x2*)(p + 4);
+        return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    } else {
+        return *(const NrRaw<V>*)p;
+    }
+}
 template <int ET, int V>
 __device__ __forceinline__ void nr_store(uint16_t* p, const float* f) {
     if constexpr (V == 1) {
@@ -166,8 +176,8 @@ __global__ __launch_bounds__(kNrThreads) void norm_rotate_kernel(const NrKernel 
 #pragma unroll
         for (int e = 0; e < 2 * V; ++e) g[k][e] = 1.0f;
         if (Gamma && V * i < pairs) {
-            nr_widen<ET, V>(*(const Raw*)(Gamma + first(i)), g[k]);
-            nr_widen<ET, V>(*(const Raw*)(Gamma + second(i)), g[k] + V);
+            nr_widen<ET, V>(nr_read8<V>(Gamma + first(i)), g[k]);
+            nr_widen<ET, V>(nr_read8<V>(Gamma + second(i)), g[k] + V);
         }
     }
 
