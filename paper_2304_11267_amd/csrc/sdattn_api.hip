@@ -661,6 +661,6 @@ const char* sdattn_status_str(int status) {
 
 int sdattn_last_hip_error(void) { return g_last_hip_error; }
 
-const char* sdattn_version(void) { return "sdattn 0.1.0 (gfx950)"; }
+const char* sdattn_version(void) { return "sdattn 0.2.0 (gfx950)"; }
 
 }  // extern "C"
