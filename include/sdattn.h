@@ -183,7 +183,8 @@ int sdattn_linear(const void *x, const void *w, const void *bias, void *y, int B
  *   the caller, for calls that may run at the same time one each; long or low-rank
  *   requests leave it as it is, others write scales[i] * down_i x to it
  *
- * scales[i] * down_i x is rounded to `dtype`, all other sums are fp32, rounded once.
+ * scales[i] * down_i x is rounded to `dtype` (in fp16 to infinity from 65520 on, where
+ * its product with up_i may well be a number), all other sums are fp32, rounded once.
  *
  * The other arguments are sdattn_linear's.  Adapters of different ranks share a
  * call with the smaller ones' missing ranks as zeros in down (rows) and up

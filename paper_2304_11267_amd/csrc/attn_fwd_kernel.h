@@ -109,9 +109,8 @@ __global__ __launch_bounds__((Geom<D, GEO>::kThreads), (Geom<D, GEO>::kWavesPerS
     // SPARSE: where a tile's rows start in the same LDS banks every 16 / kSw rows (kSw > 1),
     // their 16-byte chunks lie permuted, chunk c of row r in the place of chunk c ^ chunk_swap(r), so that
     // 16 rows' equal chunks fall into different banks.  (D = 128's rows all start
-    // in the same banks: 17550 tokens, 40 blocks for 128 queries, 16 heads, bf16 925 us
-    // without, 443 with, 401 in kGeoSolo; D = 64's every second: 16384 tokens, 32 blocks, 8 heads 91
-    // and 80.)
+    // in the same banks: 17550 tokens, 40 blocks for 128 queries, 16 heads, bf16, kGeoNormal 925 us
+    // without, 443 with; D = 64's every second: 16384 tokens, 32 blocks, 8 heads 91 and 80.)
     constexpr int kSw = SPARSE ? (D / 8) & -(D / 8) & 31 : 1;
     constexpr int kSwap = kSw > 16 ? 16 : kSw;
     auto chunk_swap = [](int row) __attribute__((always_inline)) { return kSwap > 1 ? row / (16 / kSwap) & (kSwap - 1) : 0; };

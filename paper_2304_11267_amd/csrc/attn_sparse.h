@@ -18,12 +18,15 @@ namespace {
 // 64 queries: kGeoNarrow, four waves of 32 of them and half of the blocks (16384 tokens, 32 blocks, 8
 // heads, bf16, D = 64: 103 us; two waves of all 64 leave two of a CU's SIMDs without work, 178); for D > 80
 // and more than one round over the CUs kGeoNarrowSolo (kGeoNarrow / kGeoNarrowSolo, us: those tokens
-// D = 80 129 / 169, D = 128 241 / 207, D = 160 275 / 258; 1024 tokens, 4 blocks, 16 heads D = 128 9.7 / 10.7).
-// At D = 40 (a 64x64 latent, 16 of 64 blocks 22.9 us) the vector unit is busy for 72 % of the waves' life, the
-// matrix core for 39 %: 16 exponentials, multiplies, 8 conversions and 8 sums per 32 x 32 pairs.
+// D = 80 129 / 169, D = 96 181 / 160, D = 128 236 / 195, D = 160 272 / 242; 1024 tokens, 4 blocks, 16 heads
+// D = 128 9.9 / 10.5).  At D = 40 the call costs 6 us and one for each block (a 64x64 latent, 1 / 2 / 4 / 8 / 16
+// / 32 of 64 blocks: 6.8 / 7.3 / 10.0 / 14.7 / 22.2 / 38.0 us); at 16 blocks the vector unit is busy for 72 %
+// of the waves' life, the matrix core for 39 %: 16 exponentials, multiplies, 8 conversions and 8 sums per 32 x 32
+// pairs.
 // 128 queries: kGeoNormal, or past one round over the CUs kGeoPair (D = 56, 64) or kGeoSolo (D > 64).
-// kGeoNormal / kGeoSolo, us: 16384 tokens, 32 blocks, 8 heads, bf16 D = 80 125 / 112, D = 128 179 / 151,
-// D = 160 216 / 184; 1024 tokens, 4 blocks, 8 heads D = 80 7.9 / 8.9.
+// kGeoNormal / the other, us: 16384 tokens, 32 blocks, 8 heads, bf16 D = 64 99 / 79, D = 80 112 / 100, D = 128
+// 174 / 150, D = 160 221 / 187; 17550 tokens, 40 blocks, 16 heads, D = 128 458 / 403; 1024 tokens, 4 blocks,
+// 8 heads D = 80 7.6 / 7.7.
 template <int ET, int D>
 hipError_t launch_sparse_d(const SparseArgs& s) {
     const AttnArgs a{s.q, s.k, s.v, s.out, nullptr, s.B, s.H, s.Lq, s.Lk, D, s.scale, s.dtype, s.stream};

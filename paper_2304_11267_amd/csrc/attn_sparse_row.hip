@@ -5,7 +5,9 @@
 // every CU.  A workgroup of 16 waves takes one (batch, head), or where those are fewer than
 // the CUs one half or quarter of its columns of V: all of the scores, then its part of O,
 // with the parts of a head next to each other on one XCD, whose L2 gives K to the later
-// ones (a split of the keys would have to be joined through memory).  Nothing is staged in
+// ones.  (The keys are not split over workgroups: those parts would have to be joined through
+// memory.  What that costs, and what it would give where few heads leave CUs empty, is not
+// measured.)  Nothing is staged in
 // LDS: a row of D values lies over a team of T lanes, 16 bytes each, and a wave takes 32
 // keys at a time (16 where T = 32; 64 where a lane holds a whole row of V's part, so that a load
 // of V never leaves its block), K of the next ones asked for when these scores are
@@ -13,8 +15,8 @@
 // fp32) over DPP moves; the scores pass through LDS to the lanes that hold V, whose rows lie
 // over T / N lanes.  Each wave keeps its own running maximum, sum and O in fp32 (the weights
 // too: no matrix core asks for 16 bits), and the waves are joined by the block-merge rule.
-//   8 heads of 8 sequences, 32 of 512 blocks, D = 128, bf16 (67 MB): 19.4 us (3.5 TB/s, from
-// memory in pieces of 16 KB); the tiled kernel 30.
+//   8 heads of 8 sequences, 32 of 512 blocks, D = 128, bf16 (67 MB): 16.0 us (4.2 TB/s, from
+// memory in pieces of 16 KB); the tiled kernel takes 30.4 for two queries a head.
 #include "device.h"
 #include "launch.h"
 
@@ -208,8 +210,9 @@ hipError_t launch_row_n(const SparseArgs& s) {
 
 template <int ET>
 hipError_t launch_row_e(const SparseArgs& s) {
-    // Parts of a head, whole / halves / quarters, us: 64 heads, 32 blocks, D = 128 24.4 / 20.0
-    // / 19.4; 128 heads, D = 80 24.8 / 22.5 / 33.9; 320 heads, 16 blocks, D = 128 42.4 / 44.5 / 61.8.
+    // Parts of a head, whole / halves / quarters, us: 1 head, 32 blocks, D = 128 14.9 / 12.7 / 11.4; 8 heads
+    // 15.9 / 13.3 / 12.2; 64 20.8 / 17.1 / 16.0; 128 29.3 / 26.4 / 38.3, D = 80 19.8 / 17.9 / 29.4; 320 heads,
+    // 16 blocks, D = 128 40.7 / 42.4 / 58.8.
     const long long heads = (long long)s.B * s.H;
     return heads <= 64 ? launch_row_n<ET, 4>(s) : heads <= 128 ? launch_row_n<ET, 2>(s) : launch_row_n<ET, 1>(s);
 }

@@ -8,8 +8,8 @@
 //
 // A choice between two scores is a choice between two blocks, so sums and scores are
 // held in 64 bits: the sum of 64 fp16 values is exact there, the products of two
-// fp32 means are too, and only scores that agree to 50 bits could fall otherwise than
-// the formula says.
+// fp32 means are too, and their sum is off by at most D 2^-53 sum_d |mq_i[d] mk_j[d]|: only
+// scores that are closer than twice that could fall otherwise than the formula says.
 #include "device.h"
 #include "launch.h"
 
@@ -195,8 +195,9 @@ __device__ __forceinline__ void bs_query_mean(const uint16_t* __restrict__ q, in
 // mean, the scores of 16 query blocks (zeros past the workgroup's own) and 16 key blocks at
 // a time on 16x16x4 fp64 MFMAs (lane l brings 4 consecutive values of key l % 16, a step of
 // 16 values for all lanes; on the vector unit, with sums over lanes, the products took
-// four times as long), then one block's choice.  Bound by reading q and widening it to
-// 64 bits (three instructions a value), then by the three parts' latencies.
+// four times as long), then one block's choice.  Bound by its three parts one after the
+// other: with one workgroup a CU nothing runs beside any of them (17550 queries of 16 heads, 128
+// a block, D = 128, bf16: 28.9 us, where block_means_kernel reads and widens as many values in 13.7).
 constexpr int kTileSteps = 8;   // steps of 16 values in flight
 constexpr size_t select_tile_lds(int queries, int D, int nb) {
     return (size_t)queries * 8 * ((D + 2) + (nb > 512 ? nb : 512));
@@ -340,7 +341,11 @@ hipError_t launch_select_e(const SelectArgs& a) {
         return launch_select_with(k, a, nq, heads * nq, 1024, lds);
     }
     // Else as many query blocks a workgroup as leave the fullest CU the fewest, of two
-    // such numbers the larger.
+    // such numbers the larger.  The rule's number / 4 / 5 / 8 / 9 / 12 / 16, us (bf16): 16 heads, 138 query
+    // blocks, 275 key blocks, D = 128 (9) 28.9 / 40.7 / 36.2 / 37.1 / 28.8 / 27.1 / 28.5; 16, 64, 64,
+    // D = 40 (4) 6.6 / 6.6 / 7.0 / 7.4 / 8.2 / 8.6 / 9.5; 8, 256, 256, D = 64 (8) 12.4 / 15.4 / 16.0 / 12.3 / 13.1
+    // / 12.6 / 13.2; 64, 64, 64, D = 128 (16) 20.1 / 21.5 / 25.2 / 20.3 / 26.6 / 25.7 / 20.1; 48, 64, 128,
+    // D = 64 (12) 18.2 / 18.1 / 19.2 / 17.1 / 23.5 / 24.1 / 17.3.
     int best = 4;
     long long load = 0;
     for (int n = 4; n <= 16 && select_tile_lds(n, a.D, a.NB) <= 160 * 1024; ++n) {

@@ -1238,9 +1238,11 @@ hipError_t launch_down(const LinearArgs& a, const AdapterArgs& d) {
     };
     // 64 ranks a workgroup read x least often; fewer while the workgroups are too few to have enough of
     // down in flight (a T's sum is the same either way).  The whole call with 64 / 32 / 16 ranks, us: 64
-    // tokens of 64 requests, K = N = 1280, R 64 (64 / 128 / 256 workgroups) 18.3 / 15.3 / 13.9; 8 of 77, 768,
-    // 640, R 64 (24 / 48 / 160) 15.0 / 12.7 / 10.7; 4 of 1024, 1280, 1280, R 64 (128 / 256 / 1024) 43.1 / 39.6 /
-    // 43.1; 4096 rows, 640, 640, R 128 (256 / 512 / 2048) 24.5 / 25.6 / 32.2.
+    // tokens of 64 requests, K = N = 1280, R 64 (64 / 128 / 256 workgroups) 18.1 / 15.1 / 13.5; 8 of 77, 768,
+    // 640, R 64 (24 / 48 / 160) 17.3 / 14.4 / 12.3; 16 of 77, 1280, 1280, R 64 (48 / 96 / 320) 28.6 / 24.3 / 23.4;
+    // 2 of 1024, 1280, 1280, R 64 (64 / 128 / 512) 31.8 / 28.0 / 27.0, 640, 640 19.8 / 16.9 / 16.6; 4 of 1024,
+    // 1280, 1280, R 64 (128 / 256 / 1024) 42.7 / 39.1 / 43.0; 8 of 1024, 640, 640, R 64 (256 / 512 / 2048) 31.0 /
+    // 31.5 / 37.6; 4096 rows, 640, 640, R 128 (as many) 25.7 / 26.3 / 32.8.
     int rb = d.R <= 16 ? 1 : d.R <= 32 ? 2 : 4;
     if (groups(1) <= 512) rb = 1;
     else if (rb > 2 && groups(2) < 512) rb = 2;
