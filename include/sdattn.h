@@ -230,7 +230,8 @@ int sdattn_linear_adapters(const void *x, const void *w, const void *bias, const
  */
 typedef enum {
     SDATTN_NORM_NONE = 0,
-    SDATTN_NORM_RMS = 1
+    SDATTN_NORM_RMS = 1,
+    SDATTN_NORM_LAYER = 2        /* sdattn_gated_norm only */
 } sdattn_norm;
 typedef enum {
     SDATTN_PAIR_ADJACENT = 0,
@@ -276,6 +277,127 @@ int sdattn_select_blocks(const void *q, const float *means, void *mask, int B, i
                          int D, int qblock, int keep, sdattn_dtype dtype, void *stream);
 int sdattn_sparse_forward(const void *q, const void *k, const void *v, const void *mask, void *out,
                           int B, int H, int Lq, int Lk, int D, int qblock, float scale,
+                          sdattn_dtype dtype, void *stream);
+
+/*
+ * The steps between two blocks of a transformer in one pass, over tokens x [B, L, C]
+ * (the residual stream) and the last block's output r [B, L, C]:
+ *   h = skip * x + gate * post(r)               (h = skip * x without r)
+ *   y = pre(h) * (1 + scale) + shift
+ * post and pre are one of
+ *   SDATTN_NORM_NONE    the values themselves (gamma and beta are not looked at)
+ *   SDATTN_NORM_RMS     v / sqrt(mean_c v_c^2 + eps) * gamma + beta
+ *   SDATTN_NORM_LAYER   (v - mean_c v_c) / sqrt(var_c + eps) * gamma + beta (population variance)
+ * with gamma_r alone for post, gamma and beta for pre.
+ *
+ *   x, h      [B, L, C] of `x_dtype`: `dtype`, or SDATTN_F32 for a residual stream in 32 bits; h may
+ *             be x, or NULL
+ *   r, y      [B, L, C] of `dtype` (fp16 or bf16); r may be NULL, and one of h and y
+ *   gate, scale, shift  of `dtype`, each NULL (for 1, 0, 0) or [mod_batches, groups, C] with row
+ *             (b, g) of C values at (b * groups + g) * its stride (in values): slices of one
+ *             projection's output.  Group g is tokens g L / groups .. (g + 1) L / groups - 1 (the frames of a
+ *             video); mod_batches = B, or 1 where all batch items share them
+ *   gamma_r, gamma, beta  [C] of `dtype` or NULL (for 1, 1, 0)
+ *
+ * y is computed from h before its rounding; fp32 arithmetic, each output rounded once.
+ * One launch on `stream`.  Requirements: C % 8 == 0, C <= 16384; L % groups == 0; skip finite; eps
+ * finite and >= 0; strides >= 0 and multiples of 8; every pointer 16-byte aligned; no output may overlap
+ * another argument otherwise; no launch of 2^32 threads or more (SDATTN_ERR_UNSUPPORTED,
+ * here and for the calls up to sdattn_window_forward).
+ */
+int sdattn_gated_norm(const void *x, const void *r, const void *gate, const void *scale,
+                      const void *shift, const void *gamma_r, const void *gamma, const void *beta,
+                      void *h, void *y, int B, int L, int C, int mod_batches, int groups,
+                      long long gate_stride, long long scale_stride, long long shift_stride,
+                      float skip, sdattn_norm norm_r, sdattn_norm norm, float eps,
+                      sdattn_dtype x_dtype, sdattn_dtype dtype, void *stream);
+
+/*
+ * Keys and values of the tokens so far in 8 bits, for sequences that grow: pages of
+ * SDATTN_CACHE_PAGE tokens, and for each page and key head one scale of K and one of V.
+ *   k_pages, v_pages    [pages, Hk, 64, D] bytes, e4m3 codes (4 exponent bits, 3 of mantissa, 0x7f and
+ *                       0xff no numbers); a code stands for its value times the page's scale
+ *   k_scales, v_scales  [pages, Hk] fp32, powers of two
+ *   table   [B, slots] 32-bit integers: position p of batch item b is token p % 64 of page
+ *           table[b, p / 64].  Entries outside [0, pages) are pages that are not there
+ *   starts  [B] 32-bit integers: the position of each item's first new token
+ *   counts  [B] 32-bit integers, or NULL (for L): how many new tokens each item has; what is
+ *           past L counts as L, and below 0 as 0
+ * The integers are read on the device.  Positions outside [0, 64 slots) and pages that are not
+ * there are neither read nor written.
+ *
+ * sdattn_cache_write puts tokens l < counts[b] of k and v at positions starts[b] + l, which
+ * then end their sequence: what a page had behind them is no longer part of it.  The scale is 2^e with the
+ * least e in [-100, 120] for which no value of the page is past 448 * 2^e, and never less than
+ * the scale of the tokens before starts[b] that the page keeps, which are coded anew if it grows.
+ * Codes are rounded to nearest even: a value is off by at most 2^-4 of itself, or 2^(e - 10)
+ * (once more for each time that its page is coded anew, where that takes it below 2^(e - 6)).  Finite values past 1.875 * 2^15
+ * (fp16) or 1.875 * 2^127 (bf16) are held as that; NaN and infinities come back as NaN and do not count for
+ * the scale.  A page that is written belongs to one item: two that write to the same page in one call
+ * leave it unspecified.
+ *
+ * sdattn_cache_read gives the values of positions starts[b] + l, l < counts[b], back in 16 bits
+ * (zeros for what is not there); rows of k and v from counts[b] on are left as they were.
+ *
+ *   k, v    token rows of Hk heads of D values in `layout`, `dtype` (fp16 or bf16)
+ *
+ * One launch on `stream` each.  Requirements: D % 8 == 0, D <= 256; Hk <= 65536; L and 64 slots at most
+ * 2^30; k, v and pages 16-byte aligned, the rest 4-byte; no output (pages and scales, or k and v)
+ * may overlap another argument.
+ */
+#define SDATTN_CACHE_PAGE 64
+int sdattn_cache_write(const void *k, const void *v, void *k_pages, void *v_pages, float *k_scales,
+                       float *v_scales, const int *table, const int *starts, const int *counts,
+                       int B, int Hk, int L, int D, int pages, int slots, sdattn_layout layout,
+                       sdattn_dtype dtype, void *stream);
+int sdattn_cache_read(const void *k_pages, const void *v_pages, const float *k_scales,
+                      const float *v_scales, const int *table, const int *starts, const int *counts,
+                      void *k, void *v, int B, int Hk, int L, int D, int pages, int slots,
+                      sdattn_layout layout, sdattn_dtype dtype, void *stream);
+
+/*
+ * Attention of a sequence's new tokens over what their places let them see:
+ *   out[b, h, l, :] = sum_j softmax_j(scale * q_l . k_j) v_j  over the keys j that l sees, zeros
+ *                     where it sees none;  k and v of key head h / (H / Hk)
+ * Token l < counts[b] is at position p = starts[b] + l of a sequence of n = starts[b] + counts[b] keys
+ * (at most those that there is room for).  With
+ *   hi = min(n, (floor(p / frame) + 1) * frame), or n with frame = 0;  lo = hi - window, or 0 with window = 0
+ * it sees key j where j < hi, and j >= lo or j < sinks: everything up to the end of its frame of `frame`
+ * tokens (1: up to itself; 0: the whole sequence), of that the last `window` keys (0: all) and
+ * the first `sinks`.  Keys that it does not see have no influence, whatever their values.
+ *
+ *   q, out  token rows of H heads of D values in `x_layout` and `y_layout`, [B, Lq tokens]; rows from
+ *           counts[b] on are left as they were
+ *   workspace: at least the bytes that the _workspace function gives for the same sizes (often 0: then it
+ *   may be NULL), owned by the caller, for calls that may run at the same time one each; it holds the parts
+ *   of keys that are split over workgroups
+ *
+ * sdattn_cache_forward reads keys and values from the pages of sdattn_cache_write, codes times scales
+ * (starts and counts those of that call, for the new tokens to see themselves); keys
+ * without a page are not seen.  `dtype` is the one that wrote them.
+ * sdattn_window_forward reads k, v: token rows of Hk heads and Lk tokens in `x_layout`, `dtype`;
+ * starts may be NULL (for Lk - Lq: the queries are the last tokens), and so may counts (for Lq).
+ *
+ * Weights are rounded to `dtype` before they meet v, as in sdattn_forward.  One launch on `stream`, or two.
+ * Requirements: 32 <= D <= 160 with D % 8 == 0; Hk divides H, H <= 65536; Lq, Lk, 64 slots and Lq H / Hk at
+ * most 2^30; frame, window, sinks >= 0; finite scale; q, k, v, pages, out and workspace 16-byte
+ * aligned, the rest 4-byte; out and the workspace must not overlap each other or an input.
+ */
+long long sdattn_cache_forward_workspace(int B, int H, int Hk, int Lq, int D, int slots, int frame,
+                                         int window, int sinks);
+int sdattn_cache_forward(const void *q, const void *k_pages, const void *v_pages,
+                         const float *k_scales, const float *v_scales, const int *table,
+                         const int *starts, const int *counts, void *out, void *workspace,
+                         long long workspace_bytes, int B, int H, int Hk, int Lq, int D, int pages,
+                         int slots, int frame, int window, int sinks, float scale,
+                         sdattn_layout x_layout, sdattn_layout y_layout, sdattn_dtype dtype,
+                         void *stream);
+long long sdattn_window_forward_workspace(int B, int H, int Hk, int Lq, int Lk, int D, int frame,
+                                          int window, int sinks);
+int sdattn_window_forward(const void *q, const void *k, const void *v, const int *starts,
+                          const int *counts, void *out, void *workspace, long long workspace_bytes,
+                          int B, int H, int Hk, int Lq, int Lk, int D, int frame, int window,
+                          int sinks, float scale, sdattn_layout x_layout, sdattn_layout y_layout,
                           sdattn_dtype dtype, void *stream);
 
 /*

@@ -7,10 +7,11 @@ arithmetic of the attention happens here.  The library is loaded from the
 package directory on first use; a missing library raises, there is no other
 code path.
 
-Fifteen functions are marshalled by the extension module _marshal (csrc/marshal.cpp):
+Twenty functions are marshalled by the extension module _marshal (csrc/marshal.cpp):
 forward, forward_ex, softmax_rows, logits, softmax_pv, attention_block,
 attention_block_kv, group_norm, geglu, conv3x3, linear_adapters, norm_rotate,
-block_means, select_blocks and sparse_forward, in 3 us a call where Python
+block_means, select_blocks, sparse_forward, gated_norm, cache_write, cache_read,
+cache_forward and window_forward, in 3 us a call where Python
 and ctypes take 10, as long as two of the smaller kernels.  linear,
 attention_block_static, project_kv and winograd_weights go through ctypes below,
 as does what the module does not take (it answers None); errors are raised there.
@@ -44,6 +45,9 @@ EXPORTS = ("sdattn_forward", "sdattn_forward_ex", "sdattn_softmax_rows", "sdattn
            "sdattn_winograd_weights", "sdattn_conv3x3_workspace", "sdattn_conv3x3",
            "sdattn_linear_adapters_workspace", "sdattn_linear_adapters", "sdattn_norm_rotate",
            "sdattn_block_means", "sdattn_select_blocks", "sdattn_sparse_forward",
+           "sdattn_gated_norm", "sdattn_cache_write", "sdattn_cache_read",
+           "sdattn_cache_forward_workspace", "sdattn_cache_forward",
+           "sdattn_window_forward_workspace", "sdattn_window_forward",
            "sdattn_status_str", "sdattn_last_hip_error", "sdattn_version")
 
 LAYOUT_ROWS = 0
@@ -51,9 +55,11 @@ LAYOUT_HEADS = 1
 
 NORM_NONE = 0
 NORM_RMS = 1
+NORM_LAYER = 2
 PAIR_ADJACENT = 0
 PAIR_HALVES = 1
 SPARSE_BLOCK = 64
+CACHE_PAGE = 64
 
 _lib = None
 _native = None   # the extension module; None: not loaded (or not built)
@@ -131,6 +137,20 @@ def load_library():
     lib.sdattn_select_blocks.restype = i32
     lib.sdattn_sparse_forward.argtypes = [vp] * 5 + [i32] * 6 + [f32, i32, vp]
     lib.sdattn_sparse_forward.restype = i32
+    lib.sdattn_gated_norm.argtypes = [vp] * 10 + [i32] * 5 + [i64] * 3 + [f32, i32, i32, f32, i32, i32, vp]
+    lib.sdattn_gated_norm.restype = i32
+    lib.sdattn_cache_write.argtypes = [vp] * 9 + [i32] * 8 + [vp]
+    lib.sdattn_cache_write.restype = i32
+    lib.sdattn_cache_read.argtypes = [vp] * 9 + [i32] * 8 + [vp]
+    lib.sdattn_cache_read.restype = i32
+    lib.sdattn_cache_forward_workspace.argtypes = [i32] * 9
+    lib.sdattn_cache_forward_workspace.restype = i64
+    lib.sdattn_cache_forward.argtypes = [vp] * 10 + [i64] + [i32] * 10 + [f32, i32, i32, i32, vp]
+    lib.sdattn_cache_forward.restype = i32
+    lib.sdattn_window_forward_workspace.argtypes = [i32] * 9
+    lib.sdattn_window_forward_workspace.restype = i64
+    lib.sdattn_window_forward.argtypes = [vp] * 7 + [i64] + [i32] * 9 + [f32, i32, i32, i32, vp]
+    lib.sdattn_window_forward.restype = i32
     lib.sdattn_status_str.argtypes = [i32]
     lib.sdattn_status_str.restype = ctypes.c_char_p
     lib.sdattn_last_hip_error.argtypes = []
@@ -690,4 +710,229 @@ def sparse_forward(q, k, v, mask, out, scale: float, qblock=64, stream=None):
         _here(q, "q"), _here(k, "k"), _here(v, "v"), _here(mask, "mask"), _here(out, "out"), B, H, Lq, Lk, D, qblock,
         ctypes.c_float(scale), _dtype_code(q), _stream(stream))
     _check("sdattn_sparse_forward", status)
+    return out
+
+
+def _maybe(t, name):
+    return _here(t, name) if t is not None else None
+
+
+def _expect_type(t, dtype, name):
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+
+
+def _row_stride(t, name, shape, like):
+    """Row stride of a modulation tensor [batches, groups, C], a slice of a wider one perhaps."""
+    if t is None:
+        return 0
+    _expect(t, shape, like, name)
+    rows, stride = shape[0] * shape[1], 0
+    if rows > 1:
+        stride = t.stride(1) if shape[1] > 1 else t.stride(0)
+        if shape[0] > 1 and shape[1] > 1 and t.stride(0) != shape[1] * stride:
+            raise ValueError(f"{name}'s rows must be evenly spaced")
+    if shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}'s channels must lie side by side")
+    return stride
+
+
+def _strided(t, name):
+    """_maybe for a tensor whose strides the call takes."""
+    import torch
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def gated_norm(x, y=None, r=None, h=None, gate=None, scale=None, shift=None, gamma_r=None, gamma=None, beta=None,
+               skip=1.0, norm_r=NORM_NONE, norm=NORM_LAYER, eps=1e-6, stream=None):
+    """h = skip * x + gate * norm_r(r), y = norm(h) * (1 + scale) + shift over tokens [B, L, C]; x and h
+    of r's (y's) type or float32, h may be x; gate, scale, shift [B or 1, groups, C] (rows evenly
+    spaced) or None; gammas and beta [C] or None.  Returns (h, y)."""
+    if _native and _done("sdattn_gated_norm", _native.gated_norm(
+            _fn["sdattn_gated_norm"], x, y, r, h, gate, scale, shift, gamma_r, gamma, beta, skip, norm_r, norm, eps, stream)):
+        return h, y
+    import torch
+    B, L, C = x.shape
+    _ints(B=B, L=L, C=C, norm_r=norm_r, norm=norm)
+    if y is None and h is None:
+        raise ValueError("neither y nor h is given")
+    like = next((t for t in (y, r, gate, scale, shift, gamma_r, gamma, beta) if t is not None), x)
+    if x.dtype != torch.float32:
+        _expect_type(x, like.dtype, "x")
+    for t, name in ((y, "y"), (r, "r")):
+        if t is not None:
+            _expect(t, x.shape, like, name)
+    if h is not None:
+        _expect(h, x.shape, x, "h")
+    mods = [t for t in (gate, scale, shift) if t is not None]
+    batches, groups = (mods[0].shape[0], mods[0].shape[1]) if mods else (1, 1)
+    if batches != 1:
+        batches = B
+    _ints(groups=groups)
+    sg, ss, st = (_row_stride(t, name, (batches, groups, C), like)
+                  for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")))
+    for t, name in ((gamma_r, "gamma_r"), (gamma, "gamma"), (beta, "beta")):
+        if t is not None:
+            _expect(t, (C,), like, name)
+    status = load_library().sdattn_gated_norm(
+        _here(x, "x"), _maybe(r, "r"), _strided(gate, "gate"), _strided(scale, "scale"), _strided(shift, "shift"),
+        _maybe(gamma_r, "gamma_r"), _maybe(gamma, "gamma"),
+        _maybe(beta, "beta"), _maybe(h, "h"), _maybe(y, "y"), B, L, C, batches, groups, sg, ss, st, ctypes.c_float(skip),
+        norm_r, norm, ctypes.c_float(eps), _dtype_code(x), _dtype_code(like), _stream(stream))
+    _check("sdattn_gated_norm", status)
+    return h, y
+
+
+def _expect_cache(k_pages, v_pages, k_scales, v_scales, table, starts, counts, B, Hk, D):
+    """Shapes and types of the cache's tensors; returns (pages, slots)."""
+    import torch
+    P = k_pages.shape[0]
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        _expect(t, (P, Hk, CACHE_PAGE, D), None, name)
+        if t.dtype not in (torch.uint8, torch.float8_e4m3fn):
+            raise TypeError(f"{name} is {t.dtype}, expected torch.uint8 or torch.float8_e4m3fn")
+    for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+        _expect(t, (P, Hk), None, name)
+        _expect_type(t, torch.float32, name)
+    slots = table.shape[-1]
+    _expect(table, (B, slots), None, "table")
+    for t, name in ((starts, "starts"), (counts, "counts")):
+        if t is not None:
+            _expect(t, (B,), None, name)
+    for t, name in ((table, "table"), (starts, "starts"), (counts, "counts")):
+        if t is not None:
+            _expect_type(t, torch.int32, name)
+    _ints(pages=P, slots=slots)
+    return P, slots
+
+
+def _rows_of(t, layout, heads, name):
+    """(B, L, D) of token rows [B, L, heads * D] or [B, heads, L, D]."""
+    if layout == LAYOUT_HEADS:
+        B, H, L, D = t.shape
+        if H != heads:
+            raise ValueError(f"{name}'s head count differs from heads")
+        return B, L, D
+    B, L, C = t.shape
+    if heads < 1 or C % heads:
+        raise ValueError("heads must divide the channels")
+    return B, L, C // heads
+
+
+def _rows_shape(layout, B, H, L, D):
+    return (B, H, L, D) if layout == LAYOUT_HEADS else (B, L, H * D)
+
+
+def _cache_call(name, order, k, v, k_pages, v_pages, k_scales, v_scales, table, starts, counts, layout, stream):
+    Hk = k_pages.shape[1]
+    _ints(layout=layout, Hk=Hk)
+    B, L, D = _rows_of(k, layout, Hk, "k")
+    _ints(B=B, L=L, D=D)
+    _expect(v, k.shape, k, "v")
+    P, slots = _expect_cache(k_pages, v_pages, k_scales, v_scales, table, starts, counts, B, Hk, D)
+    at = dict(k=_here(k, "k"), v=_here(v, "v"), k_pages=_here(k_pages, "k_pages"), v_pages=_here(v_pages, "v_pages"),
+              k_scales=_here(k_scales, "k_scales"), v_scales=_here(v_scales, "v_scales"), table=_here(table, "table"),
+              starts=_here(starts, "starts"), counts=_maybe(counts, "counts"))
+    status = getattr(load_library(), name)(*(at[n] for n in order), B, Hk, L, D, P, slots, layout, _dtype_code(k),
+                                           _stream(stream))
+    _check(name, status)
+
+
+def cache_write(k, v, k_pages, v_pages, k_scales, v_scales, table, starts, counts=None, layout=LAYOUT_HEADS, stream=None):
+    """Quantises tokens l < counts[b] of k and v ([B, Hk, L, D], or [B, L, Hk*D] in rows layout) to 8 bits at
+    positions starts[b] + l: pages uint8 or float8_e4m3fn [P, Hk, 64, D], scales fp32 [P, Hk], table int32
+    [B, slots] of each position's page, starts and counts int32 [B] (counts None: all L)."""
+    if _native and _done("sdattn_cache_write", _native.cache_write(
+            _fn["sdattn_cache_write"], k, v, k_pages, v_pages, k_scales, v_scales, table, starts, counts, layout, stream)):
+        return
+    _cache_call("sdattn_cache_write", ("k", "v", "k_pages", "v_pages", "k_scales", "v_scales", "table", "starts", "counts"),
+                k, v, k_pages, v_pages, k_scales, v_scales, table, starts, counts, layout, stream)
+
+
+def cache_read(k, v, k_pages, v_pages, k_scales, v_scales, table, starts, counts=None, layout=LAYOUT_HEADS, stream=None):
+    """The values of positions starts[b] + l, l < counts[b], of cache_write's pages into k and v (zeros
+    where there is no page); the rows behind them stay as they are.  Returns (k, v)."""
+    if _native and _done("sdattn_cache_read", _native.cache_read(
+            _fn["sdattn_cache_read"], k, v, k_pages, v_pages, k_scales, v_scales, table, starts, counts, layout, stream)):
+        return k, v
+    _cache_call("sdattn_cache_read", ("k_pages", "v_pages", "k_scales", "v_scales", "table", "starts", "counts", "k", "v"),
+                k, v, k_pages, v_pages, k_scales, v_scales, table, starts, counts, layout, stream)
+    return k, v
+
+
+def cache_forward_workspace(B, H, Hk, Lq, D, slots, frame=1, window=0, sinks=0):
+    """Bytes of workspace sdattn_cache_forward needs (0: none); -1 for sizes that it refuses."""
+    _ints(B=B, H=H, Hk=Hk, Lq=Lq, D=D, slots=slots, frame=frame, window=window, sinks=sinks)
+    return int(load_library().sdattn_cache_forward_workspace(B, H, Hk, Lq, D, slots, frame, window, sinks))
+
+
+def _workspace(t):
+    return (None, 0) if t is None or t.numel() == 0 else (_here(t, "workspace"), t.numel() * t.element_size())
+
+
+def cache_forward(q, k_pages, v_pages, k_scales, v_scales, table, starts, out, scale: float, heads, workspace=None,
+                  counts=None, frame=1, window=0, sinks=0, x_layout=LAYOUT_HEADS, y_layout=LAYOUT_HEADS, stream=None):
+    """out = softmax(scale * q k^T) v of tokens l < counts[b] of q, at positions starts[b] + l, over the
+    cache's keys up to the end of each one's frame of `frame` tokens (1: itself; 0: the whole sequence), of
+    these the last `window` (0: all) and the first `sinks`.  q, out [B, H, Lq, D], or [B, Lq, H*D] in rows
+    layout; workspace of cache_forward_workspace(...) bytes (None where that is 0)."""
+    if _native and _done("sdattn_cache_forward", _native.cache_forward(
+            _fn["sdattn_cache_forward"], q, k_pages, v_pages, k_scales, v_scales, table, starts, out, scale, heads, workspace,
+            counts, frame, window, sinks, x_layout, y_layout, stream)):
+        return out
+    _ints(heads=heads, x_layout=x_layout, y_layout=y_layout, frame=frame, window=window, sinks=sinks)
+    B, Lq, D = _rows_of(q, x_layout, heads, "q")
+    Hk = k_pages.shape[1]
+    _ints(B=B, Lq=Lq, D=D, Hk=Hk)
+    _expect(out, _rows_shape(y_layout, B, heads, Lq, D), q, "out")
+    P, slots = _expect_cache(k_pages, v_pages, k_scales, v_scales, table, starts, counts, B, Hk, D)
+    ws, nws = _workspace(workspace)
+    status = load_library().sdattn_cache_forward(
+        _here(q, "q"), _here(k_pages, "k_pages"), _here(v_pages, "v_pages"), _here(k_scales, "k_scales"),
+        _here(v_scales, "v_scales"), _here(table, "table"), _here(starts, "starts"), _maybe(counts, "counts"),
+        _here(out, "out"), ws, nws, B, heads, Hk, Lq, D, P, slots, frame, window, sinks, ctypes.c_float(scale), x_layout,
+        y_layout, _dtype_code(q), _stream(stream))
+    _check("sdattn_cache_forward", status)
+    return out
+
+
+def window_forward_workspace(B, H, Hk, Lq, Lk, D, frame=1, window=0, sinks=0):
+    """Bytes of workspace sdattn_window_forward needs (0: none); -1 for sizes that it refuses."""
+    _ints(B=B, H=H, Hk=Hk, Lq=Lq, Lk=Lk, D=D, frame=frame, window=window, sinks=sinks)
+    return int(load_library().sdattn_window_forward_workspace(B, H, Hk, Lq, Lk, D, frame, window, sinks))
+
+
+def window_forward(q, k, v, out, scale: float, heads, kv_heads=None, workspace=None, starts=None, counts=None, frame=1,
+                   window=0, sinks=0, x_layout=LAYOUT_HEADS, y_layout=LAYOUT_HEADS, stream=None):
+    """cache_forward over 16-bit k, v [B, kv_heads, Lk, D] (or [B, Lk, kv_heads*D] in rows layout);
+    kv_heads None: heads; starts None: the queries are the last of the Lk tokens."""
+    kv_heads = heads if kv_heads is None else kv_heads
+    if _native and _done("sdattn_window_forward", _native.window_forward(
+            _fn["sdattn_window_forward"], q, k, v, out, scale, heads, kv_heads, workspace, starts, counts, frame, window,
+            sinks, x_layout, y_layout, stream)):
+        return out
+    import torch
+    _ints(heads=heads, kv_heads=kv_heads, x_layout=x_layout, y_layout=y_layout, frame=frame, window=window, sinks=sinks)
+    B, Lq, D = _rows_of(q, x_layout, heads, "q")
+    Lk = k.shape[2] if x_layout == LAYOUT_HEADS else k.shape[1]
+    _ints(B=B, Lq=Lq, Lk=Lk, D=D)
+    for t, name in ((k, "k"), (v, "v")):
+        _expect(t, _rows_shape(x_layout, B, kv_heads, Lk, D), q, name)
+    _expect(out, _rows_shape(y_layout, B, heads, Lq, D), q, "out")
+    for t, name in ((starts, "starts"), (counts, "counts")):
+        if t is not None:
+            _expect(t, (B,), None, name)
+            _expect_type(t, torch.int32, name)
+    ws, nws = _workspace(workspace)
+    status = load_library().sdattn_window_forward(
+        _here(q, "q"), _here(k, "k"), _here(v, "v"), _maybe(starts, "starts"), _maybe(counts, "counts"), _here(out, "out"),
+        ws, nws, B, heads, kv_heads, Lq, Lk, D, frame, window, sinks, ctypes.c_float(scale), x_layout, y_layout,
+        _dtype_code(q), _stream(stream))
+    _check("sdattn_window_forward", status)
     return out

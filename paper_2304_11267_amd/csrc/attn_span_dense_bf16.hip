@@ -1,0 +1,8 @@
+// attn_span_dense_bf16.hip -- instantiations of attn_span.h: bf16, 16-bit keys and values.
+#include "attn_span.h"
+
+namespace sdattn {
+
+hipError_t launch_span_dense_bf16(const SpanArgs& s) { return span_launch<kBF16, false>(s); }
+
+}  // namespace sdattn

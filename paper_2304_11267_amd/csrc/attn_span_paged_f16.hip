@@ -1,0 +1,8 @@
+// attn_span_paged_f16.hip -- instantiations of attn_span.h: fp16, 8-bit pages.
+#include "attn_span.h"
+
+namespace sdattn {
+
+hipError_t launch_span_paged_f16(const SpanArgs& s) { return span_launch<kF16, true>(s); }
+
+}  // namespace sdattn

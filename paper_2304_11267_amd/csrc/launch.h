@@ -198,6 +198,87 @@ hipError_t launch_attn_sparse_row(const SparseArgs& a);
 // the bf16 instantiations (a translation unit of their own)
 hipError_t launch_attn_sparse_bf16(const SparseArgs& a);
 
+// The steps between two blocks of a transformer (gated_norm.hip).
+constexpr int kNormNone = 0, kNormRms = 1, kNormLayer = 2;
+constexpr int kGatedMaxC = 16384;
+struct GatedNormArgs {
+    const void* x;        // [B, L, C], fp32 with `wide`
+    const void* r;        // [B, L, C] or null
+    const void* gate;     // [mod_batches, groups, C] each, or null; strides from one row to the next
+    const void* scale;
+    const void* shift;
+    const void* gamma_r;  // [C] each, or null
+    const void* gamma;
+    const void* beta;
+    void* h;              // like x (may be x), or null
+    void* y;              // [B, L, C] or null
+    int B, L, C;
+    int mod_batches, groups;
+    long long gate_stride, scale_stride, shift_stride;
+    float skip, eps;
+    int norm_r, norm;     // kNormNone, kNormRms or kNormLayer
+    bool wide;
+    int dtype;
+    void* stream;
+};
+hipError_t launch_gated_norm(const GatedNormArgs& a);
+
+// Keys and values in 8-bit pages (kv_cache.hip).
+constexpr int kCachePage = 64;       // tokens of a page
+struct CacheArgs {
+    const void* k;        // new tokens (write), or where they go (read); [B, Hk, L, D] with `heads`, else [B, L, Hk D]
+    const void* v;
+    void* k_pages;        // [pages, Hk, 64, D] codes
+    void* v_pages;
+    float* k_scales;      // [pages, Hk]
+    float* v_scales;
+    const int* table;     // [B, slots]
+    const int* starts;    // [B]
+    const int* counts;    // [B] or null
+    int B, Hk, L, D, pages, slots;
+    bool heads;
+    int dtype;
+    void* stream;
+};
+hipError_t launch_cache_write(const CacheArgs& a);
+hipError_t launch_cache_read(const CacheArgs& a);
+
+// Attention over what each query's place lets it see (attn_span.h): 16-bit keys and values, or
+// the cache's pages (table not null).
+constexpr int kSpanMinD = 32, kSpanMaxD = 160;
+struct SpanArgs {
+    const void* q;        // [B, H, Lq, D] with x_heads, else [B, Lq, H D]
+    const void* k;        // like q, of Hk heads and Lk tokens; or pages
+    const void* v;
+    const float* k_scales;
+    const float* v_scales;
+    const int* table;     // [B, slots] or null
+    const int* starts;    // [B] or null
+    const int* counts;    // [B] or null
+    void* out;            // like q, by y_heads
+    void* workspace;
+    int B, H, Hk, Lq, Lk, D;   // pages: Lk = 64 slots
+    int pages, slots;
+    int frame, window, sinks;
+    float scale;
+    bool x_heads, y_heads;
+    int dtype;
+    void* stream;
+};
+// How a call is cut up: blocks of query rows, and parts of each one's keys that are joined
+// afterwards through the workspace.
+struct SpanPlan {
+    int row_blocks, splits;
+    long long workspace;   // bytes; -1: too large
+};
+SpanPlan span_plan(const SpanArgs& a);
+hipError_t launch_span(const SpanArgs& a);
+// the instantiations (a translation unit each)
+hipError_t launch_span_dense_f16(const SpanArgs& a);
+hipError_t launch_span_dense_bf16(const SpanArgs& a);
+hipError_t launch_span_paged_f16(const SpanArgs& a);
+hipError_t launch_span_paged_bf16(const SpanArgs& a);
+
 // Winograd F(4x4, 3x3) convolution (winograd.hip).
 struct WinoFilterArgs {
     const void* w;        // [Co, Ci, 3, 3]

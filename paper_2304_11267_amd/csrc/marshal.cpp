@@ -38,6 +38,14 @@ struct Args {
         if (t && (t->sizes() != shape || t->scalar_type() != type)) return fail();
         return t;
     }
+    // tensor i of any strides, or null and ok = false
+    const at::Tensor* strided(Py_ssize_t i) {
+        if (!ok || i >= n || !THPVariable_CheckExact(v[i])) return fail();
+        const at::Tensor& t = THPVariable_Unpack(v[i]);
+        if (!t.defined() || !t.has_storage() || t.layout() != c10::kStrided || !t.is_cuda()) return fail();
+        return &t;
+    }
+    bool none(Py_ssize_t i) { return i < n && v[i] == Py_None; }
     // a tensor or None (then null, with ok as it was)
     const at::Tensor* maybe(Py_ssize_t i, at::IntArrayRef shape, c10::ScalarType type) {
         return ok && i < n && v[i] == Py_None ? nullptr : tensor(i, shape, type);
@@ -423,6 +431,155 @@ PyObject* sparse_forward(Args& a) {
                 scale, code, s);
 }
 
+// fn, x, y, r, h, gate, scale, shift, gamma_r, gamma, beta, skip, norm_r, norm, eps, stream
+PyObject* gated_norm(Args& a) {
+    const at::Tensor* x = a.tensor(1);
+    if (!x || x->dim() != 3 || a.n < 16 || (a.none(2) && a.none(4))) return nullptr;
+    const int64_t B = x->size(0), L = x->size(1), C = x->size(2), c1[] = {C};
+    // the 16-bit type is that of any tensor that has to have it
+    auto type = x->scalar_type();
+    for (Py_ssize_t i : {2, 3, 5, 6, 7, 8, 9, 10}) {
+        if (a.none(i)) continue;
+        const at::Tensor* t = a.strided(i);
+        if (!t) return nullptr;
+        type = t->scalar_type();
+        break;
+    }
+    if (type == c10::kFloat || (x->scalar_type() != type && x->scalar_type() != c10::kFloat)) return nullptr;
+    const at::Tensor *y = a.maybe(2, x->sizes(), type), *r = a.maybe(3, x->sizes(), type),
+                     *h = a.maybe(4, x->sizes(), x->scalar_type());
+    int64_t batches = 1, groups = 1, strides[3] = {0, 0, 0};
+    const at::Tensor* mods[3] = {nullptr, nullptr, nullptr};
+    bool first = true;
+    for (int i = 0; i < 3; ++i) {
+        if (a.none(5 + i)) continue;
+        const at::Tensor* t = mods[i] = a.strided(5 + i);
+        if (!t || t->dim() != 3 || t->scalar_type() != type || t->size(2) != C) return nullptr;
+        if (first) batches = t->size(0), groups = t->size(1);
+        first = false;
+        if (t->size(0) != batches || t->size(1) != groups || (batches != 1 && batches != B)) return nullptr;
+        if (C > 1 && t->stride(2) != 1) return nullptr;
+        if (batches * groups > 1) strides[i] = groups > 1 ? t->stride(1) : t->stride(0);
+        if (batches > 1 && groups > 1 && t->stride(0) != groups * strides[i]) return nullptr;
+    }
+    const at::Tensor *gr = a.maybe(8, c1, type), *g = a.maybe(9, c1, type), *beta = a.maybe(10, c1, type);
+    const float skip = a.real(11), eps = a.real(14);
+    const long long norm_r = a.integer(12), norm = a.integer(13);
+    void* s = a.stream_here(15);
+    const int xcode = type_code(*x);
+    const int code = type == c10::kHalf ? 0 : type == c10::kBFloat16 ? 1 : -1;
+    if (!a.ok || code < 0 || xcode < 0 || !fits({B, L, C, groups})) return nullptr;
+    return call(a.fn(), ptr(x), ptr(r), ptr(mods[0]), ptr(mods[1]), ptr(mods[2]), ptr(gr), ptr(g), ptr(beta), ptr(h), ptr(y),
+                (int)B, (int)L, (int)C, (int)batches, (int)groups, (long long)strides[0], (long long)strides[1],
+                (long long)strides[2], skip, (int)norm_r, (int)norm, eps, xcode, code, s);
+}
+
+// The cache's tensors from argument i on: k_pages, v_pages, k_scales, v_scales, table, starts
+struct Cache {
+    const at::Tensor *kp, *vp, *ks, *vs, *table, *starts;
+    int64_t pages, Hk, slots;
+};
+bool cache_of(Args& a, Py_ssize_t i, int64_t B, int64_t D, Cache* c) {
+    c->kp = a.tensor(i);
+    if (!c->kp || c->kp->dim() != 4) return false;
+    c->pages = c->kp->size(0), c->Hk = c->kp->size(1);
+    const int64_t ps[] = {c->pages, c->Hk, 64, D}, ss[] = {c->pages, c->Hk}, b1[] = {B};
+    for (Py_ssize_t j = 0; j < 2; ++j) {
+        const at::Tensor* t = a.tensor(i + j);
+        if (!t || t->sizes() != at::IntArrayRef(ps) || (t->scalar_type() != c10::kByte && t->scalar_type() != c10::kFloat8_e4m3fn))
+            return false;
+        (j ? c->vp : c->kp) = t;
+    }
+    c->ks = a.tensor(i + 2, ss, c10::kFloat);
+    c->vs = a.tensor(i + 3, ss, c10::kFloat);
+    c->table = a.tensor(i + 4);
+    if (!a.ok || c->table->dim() != 2 || c->table->size(0) != B || c->table->scalar_type() != c10::kInt) return false;
+    c->slots = c->table->size(1);
+    c->starts = a.tensor(i + 5, b1, c10::kInt);
+    return a.ok && fits({c->pages, c->Hk, c->slots});
+}
+
+// fn, k, v, k_pages, v_pages, k_scales, v_scales, table, starts, counts, layout, stream
+template <bool WRITE>
+PyObject* cache_call(Args& a) {
+    const at::Tensor *k = a.tensor(1), *kp = a.tensor(3);
+    const long long layout = a.integer(10);
+    int64_t B, L, C;
+    if (!a.ok || kp->dim() != 4 || kp->size(1) < 1 || !row_sizes(*k, layout, kp->size(1), &B, &L, &C) || C % kp->size(1))
+        return nullptr;
+    const int64_t D = C / kp->size(1), b1[] = {B};
+    Cache c;
+    if (!cache_of(a, 3, B, D, &c)) return nullptr;
+    const at::Tensor *v = a.tensor(2, k->sizes(), k->scalar_type()), *counts = a.maybe(9, b1, c10::kInt);
+    void* s = a.stream_here(11);
+    const int code = type_code(*k);
+    if (!a.ok || code < 0 || !fits({B, L, D})) return nullptr;
+    if (WRITE)
+        return call(a.fn(), ptr(k), ptr(v), ptr(c.kp), ptr(c.vp), ptr(c.ks), ptr(c.vs), ptr(c.table), ptr(c.starts),
+                    ptr(counts), (int)B, (int)c.Hk, (int)L, (int)D, (int)c.pages, (int)c.slots, (int)layout, code, s);
+    return call(a.fn(), ptr(c.kp), ptr(c.vp), ptr(c.ks), ptr(c.vs), ptr(c.table), ptr(c.starts), ptr(counts), ptr(k), ptr(v),
+                (int)B, (int)c.Hk, (int)L, (int)D, (int)c.pages, (int)c.slots, (int)layout, code, s);
+}
+PyObject* cache_write(Args& a) { return cache_call<true>(a); }
+PyObject* cache_read(Args& a) { return cache_call<false>(a); }
+
+// the workspace: a tensor, or None (then no bytes)
+bool workspace_of(Args& a, Py_ssize_t i, void** p, long long* bytes) {
+    *p = nullptr, *bytes = 0;
+    if (a.none(i)) return true;
+    const at::Tensor* t = a.tensor(i);
+    if (!t) return false;
+    if (t->numel() > 0) *p = t->data_ptr(), *bytes = (long long)(t->numel() * t->element_size());
+    return true;
+}
+
+// fn, q, k_pages, v_pages, k_scales, v_scales, table, starts, out, scale, heads, workspace, counts, frame, window,
+// sinks, x_layout, y_layout, stream
+PyObject* cache_forward(Args& a) {
+    const at::Tensor *q = a.tensor(1), *out = a.tensor(8);
+    const float scale = a.real(9);
+    const long long H = a.integer(10), frame = a.integer(13), window = a.integer(14), sinks = a.integer(15),
+                    xl = a.integer(16), yl = a.integer(17);
+    int64_t B, L, C;
+    if (!a.ok || H < 1 || !row_sizes(*q, xl, H, &B, &L, &C) || C % H) return nullptr;
+    const int64_t D = C / H, b1[] = {B};
+    Cache c;
+    void* ws;
+    long long nws;
+    if (!cache_of(a, 2, B, D, &c) || !workspace_of(a, 11, &ws, &nws)) return nullptr;
+    const at::Tensor* counts = a.maybe(12, b1, c10::kInt);
+    void* s = a.stream_here(18);
+    const int code = type_code(*q);
+    if (!a.ok || code < 0 || !is_rows(out, yl, H, B, L, C, q->scalar_type()) || !fits({B, L, D})) return nullptr;
+    return call(a.fn(), ptr(q), ptr(c.kp), ptr(c.vp), ptr(c.ks), ptr(c.vs), ptr(c.table), ptr(c.starts), ptr(counts), ptr(out),
+                ws, nws, (int)B, (int)H, (int)c.Hk, (int)L, (int)D, (int)c.pages, (int)c.slots, (int)frame, (int)window,
+                (int)sinks, scale, (int)xl, (int)yl, code, s);
+}
+
+// fn, q, k, v, out, scale, heads, kv_heads, workspace, starts, counts, frame, window, sinks, x_layout, y_layout, stream
+PyObject* window_forward(Args& a) {
+    const at::Tensor *q = a.tensor(1), *k = a.tensor(2), *out = a.tensor(4);
+    const float scale = a.real(5);
+    const long long H = a.integer(6), Hk = a.integer(7), frame = a.integer(11), window = a.integer(12), sinks = a.integer(13),
+                    xl = a.integer(14), yl = a.integer(15);
+    int64_t B, L, C, Bk, Lk, Ck;
+    if (!a.ok || H < 1 || Hk < 1 || !row_sizes(*q, xl, H, &B, &L, &C) || C % H || !row_sizes(*k, xl, Hk, &Bk, &Lk, &Ck))
+        return nullptr;
+    const int64_t D = C / H, b1[] = {B};
+    const auto type = q->scalar_type();
+    if (Bk != B || Ck != Hk * D || k->scalar_type() != type) return nullptr;
+    void* ws;
+    long long nws;
+    if (!workspace_of(a, 8, &ws, &nws)) return nullptr;
+    const at::Tensor *v = a.tensor(3, k->sizes(), type), *starts = a.maybe(9, b1, c10::kInt),
+                     *counts = a.maybe(10, b1, c10::kInt);
+    void* s = a.stream_here(16);
+    const int code = type_code(*q);
+    if (!a.ok || code < 0 || !is_rows(out, yl, H, B, L, C, type) || !fits({B, L, Lk, D})) return nullptr;
+    return call(a.fn(), ptr(q), ptr(k), ptr(v), ptr(starts), ptr(counts), ptr(out), ws, nws, (int)B, (int)H, (int)Hk, (int)L,
+                (int)Lk, (int)D, (int)frame, (int)window, (int)sinks, scale, (int)xl, (int)yl, code, s);
+}
+
 PyObject* use_streams(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (n == 2) {
         Py_INCREF(v[0]);
@@ -438,6 +595,7 @@ PyMethodDef methods[] = {{"use_streams", (PyCFunction)(void (*)(void))use_stream
                          FAST(forward), FAST(forward_ex), FAST(softmax_rows), FAST(logits), FAST(softmax_pv), FAST(attention_block),
                          FAST(attention_block_kv), FAST(group_norm), FAST(geglu), FAST(conv3x3),
                          FAST(linear_adapters), FAST(norm_rotate), FAST(block_means), FAST(select_blocks), FAST(sparse_forward),
+                         FAST(gated_norm), FAST(cache_write), FAST(cache_read), FAST(cache_forward), FAST(window_forward),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -198,6 +198,101 @@ constexpr int kMaxSparseLength = 1 << 30;
 int blocks_of(int L, int block) { return (L + block - 1) / block; }
 int mask_words(int nb) { return (nb + 63) / 64; }
 
+// The sizes of the cache's calls, and its bytes of pages and of scales.
+int check_cache(int B, int Hk, int D, int pages, int slots, unsigned long long* page_bytes,
+                unsigned long long* scale_bytes) {
+    if (B < 1 || Hk < 1 || D < 1 || pages < 1 || slots < 1) return SDATTN_ERR_INVALID_ARG;
+    if (D % 8 != 0 || D > 256 || Hk > 65536 || slots > kMaxSparseLength / SDATTN_CACHE_PAGE) return SDATTN_ERR_UNSUPPORTED;
+    const long long n = checked_mul({pages, Hk, SDATTN_CACHE_PAGE, D}), t = checked_mul({B, slots, 4});
+    if (n < 0 || t < 0) return SDATTN_ERR_UNSUPPORTED;
+    *page_bytes = (unsigned long long)n;
+    *scale_bytes = 4ULL * pages * Hk;
+    return SDATTN_OK;
+}
+
+// Checks of sdattn_cache_write and sdattn_cache_read: `out` and `in` are the addresses that
+// the call writes and reads of k, v, k_pages, v_pages, k_scales and v_scales.
+int run_cache(bool write, const sdattn::CacheArgs& a, int layout) {
+    if (!a.k || !a.v || !a.k_pages || !a.v_pages || !a.k_scales || !a.v_scales || !a.table || !a.starts)
+        return SDATTN_ERR_INVALID_ARG;
+    if (a.L < 1 || !is_layout(layout)) return SDATTN_ERR_INVALID_ARG;
+    int st = check_16bit(a.dtype);
+    if (st != SDATTN_OK) return st;
+    unsigned long long pb, sb;
+    if ((st = check_cache(a.B, a.Hk, a.D, a.pages, a.slots, &pb, &sb)) != SDATTN_OK) return st;
+    const long long n = checked_mul({a.B, a.Hk, a.L, a.D});
+    if (n < 0 || a.L > kMaxSparseLength) return SDATTN_ERR_UNSUPPORTED;
+    if (!aligned(a.k, 16) || !aligned(a.v, 16) || !aligned(a.k_pages, 16) || !aligned(a.v_pages, 16) ||
+        !aligned(a.k_scales, 4) || !aligned(a.v_scales, 4) || !aligned(a.table, 4) || !aligned(a.starts, 4) ||
+        (a.counts && !aligned(a.counts, 4)))
+        return SDATTN_ERR_MISALIGNED;
+    const unsigned long long nb = 2ULL * n;
+    const Span tokens[] = {{a.k, nb}, {a.v, nb}};
+    const Span cache[] = {{a.k_pages, pb}, {a.v_pages, pb}, {a.k_scales, sb}, {a.v_scales, sb}};
+    const std::initializer_list<Span> plan = {{a.table, 4ULL * a.B * a.slots}, {a.starts, 4ULL * a.B}, {a.counts, 4ULL * a.B}};
+    // outputs against each other, the rest and the plan
+    const Span* out = write ? cache : tokens;
+    const Span* in = write ? tokens : cache;
+    const int nout = write ? 4 : 2, nin = write ? 2 : 4;
+    for (int i = 0; i < nout; ++i) {
+        if (meets(out[i].p, out[i].n, plan)) return SDATTN_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return SDATTN_ERR_INVALID_ARG;
+        for (int j = 0; j < nin; ++j)
+            if (overlap(out[i].p, out[i].n, in[j].p, in[j].n)) return SDATTN_ERR_INVALID_ARG;
+    }
+    (void)hipGetLastError();
+    return finish_grid(write ? sdattn::launch_cache_write(a) : sdattn::launch_cache_read(a));
+}
+
+// The sizes of the attention over what a query sees.
+int check_span_sizes(const sdattn::SpanArgs& a) {
+    if (a.B < 1 || a.H < 1 || a.Hk < 1 || a.Lq < 1 || a.Lk < 1 || a.D < 1) return SDATTN_ERR_INVALID_ARG;
+    if (a.H % a.Hk != 0 || a.frame < 0 || a.window < 0 || a.sinks < 0) return SDATTN_ERR_INVALID_ARG;
+    if (a.D % 8 != 0 || a.D < sdattn::kSpanMinD || a.D > sdattn::kSpanMaxD || a.H > 65536) return SDATTN_ERR_UNSUPPORTED;
+    if (a.Lq > kMaxSparseLength || a.Lk > kMaxSparseLength || (long long)a.Lq * (a.H / a.Hk) > kMaxSparseLength)
+        return SDATTN_ERR_UNSUPPORTED;
+    if (checked_mul({a.B, a.H, a.Lq, a.D}) < 0 || checked_mul({a.B, a.Hk, a.Lk, a.D}) < 0) return SDATTN_ERR_UNSUPPORTED;
+    if (checked_mul({a.B, a.Hk, (a.Lq * (long long)(a.H / a.Hk) + 127) / 128}) > INT_MAX) return SDATTN_ERR_UNSUPPORTED;
+    return SDATTN_OK;
+}
+
+// the workspace of sizes that are in order, or -1
+long long span_workspace(const sdattn::SpanArgs& a) {
+    return check_span_sizes(a) == SDATTN_OK ? sdattn::span_plan(a).workspace : -1;
+}
+
+// What both calls check, `inputs` being the tensors of keys.
+int run_span(const sdattn::SpanArgs& a, long long workspace_bytes, int x_layout, int y_layout,
+             std::initializer_list<Span> inputs) {
+    if (!is_layout(x_layout) || !is_layout(y_layout) || !isfinite(a.scale)) return SDATTN_ERR_INVALID_ARG;
+    const int st = check_16bit(a.dtype);
+    if (st != SDATTN_OK) return st;
+    const long long need = sdattn::span_plan(a).workspace;
+    if (need < 0) return SDATTN_ERR_UNSUPPORTED;
+    if (need > 0 && (!a.workspace || workspace_bytes < need)) return SDATTN_ERR_INVALID_ARG;
+    if (!aligned(a.q, 16) || !aligned(a.k, 16) || !aligned(a.v, 16) || !aligned(a.out, 16) || !aligned(a.workspace, 16) ||
+        !aligned(a.k_scales, 4) || !aligned(a.v_scales, 4) || !aligned(a.table, 4) || !aligned(a.starts, 4) ||
+        !aligned(a.counts, 4))
+        return SDATTN_ERR_MISALIGNED;
+    const unsigned long long qb = 2ULL * a.B * a.H * a.Lq * a.D, wb = (unsigned long long)need;
+    const std::initializer_list<Span> more = {{a.q, qb}, {a.starts, 4ULL * a.B}, {a.counts, 4ULL * a.B}};
+    if (meets(a.out, qb, more) || meets(a.out, qb, inputs)) return SDATTN_ERR_INVALID_ARG;
+    if (need > 0 && (meets(a.workspace, wb, more) || meets(a.workspace, wb, inputs) || overlap(a.workspace, wb, a.out, qb)))
+        return SDATTN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    return finish_grid(sdattn::launch_span(a));
+}
+
+sdattn::SpanArgs cache_span(int B, int H, int Hk, int Lq, int D, int slots, int frame, int window, int sinks) {
+    sdattn::SpanArgs a{};
+    a.B = B, a.H = H, a.Hk = Hk, a.Lq = Lq, a.D = D, a.slots = slots;
+    // (more slots than there may be: refused as so many keys)
+    a.Lk = slots > kMaxSparseLength / SDATTN_CACHE_PAGE ? INT_MAX : slots < 1 ? 0 : slots * SDATTN_CACHE_PAGE;
+    a.frame = frame, a.window = window, a.sinks = sinks;
+    return a;
+}
+
 // Q, K, V (heads layout) and O (heads merged), each rounded up to 256 bytes
 long long block_part(long long elems) { return (2 * elems + 255) / 256 * 256; }
 
@@ -411,6 +506,120 @@ int sdattn_sparse_forward(const void* q, const void* k, const void* v, const voi
     if (overlap(out, 2ULL * B * H * Lq * D, mask, 8ULL * nk)) return SDATTN_ERR_INVALID_ARG;
     (void)hipGetLastError();
     return finish_grid(sdattn::launch_attn_sparse({q, k, v, mask, out, B, H, Lq, Lk, D, qblock, scale, (int)dtype, stream}));
+}
+
+int sdattn_gated_norm(const void* x, const void* r, const void* gate, const void* scale,
+                      const void* shift, const void* gamma_r, const void* gamma, const void* beta,
+                      void* h, void* y, int B, int L, int C, int mod_batches, int groups,
+                      long long gate_stride, long long scale_stride, long long shift_stride,
+                      float skip, sdattn_norm norm_r, sdattn_norm norm, float eps,
+                      sdattn_dtype x_dtype, sdattn_dtype dtype, void* stream) {
+    if (!x || (!h && !y) || (gate && !r)) return SDATTN_ERR_INVALID_ARG;
+    if (B < 1 || L < 1 || C < 1 || groups < 1 || L % groups != 0) return SDATTN_ERR_INVALID_ARG;
+    if (mod_batches != 1 && mod_batches != B) return SDATTN_ERR_INVALID_ARG;
+    if (!isfinite(skip) || !isfinite(eps) || eps < 0.0f) return SDATTN_ERR_INVALID_ARG;
+    for (const int n : {(int)norm_r, (int)norm})
+        if (n != SDATTN_NORM_NONE && n != SDATTN_NORM_RMS && n != SDATTN_NORM_LAYER) return SDATTN_ERR_INVALID_ARG;
+    const int st = check_16bit((int)dtype);
+    if (st != SDATTN_OK) return st;
+    if (x_dtype != dtype && x_dtype != SDATTN_F32)
+        return x_dtype == SDATTN_F16 || x_dtype == SDATTN_BF16 ? SDATTN_ERR_UNSUPPORTED : SDATTN_ERR_INVALID_ARG;
+    if (C % 8 != 0 || C > sdattn::kGatedMaxC) return SDATTN_ERR_UNSUPPORTED;
+    const long long n = checked_mul({B, L, C});
+    if (n < 0 || (long long)B * L > INT_MAX / 2) return SDATTN_ERR_UNSUPPORTED;
+    const long long rows = (long long)mod_batches * groups;
+    unsigned long long mb[3];   // bytes from the first modulation row to the end of the last
+    const long long strides[] = {gate_stride, scale_stride, shift_stride};
+    const void* mods[] = {gate, scale, shift};
+    for (int i = 0; i < 3; ++i) {
+        mb[i] = 0;
+        if (!mods[i]) continue;
+        if (strides[i] < 0) return SDATTN_ERR_INVALID_ARG;
+        if (strides[i] % 8 != 0) return SDATTN_ERR_MISALIGNED;
+        if (strides[i] > 0 && checked_mul({rows, strides[i], 2}) < 0) return SDATTN_ERR_UNSUPPORTED;
+        mb[i] = 2ULL * ((rows - 1) * strides[i] + C);
+    }
+    for (const void* p : {x, r, gate, scale, shift, gamma_r, gamma, beta, (const void*)h, (const void*)y})
+        if (!aligned(p, 16)) return SDATTN_ERR_MISALIGNED;
+    const bool wide = x_dtype == SDATTN_F32;
+    const unsigned long long nb = 2ULL * n, xb = wide ? 4ULL * n : nb, cb = 2ULL * C;
+    const std::initializer_list<Span> small = {{gate, mb[0]}, {scale, mb[1]}, {shift, mb[2]},
+                                               {gamma_r, cb}, {gamma, cb}, {beta, cb}, {r, nb}};
+    if (h && (meets(h, xb, small) || (h != x && overlap(h, xb, x, xb)) || (y && overlap(h, xb, y, nb))))
+        return SDATTN_ERR_INVALID_ARG;
+    if (y && (meets(y, nb, small) || overlap(y, nb, x, xb))) return SDATTN_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    return finish_grid(sdattn::launch_gated_norm({x, r, gate, scale, shift, gamma_r, gamma, beta, h, y, B, L, C,
+                                                  mod_batches, groups, gate_stride, scale_stride, shift_stride, skip, eps,
+                                                  (int)norm_r, (int)norm, wide, (int)dtype, stream}));
+}
+
+int sdattn_cache_write(const void* k, const void* v, void* k_pages, void* v_pages, float* k_scales,
+                       float* v_scales, const int* table, const int* starts, const int* counts,
+                       int B, int Hk, int L, int D, int pages, int slots, sdattn_layout layout,
+                       sdattn_dtype dtype, void* stream) {
+    return run_cache(true, {k, v, k_pages, v_pages, k_scales, v_scales, table, starts, counts, B, Hk, L, D, pages, slots,
+                            layout == SDATTN_HEADS, (int)dtype, stream}, (int)layout);
+}
+
+int sdattn_cache_read(const void* k_pages, const void* v_pages, const float* k_scales,
+                      const float* v_scales, const int* table, const int* starts, const int* counts,
+                      void* k, void* v, int B, int Hk, int L, int D, int pages, int slots,
+                      sdattn_layout layout, sdattn_dtype dtype, void* stream) {
+    return run_cache(false, {k, v, (void*)k_pages, (void*)v_pages, (float*)k_scales, (float*)v_scales, table, starts, counts,
+                             B, Hk, L, D, pages, slots, layout == SDATTN_HEADS, (int)dtype, stream}, (int)layout);
+}
+
+long long sdattn_cache_forward_workspace(int B, int H, int Hk, int Lq, int D, int slots, int frame,
+                                         int window, int sinks) {
+    sdattn::SpanArgs a = cache_span(B, H, Hk, Lq, D, slots, frame, window, sinks);
+    return span_workspace(a);
+}
+
+int sdattn_cache_forward(const void* q, const void* k_pages, const void* v_pages,
+                         const float* k_scales, const float* v_scales, const int* table,
+                         const int* starts, const int* counts, void* out, void* workspace,
+                         long long workspace_bytes, int B, int H, int Hk, int Lq, int D, int pages,
+                         int slots, int frame, int window, int sinks, float scale,
+                         sdattn_layout x_layout, sdattn_layout y_layout, sdattn_dtype dtype,
+                         void* stream) {
+    if (!q || !k_pages || !v_pages || !k_scales || !v_scales || !table || !starts || !out) return SDATTN_ERR_INVALID_ARG;
+    sdattn::SpanArgs a = cache_span(B, H, Hk, Lq, D, slots, frame, window, sinks);
+    unsigned long long pb, sb;
+    int st;
+    if ((st = check_span_sizes(a)) != SDATTN_OK || (st = check_cache(B, Hk, D, pages, slots, &pb, &sb)) != SDATTN_OK) return st;
+    a.q = q, a.k = k_pages, a.v = v_pages, a.k_scales = k_scales, a.v_scales = v_scales;
+    a.table = table, a.starts = starts, a.counts = counts, a.out = out, a.workspace = workspace;
+    a.pages = pages, a.scale = scale, a.dtype = (int)dtype, a.stream = stream;
+    a.x_heads = x_layout == SDATTN_HEADS, a.y_heads = y_layout == SDATTN_HEADS;
+    return run_span(a, workspace_bytes, (int)x_layout, (int)y_layout,
+                    {{k_pages, pb}, {v_pages, pb}, {k_scales, sb}, {v_scales, sb}, {table, 4ULL * B * slots}});
+}
+
+long long sdattn_window_forward_workspace(int B, int H, int Hk, int Lq, int Lk, int D, int frame,
+                                          int window, int sinks) {
+    sdattn::SpanArgs a{};
+    a.B = B, a.H = H, a.Hk = Hk, a.Lq = Lq, a.Lk = Lk, a.D = D;
+    a.frame = frame, a.window = window, a.sinks = sinks;
+    return span_workspace(a);
+}
+
+int sdattn_window_forward(const void* q, const void* k, const void* v, const int* starts,
+                          const int* counts, void* out, void* workspace, long long workspace_bytes,
+                          int B, int H, int Hk, int Lq, int Lk, int D, int frame, int window,
+                          int sinks, float scale, sdattn_layout x_layout, sdattn_layout y_layout,
+                          sdattn_dtype dtype, void* stream) {
+    if (!q || !k || !v || !out) return SDATTN_ERR_INVALID_ARG;
+    sdattn::SpanArgs a{};
+    a.B = B, a.H = H, a.Hk = Hk, a.Lq = Lq, a.Lk = Lk, a.D = D;
+    a.frame = frame, a.window = window, a.sinks = sinks;
+    const int st = check_span_sizes(a);
+    if (st != SDATTN_OK) return st;
+    a.q = q, a.k = k, a.v = v, a.starts = starts, a.counts = counts, a.out = out, a.workspace = workspace;
+    a.scale = scale, a.dtype = (int)dtype, a.stream = stream;
+    a.x_heads = x_layout == SDATTN_HEADS, a.y_heads = y_layout == SDATTN_HEADS;
+    const unsigned long long kb = 2ULL * B * Hk * Lk * D;
+    return run_span(a, workspace_bytes, (int)x_layout, (int)y_layout, {{k, kb}, {v, kb}});
 }
 
 long long sdattn_attention_block_workspace(int B, int Lq, int Lk, int C) {
@@ -661,6 +870,6 @@ const char* sdattn_status_str(int status) {
 
 int sdattn_last_hip_error(void) { return g_last_hip_error; }
 
-const char* sdattn_version(void) { return "sdattn 0.2.0 (gfx950)"; }
+const char* sdattn_version(void) { return "sdattn 0.3.0 (gfx950)"; }
 
 }  // extern "C"
