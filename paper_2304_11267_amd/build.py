@@ -26,7 +26,8 @@ ARCH = "gfx950"
 SOURCES = ["attn_fwd.hip", "attn_fwd_bf16.hip", "attn_fwd_stats.hip", "attn_fwd_short.hip", "attn_fwd_generic.hip",
            "attn_sparse.hip", "attn_sparse_bf16.hip", "attn_sparse_row.hip", "block_select.hip", "softmax_rows.hip",
            "attn_span.hip", "attn_span_dense_f16.hip", "attn_span_dense_bf16.hip", "attn_span_paged_f16.hip",
-           "attn_span_paged_bf16.hip", "kv_cache.hip", "gated_norm.hip",
+           "attn_span_paged_bf16.hip", "attn_span_row_dense_f16.hip", "attn_span_row_dense_bf16.hip",
+           "attn_span_row_paged_f16.hip", "attn_span_row_paged_bf16.hip", "kv_cache.hip", "gated_norm.hip",
            "twopass.hip", "linear.hip", "norm_act.hip", "norm_rotate.hip", "winograd.hip",
            "sdattn_api.hip"]
 
@@ -54,6 +55,8 @@ EXTRA_FLAGS = {
     "attn_sparse.hip": _NO_NANS, "attn_sparse_bf16.hip": _NO_NANS,
     "attn_span_dense_f16.hip": _NO_NANS, "attn_span_dense_bf16.hip": _NO_NANS,
     "attn_span_paged_f16.hip": _NO_NANS, "attn_span_paged_bf16.hip": _NO_NANS,
+    "attn_span_row_dense_f16.hip": _NO_NANS, "attn_span_row_dense_bf16.hip": _NO_NANS,
+    "attn_span_row_paged_f16.hip": _NO_NANS, "attn_span_row_paged_bf16.hip": _NO_NANS,
     "attn_fwd_short.hip": ["-mllvm", "-amdgpu-kernarg-preload-count=14"],
 }
 

@@ -439,34 +439,9 @@ hipError_t span_dispatch(const SpanKernel& a, hipStream_t stream, std::integer_s
     hipError_t r = hipErrorInvalidValue;
     const int dp = (a.D + 15) / 16 * 16;
     ((dp == 32 + 16 * I ? (void)(r = launch_span_tile<ET, 32 + 16 * I, PAGED>(a, stream)) : (void)0), ...);
-    if (r == hipSuccess && a.splits > 1) r = launch_span_join(a, ET, stream);
     return r;
 }
 using SpanWidths = std::make_integer_sequence<int, 9>;   // 32, 48, ..., 160
-
-template <int ET, bool PAGED>
-hipError_t span_launch(const SpanArgs& s) {
-    const SpanPlan p = span_plan(s);
-    SpanKernel a{};
-    a.q = (const uint16_t*)s.q, a.out = (uint16_t*)s.out;
-    a.k = (const char*)s.k, a.v = (const char*)s.v;
-    a.ks = s.k_scales, a.vs = s.v_scales, a.table = s.table, a.starts = s.starts, a.counts = s.counts;
-    a.part = (float*)s.workspace;
-    auto strides = [](bool heads, int H, int L, int D, long long* sb, long long* sh, long long* sl) {
-        *sb = (long long)H * L * D;
-        *sh = heads ? (long long)L * D : D;
-        *sl = heads ? D : (long long)H * D;
-    };
-    strides(s.x_heads, s.H, s.Lq, s.D, &a.qb, &a.qh, &a.ql);
-    strides(s.y_heads, s.H, s.Lq, s.D, &a.ob, &a.oh, &a.ol);
-    strides(s.x_heads, s.Hk, s.Lk, s.D, &a.kb, &a.kh, &a.kl);
-    a.B = s.B, a.Hk = s.Hk, a.G = s.H / s.Hk, a.Lq = s.Lq, a.Lk = s.Lk, a.D = s.D;
-    a.pages = s.pages, a.slots = s.slots;
-    a.frame = s.frame, a.window = s.window, a.sinks = s.sinks;
-    a.row_blocks = p.row_blocks, a.splits = p.splits;
-    a.c = (s.scale < 0 ? -s.scale : s.scale) * kLog2e, a.neg = s.scale < 0;
-    return span_dispatch<ET, PAGED>(a, (hipStream_t)s.stream, SpanWidths{});
-}
 
 }  // namespace
 

@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void span_join_kernel(const SpanKernel a) {
 
 }  // namespace
 
-hipError_t launch_span_join(const SpanKernel& a, int type, hipStream_t stream) {
+static hipError_t launch_span_join(const SpanKernel& a, int type, hipStream_t stream) {
     const long long threads = (long long)a.B * a.Hk * a.Lq * a.G * (a.D / 8);
     if (!grid_fits((threads + 255) / 256, 256)) return kGridTooLarge;
     auto k = type == kF16 ? span_join_kernel<kF16> : span_join_kernel<kBF16>;
@@ -54,21 +54,22 @@ hipError_t launch_span_join(const SpanKernel& a, int type, hipStream_t stream) {
 }
 
 SpanPlan span_plan(const SpanArgs& a) {
-    constexpr int kRows = 128, kTile = 64, kEnough = 512;
     SpanPlan p{};
-    const long long rows = (long long)a.Lq * (a.H / a.Hk);
-    p.row_blocks = (int)((rows + kRows - 1) / kRows);
+    const int G = a.H / a.Hk;
+    const long long rows = (long long)a.Lq * G;
+    p.single = rows <= kSpanRows;
+    const int block = p.single ? kSpanRows : 128, tile = p.single ? 32 : 64;
+    p.row_blocks = (int)((rows + block - 1) / block);
     const long long wgs = (long long)a.B * a.Hk * p.row_blocks;
     // the most tiles that a block can see
-    long long tiles = ((long long)a.Lk + kTile - 1) / kTile;
+    long long tiles = ((long long)a.Lk + tile - 1) / tile;
     if (a.window > 0) {
-        const long long spread = (long long)kRows / (a.H / a.Hk) + a.frame;   // of the block's hi
-        const long long seen = ((long long)a.sinks + kTile - 1) / kTile + ((long long)a.window + spread) / kTile + 2;
+        const long long spread = (long long)block / G + a.frame;   // of the block's hi
+        const long long seen = ((long long)a.sinks + tile - 1) / tile + ((long long)a.window + spread) / tile + 2;
         if (seen < tiles) tiles = seen;
     }
-    const long long most = tiles / 8;
-    p.splits = 1;
-    if (wgs < kEnough && most > 1) p.splits = (int)(kEnough / wgs < most ? kEnough / wgs : most);
+    const long long most = tiles / (p.single ? 16 : 8), enough = (p.single ? 1024 : 512) / wgs;
+    p.splits = (int)(enough < most ? enough : most);
     if (p.splits < 1) p.splits = 1;
     if (p.splits > 1) {
         const __int128 bytes = (__int128)p.splits * a.B * a.Hk * rows * (a.D + 2) * 4;
@@ -77,9 +78,37 @@ SpanPlan span_plan(const SpanArgs& a) {
     return p;
 }
 
-hipError_t launch_span(const SpanArgs& a) {
-    if (a.table) return a.dtype == kF16 ? launch_span_paged_f16(a) : launch_span_paged_bf16(a);
-    return a.dtype == kF16 ? launch_span_dense_f16(a) : launch_span_dense_bf16(a);
+hipError_t launch_span(const SpanArgs& s) {
+    const SpanPlan p = span_plan(s);
+    SpanKernel a{};
+    a.q = (const uint16_t*)s.q, a.out = (uint16_t*)s.out;
+    a.k = (const char*)s.k, a.v = (const char*)s.v;
+    a.ks = s.k_scales, a.vs = s.v_scales, a.table = s.table, a.starts = s.starts, a.counts = s.counts;
+    a.part = (float*)s.workspace;
+    auto strides = [](bool heads, int H, int L, int D, long long* sb, long long* sh, long long* sl) {
+        *sb = (long long)H * L * D;
+        *sh = heads ? (long long)L * D : D;
+        *sl = heads ? D : (long long)H * D;
+    };
+    strides(s.x_heads, s.H, s.Lq, s.D, &a.qb, &a.qh, &a.ql);
+    strides(s.y_heads, s.H, s.Lq, s.D, &a.ob, &a.oh, &a.ol);
+    strides(s.x_heads, s.Hk, s.Lk, s.D, &a.kb, &a.kh, &a.kl);
+    a.B = s.B, a.Hk = s.Hk, a.G = s.H / s.Hk, a.Lq = s.Lq, a.Lk = s.Lk, a.D = s.D;
+    a.pages = s.pages, a.slots = s.slots;
+    a.frame = s.frame, a.window = s.window, a.sinks = s.sinks;
+    a.row_blocks = p.row_blocks, a.splits = p.splits;
+    a.c = (s.scale < 0 ? -s.scale : s.scale) * kLog2e, a.neg = s.scale < 0;
+    const hipStream_t stream = (hipStream_t)s.stream;
+    const bool f16 = s.dtype == kF16;
+    hipError_t r;
+    if (p.single)
+        r = s.table ? (f16 ? launch_span_row_paged_f16(a, stream) : launch_span_row_paged_bf16(a, stream))
+                    : (f16 ? launch_span_row_dense_f16(a, stream) : launch_span_row_dense_bf16(a, stream));
+    else
+        r = s.table ? (f16 ? launch_span_paged_f16(a, stream) : launch_span_paged_bf16(a, stream))
+                    : (f16 ? launch_span_dense_f16(a, stream) : launch_span_dense_bf16(a, stream));
+    if (r == hipSuccess && p.splits > 1) r = launch_span_join(a, s.dtype, stream);
+    return r;
 }
 
 }  // namespace sdattn

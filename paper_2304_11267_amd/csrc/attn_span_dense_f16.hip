@@ -3,6 +3,8 @@
 
 namespace sdattn {
 
-hipError_t launch_span_dense_f16(const SpanArgs& s) { return span_launch<kF16, false>(s); }
+hipError_t launch_span_dense_f16(const SpanKernel& a, hipStream_t stream) {
+    return span_dispatch<kF16, false>(a, stream, SpanWidths{});
+}
 
 }  // namespace sdattn

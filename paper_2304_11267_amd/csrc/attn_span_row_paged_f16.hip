@@ -1,0 +1,10 @@
+// attn_span_row_paged_f16.hip -- instantiations of attn_span_row.h: fp16, 8-bit pages.
+#include "attn_span_row.h"
+
+namespace sdattn {
+
+hipError_t launch_span_row_paged_f16(const SpanKernel& a, hipStream_t stream) {
+    return span_row_dispatch<kF16, true>(a, stream, SpanRowWidths{});
+}
+
+}  // namespace sdattn

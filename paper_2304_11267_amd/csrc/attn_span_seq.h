@@ -7,6 +7,7 @@
 
 namespace sdattn {
 
+constexpr int kSpanRows = 32;          // most rows of a key head for attn_span_row.h
 constexpr float kSpanNone = -1e30f;    // the exponent's reference before the first key
 
 struct SpanKernel {
@@ -85,7 +86,14 @@ __device__ __forceinline__ SpanRun span_run(const SpanKernel& a, const SpanSeq& 
     return r;
 }
 
-// Joins the parts of each row's keys (attn_span.hip).
-hipError_t launch_span_join(const SpanKernel& a, int type, hipStream_t stream);
+// The instantiations (a translation unit each): attn_span.h's, and for few rows attn_span_row.h's.
+hipError_t launch_span_dense_f16(const SpanKernel& a, hipStream_t stream);
+hipError_t launch_span_dense_bf16(const SpanKernel& a, hipStream_t stream);
+hipError_t launch_span_paged_f16(const SpanKernel& a, hipStream_t stream);
+hipError_t launch_span_paged_bf16(const SpanKernel& a, hipStream_t stream);
+hipError_t launch_span_row_dense_f16(const SpanKernel& a, hipStream_t stream);
+hipError_t launch_span_row_dense_bf16(const SpanKernel& a, hipStream_t stream);
+hipError_t launch_span_row_paged_f16(const SpanKernel& a, hipStream_t stream);
+hipError_t launch_span_row_paged_bf16(const SpanKernel& a, hipStream_t stream);
 
 }  // namespace sdattn

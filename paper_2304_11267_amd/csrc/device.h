@@ -183,6 +183,16 @@ __device__ __forceinline__ u32x2 lds_read_tr(const char* p) {
     return __builtin_bit_cast(u32x2, v);
 }
 
+// ds_read_b64_tr_b8: within each group of 16 lanes, lane i receives byte i % 8 of the 8 bytes
+// that lanes 2 j + i / 8 point at, j = 0..7 -- eight rows of one column of a row-major tile of bytes when lanes
+// 2 j and 2 j + 1 point at 16 consecutive columns of row j.
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2_t;
+__device__ __forceinline__ u32x2 lds_read_tr8(const char* p) {
+    const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_t*)p);
+    return __builtin_bit_cast(u32x2, v);
+}
+
 // Byte offset of an LDS pointer in the workgroup's LDS.
 __device__ __forceinline__ uint32_t lds_offset(const char* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;

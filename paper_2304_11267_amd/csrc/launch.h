@@ -268,16 +268,12 @@ struct SpanArgs {
 // How a call is cut up: blocks of query rows, and parts of each one's keys that are joined
 // afterwards through the workspace.
 struct SpanPlan {
+    bool single;           // few rows: attn_span_row.h
     int row_blocks, splits;
     long long workspace;   // bytes; -1: too large
 };
 SpanPlan span_plan(const SpanArgs& a);
 hipError_t launch_span(const SpanArgs& a);
-// the instantiations (a translation unit each)
-hipError_t launch_span_dense_f16(const SpanArgs& a);
-hipError_t launch_span_dense_bf16(const SpanArgs& a);
-hipError_t launch_span_paged_f16(const SpanArgs& a);
-hipError_t launch_span_paged_bf16(const SpanArgs& a);
 
 // Winograd F(4x4, 3x3) convolution (winograd.hip).
 struct WinoFilterArgs {
