@@ -46,6 +46,27 @@ __device__ __forceinline__ u32x4 decode8(uint32_t lo, uint32_t hi, float s) {
     return r;
 }
 
+// Keeps the compiler from moving v's computation into a later block of code that alone uses it.
+template <typename T>
+__device__ __forceinline__ void computed_here(T& v) { asm volatile("" : "+v"(v)); }
+
+// Of the 32 keys from key0 on those that a query with these ends sees, one a bit.
+__device__ __forceinline__ uint32_t span_seen(int key0, int hi, int lo, int sinks) {
+    auto below = [&](int end) __attribute__((always_inline)) {
+        const int n = min(max(end - key0, 0), 32);
+        return (uint32_t)((1ull << n) - 1);
+    };
+    return below(hi) & (~below(lo) | below(sinks));
+}
+// Scores of keys whose bit is not set as minus infinity: register r is key 8 (r / 4) + r % 4.
+__device__ __forceinline__ void span_hide(f32x16& st, uint32_t seen) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const uint32_t in = (uint32_t)((int)(seen << (31 - (8 * (r >> 2) + (r & 3)))) >> 31);
+        st[r] = __uint_as_float((__float_as_uint(st[r]) & in) | (0xff800000u & ~in));
+    }
+}
+
 // whether any of 8 16-bit values is infinite or no number
 template <int ET>
 __device__ __forceinline__ bool bad8(u32x4 w) {
@@ -58,12 +79,19 @@ __device__ __forceinline__ bool bad8(u32x4 w) {
 
 // ---------------------------------------------------------------- the tiled kernel
 
-// Workgroups of 4 waves of 32 rows; K and V tiles of 64 keys as 16-bit values in two LDS
-// buffers each, rows of DP values whose 16-byte chunks lie permuted where rows would share
-// banks (chunk c of row r in the place of c ^ swap(r)).
-template <int DP>
+// Workgroups of NW waves of 32 rows.  K and V tiles of 64 keys lie as 16-bit values in a ring of three LDS
+// buffers, rows of DP values whose 16-byte chunks are permuted where rows would share banks (chunk c of row
+// r in the place of c ^ swap(r)).
+//
+// The pass is one stream over 32-key sub-tiles p = 0, 1, ...: step p issues
+//   S^T = K Q^T of sub-tile p + 1,  the weights 2^(c s - m) of p,  O^T += V^T P^T of p - 1
+// which do not depend on each other, a few operations of the vector unit behind each matrix product, in the order
+// written here (sched_barrier keeps it: a wave issues in order, and a run of either leaves the other unit
+// to the SIMD's other wave alone).  An operand of K or V is read from LDS again, for the next step,
+// behind the product that it has fed.  m is moved to a sub-tile's maximum where a weight would pass 2^15.
+template <int DP, int NW>
 struct SpanTile {
-    static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves;
+    static constexpr int kThreads = 64 * NW, kRows = 32 * NW;
     static constexpr int KC = DP / 8;                          // chunks of a row
     static constexpr int kLow = KC & -KC;
     static constexpr int kSwap = kLow > 16 ? 16 : kLow;
@@ -71,14 +99,25 @@ struct SpanTile {
     static constexpr int DN = (DP + 31) / 32;                  // 32-row tiles of O^T
     static constexpr int kTileBytes = kSpanTile * DP * 2;
     static constexpr int kBufBytes = 2 * kTileBytes;
-    static constexpr int kLdsBytes = 2 * kBufBytes + 32;       // and three words of keys
-    static constexpr int kWavesPerSimd = 2 * kLdsBytes <= 160 * 1024 ? 2 : 1;
+    static constexpr int kBufs = 3;
+    static constexpr int kLdsBytes = kBufs * kBufBytes + 32;   // and four words of keys
+    static constexpr int kAhead = DP <= 128 ? DK : DP == 144 ? 3 : 5; static_assert(DK % kAhead == 0, "a step ends where the ring does");          // operands of K read ahead of their products (what registers there are)
     static __device__ __forceinline__ int swap(int row) { return kSwap > 1 ? row / (16 / kSwap) & (kSwap - 1) : 0; }
 };
 
-template <int ET, int DP, bool PAGED>
-__global__ __launch_bounds__(SpanTile<DP>::kThreads, SpanTile<DP>::kWavesPerSimd) void span_tile_kernel(const SpanKernel a) {
-    using G = SpanTile<DP>;
+// The tiles that all queries of a run of tokens see whole: below `sinks`, or in [from, to).
+struct SpanWhole {
+    int from, to, sinks;
+    __device__ __forceinline__ bool has(int t) const { return t < to && (t >= from || t < sinks); }
+};
+__device__ __forceinline__ SpanWhole span_whole(const SpanRun& r) {
+    constexpr int TK = kSpanTile;
+    return SpanWhole{(r.lo1 + TK - 1) / TK, r.hi0 / TK, r.sinks / TK};
+}
+
+template <int ET, int DP, int NW, bool PAGED>
+__global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_kernel(const SpanKernel a) {
+    using G = SpanTile<DP, NW>;
     constexpr int DK = G::DK, DN = G::DN, KC = G::KC, TK = kSpanTile;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x;
@@ -97,22 +136,15 @@ __global__ __launch_bounds__(SpanTile<DP>::kThreads, SpanTile<DP>::kWavesPerSimd
     const int token0 = r0 / a.G, token1 = min((r0 + G::kRows - 1) / a.G, seq.count - 1);
     if (token0 >= seq.count) return;
     const int w0 = r0 + 32 * wave;
-    const int wtoken0 = w0 / a.G, wtoken1 = min((w0 + 31) / a.G, seq.count - 1);
-    const bool idle = wtoken0 >= seq.count;
+    const int wtoken0 = min(w0 / a.G, token1), wtoken1 = max(min((w0 + 31) / a.G, seq.count - 1), wtoken0);
     const SpanTiles tiles = span_tiles(a, seq, token0, token1, TK);
-    const SpanRun block = span_run(a, seq, token0, token1);
-    const SpanRun run = span_run(a, seq, min(wtoken0, token1), wtoken1);
+    const SpanWhole block = span_whole(span_run(a, seq, token0, token1));
+    const SpanWhole whole = span_whole(span_run(a, seq, wtoken0, wtoken1));
+
     // this lane's row
-    const int row = w0 + l32;
-    const int token = min(row / a.G, seq.count - 1), head = hk * a.G + row % a.G;
+    const int row = w0 + l32, token = min(row / a.G, seq.count - 1), head = hk * a.G + row % a.G;
     const bool valid = row / a.G < seq.count && row < R;
     const int hi = span_hi(a, seq, token), lo = span_lo(a, hi), sinks = a.sinks;
-
-    // this split's tiles
-    const int per = (tiles.count + a.splits - 1) / a.splits;
-    int i = split * per;
-    const int i_end = min(i + per, tiles.count);
-
     u32x4 qreg[DK];
 #pragma unroll
     for (int s = 0; s < DK; ++s) {
@@ -120,20 +152,28 @@ __global__ __launch_bounds__(SpanTile<DP>::kThreads, SpanTile<DP>::kWavesPerSimd
         u32x4 w = {0u, 0u, 0u, 0u};
         if (valid && d0 < D) w = *(const u32x4*)(a.q + b * a.qb + head * a.qh + token * a.ql + d0);
         if (a.neg) w ^= 0x80008000u;   // a negative scale (exact)
+        if (a.zero) w = u32x4{0u, 0u, 0u, 0u};
         qreg[s] = w;
     }
 
+    // this split's tiles
+    const int per = (tiles.count + a.splits - 1) / a.splits;
+    int i = split * per;
+    const int i_end = min(i + per, tiles.count);
+
     // ---- tiles into LDS
     const uint32_t lds0 = lds_offset(smem);
-    // keys whose V is no number, of this tile, the next one and the one after that: a word is
-    // cleared two tiles before it is written, so that no barrier is needed for it
-    uint64_t* const bad = (uint64_t*)(smem + 2 * G::kBufBytes);
-    // 16-bit tensors: 1 KB copies, 2 KC of them over the waves; a lane's chunk in its row
-    constexpr int kCopies = (2 * KC + G::kWaves - 1) / G::kWaves;
+    // keys of tile c whose V is no number, in word c % 4: cleared three tiles before it is written, so that no
+    // barrier is needed for it
+    uint64_t* const bad = (uint64_t*)(smem + G::kBufs * G::kBufBytes);
+    // 16-bit tensors: 1 KB copies, 2 KC of them over the waves
+    constexpr int kCopies = (2 * KC + NW - 1) / NW;
     [[maybe_unused]] const char* Kb = nullptr;
     [[maybe_unused]] const char* Vb = nullptr;
+    [[maybe_unused]] const uint32_t row_bytes = (uint32_t)a.kl * 2;
+    [[maybe_unused]] uint32_t copy_off[kCopies];
     // pages: pieces of 16 codes over the threads
-    constexpr int kPieces = (DP + 63) / 64;
+    constexpr int kPieces = (4 * DP + G::kThreads - 1) / G::kThreads;
     [[maybe_unused]] u32x4 kraw[kPieces], vraw[kPieces];
     [[maybe_unused]] int place[kPieces][2];    // of its two chunks in a tile; -1: none
     if constexpr (PAGED) {
@@ -145,34 +185,67 @@ __global__ __launch_bounds__(SpanTile<DP>::kThreads, SpanTile<DP>::kWavesPerSimd
                 place[p][e] = r < TK ? (r * KC + (c ^ G::swap(r))) * 16 : -1;
             }
         if (D != DP) {   // values past D are never written and meet zeros of Q
-            for (int z = tid; z < 2 * G::kBufBytes / 16; z += G::kThreads) *(u32x4*)(smem + z * 16) = u32x4{0u, 0u, 0u, 0u};
+            for (int z = tid; z < G::kBufs * G::kBufBytes / 16; z += G::kThreads) *(u32x4*)(smem + z * 16) = u32x4{0u, 0u, 0u, 0u};
         }
     } else {
         Kb = a.k + 2 * (b * a.kb + hk * a.kh);
         Vb = a.v + 2 * (b * a.kb + hk * a.kh);
+#pragma unroll
+        for (int p = 0; p < kCopies; ++p) {
+            const int ci = wave + p * NW, q = (ci >= KC ? ci - KC : ci) * 64 + lane, r = q / KC;
+            int c = (q - r * KC) ^ G::swap(r);
+            if (DP != D) c = min(c, D / 8 - 1);
+            copy_off[p] = (uint32_t)r * row_bytes + c * 16;
+        }
     }
-    if (tid < 3) bad[tid] = 0;
+    if (tid < 4) bad[tid] = 0;
     __syncthreads();
 
-    // the page of tile t, or -1
-    auto page_of = [&](int t) __attribute__((always_inline)) -> int {
-        const int page = __builtin_amdgcn_readfirstlane(a.table[(size_t)b * a.slots + t]);
-        return page >= 0 && page < a.pages ? page : -1;
+    // Pages and scales of places `base` .. base + 63 of the list of tiles, one a lane.
+    [[maybe_unused]] int base = i - 64, pages = 0;
+    [[maybe_unused]] float kss = 0.0f, vss = 0.0f;
+    [[maybe_unused]] uint64_t present = 0;
+    struct Tile {
+        int t, page;       // t < 0: none
+        float ks, vs;
     };
-    // the next tile from place i on that has a page; its place in *at
-    auto next_tile = [&](int from, int* page) __attribute__((always_inline)) -> int {
-        *page = 0;
+    // the tile at the first place from i on that has a page, with i past it
+    auto next_tile = [&]() __attribute__((always_inline)) -> Tile {
+        Tile x{-1, 0, 1.0f, 1.0f};
         if constexpr (PAGED) {
-            for (; from < i_end; ++from) {
-                *page = page_of(tiles.at(from));
-                if (*page >= 0) break;
+            while (i < i_end) {
+                if (i - base >= 64) {
+                    base = i;
+                    const int at = min(i + lane, i_end - 1);
+                    const int page = a.table[(size_t)b * a.slots + tiles.at(at)];
+                    const bool there = page >= 0 && page < a.pages;
+                    pages = there ? page : 0;
+                    kss = a.ks[(size_t)pages * a.Hk + hk];
+                    vss = a.vs[(size_t)pages * a.Hk + hk];
+                    present = __ballot(there && i + lane < i_end);
+                }
+                const uint64_t left = present >> (i - base);
+                if (left) {
+                    i += __builtin_ctzll(left);
+                    const int at = i - base;
+                    x.t = tiles.at(i);
+                    x.page = __builtin_amdgcn_readlane(pages, at);
+                    x.ks = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(kss), at));
+                    x.vs = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(vss), at));
+                    ++i;
+                    return x;
+                }
+                i = base + 64;
             }
+        } else if (i < i_end) {
+            x.t = tiles.at(i);
+            ++i;
         }
-        return from;
+        return x;
     };
-    auto load = [&](int t, int page, int buf) __attribute__((always_inline)) {
+    auto load = [&](const Tile& x, int buf) __attribute__((always_inline)) {
         if constexpr (PAGED) {
-            const size_t at = ((size_t)page * a.Hk + hk) * TK * D;
+            const size_t at = ((size_t)x.page * a.Hk + hk) * TK * D;
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
                 if (place[p][0] >= 0) {
@@ -181,28 +254,28 @@ __global__ __launch_bounds__(SpanTile<DP>::kThreads, SpanTile<DP>::kWavesPerSimd
                 }
             }
         } else {
-            const char *Kt = Kb + (long long)t * TK * a.kl * 2, *Vt = Vb + (long long)t * TK * a.kl * 2;
-            const int last = seq.n - 1 - t * TK;   // keys past the last one repeat it
+            const char *Kt = Kb + (long long)x.t * TK * row_bytes, *Vt = Vb + (long long)x.t * TK * row_bytes;
+            const int last = seq.n - 1 - x.t * TK;   // keys past the last one repeat it
 #pragma unroll
             for (int p = 0; p < kCopies; ++p) {
-                const int ci = wave + p * G::kWaves;
+                const int ci = wave + p * NW;
                 if (ci < 2 * KC) {
-                    const bool isv = ci >= KC;
-                    const int q = (isv ? ci - KC : ci) * 64 + lane, r = q / KC;
-                    int c = (q - r * KC) ^ G::swap(r);
-                    if (DP != D) c = min(c, D / 8 - 1);
-                    copy16_to_lds(isv ? Vt : Kt, (uint32_t)min(r, last) * (uint32_t)(a.kl * 2) + c * 16,
-                                  lds0 + buf * G::kBufBytes + ci * 1024);
+                    uint32_t off = copy_off[p];
+                    if (last < TK - 1) {
+                        const int r = ((ci >= KC ? ci - KC : ci) * 64 + lane) / KC;
+                        if (r > last) off -= (uint32_t)(r - last) * row_bytes;
+                    }
+                    copy16_to_lds(ci >= KC ? Vt : Kt, off, lds0 + buf * G::kBufBytes + ci * 1024);
                 }
             }
         }
     };
     // pages: the codes read by load as 16-bit values (V times its scale) in buffer `buf`
-    auto store = [&](int t, float vscale, int buf, uint64_t* word) __attribute__((always_inline)) {
+    auto store = [&](const Tile& x, int buf, uint64_t* word) __attribute__((always_inline)) {
         if constexpr (PAGED) {
             char* const kt = smem + buf * G::kBufBytes;
             char* const vt = kt + G::kTileBytes;
-            const bool edge = !block.all(t * TK, TK);
+            const bool end = !block.has(x.t);
 #pragma unroll
             for (int p = 0; p < kPieces; ++p)
 #pragma unroll
@@ -210,15 +283,15 @@ __global__ __launch_bounds__(SpanTile<DP>::kThreads, SpanTile<DP>::kWavesPerSimd
                     if (place[p][e] < 0) continue;
                     uint32_t lo4 = vraw[p][2 * e], hi4 = vraw[p][2 * e + 1];
                     *(u32x4*)(kt + place[p][e]) = decode8<ET>(kraw[p][2 * e], kraw[p][2 * e + 1], 1.0f);
-                    if (edge) {
+                    if (end) {
                         const int r = place[p][e] / (KC * 16);
                         // a code that is no number: 0x7f or 0xff
                         const uint64_t w = lo4 | (uint64_t)hi4 << 32, n7 = (w & 0x7f7f7f7f7f7f7f7full) + 0x0101010101010101ull;
                         const bool nan = (n7 & 0x8080808080808080ull) != 0;
-                        if (nan || t * TK + r >= seq.n) lo4 = hi4 = 0;
+                        if (nan || x.t * TK + r >= seq.n) lo4 = hi4 = 0;
                         if (nan) atomicOr((unsigned long long*)word, 1ull << r);
                     }
-                    *(u32x4*)(vt + place[p][e]) = decode8<ET>(lo4, hi4, vscale);
+                    *(u32x4*)(vt + place[p][e]) = decode8<ET>(lo4, hi4, x.vs);
                 }
         }
     };
@@ -233,164 +306,207 @@ __global__ __launch_bounds__(SpanTile<DP>::kThreads, SpanTile<DP>::kWavesPerSimd
         }
     };
 
-    // ---- per-lane places in a buffer (as in attn_fwd_kernel.h)
-    int k_off[DK], v_off[DN], v_hi[DN];
-#pragma unroll
-    for (int s = 0; s < DK; ++s) k_off[s] = (l32 * KC + ((2 * s + half) ^ G::swap(l32))) * 16;
-    {
-        const int g = lane >> 4, e = lane & 15;
-        const int key = 4 * (g >> 1) + (e >> 2);
-#pragma unroll
-        for (int n = 0; n < DN; ++n) {
-            int d = 32 * n + 16 * (g & 1) + 4 * (e & 3);
-            if (d >= DP) d -= 16;   // rows of O^T that are not stored
-            v_off[n] = G::kTileBytes + (key * KC + ((d / 8) ^ G::swap(key))) * 16 + d % 8 * 2;
-            v_hi[n] = G::kTileBytes + ((key + 8) * KC + ((d / 8) ^ G::swap(key + 8))) * 16 + d % 8 * 2;
-        }
-    }
+    // ---- per-lane places in a buffer (as in attn_fwd_kernel.h).  Where the swap has bits that chunks of one row
+    // differ in (kXor), they come into an address by exclusive or, else by addition, as part of the instruction.
+    constexpr int kXor = G::kSwap;   // a power of two: bits below it are a chunk's in its group
+    const int k_at = (l32 * KC + (half ^ G::swap(l32))) * 16;
+    const int v_key = 4 * (lane >> 5) + ((lane & 15) >> 2), v_d = 16 * (lane >> 4 & 1) + 4 * (lane & 3);
+    const int v_at = G::kTileBytes + (v_key * KC + ((v_d / 8) ^ G::swap(v_key))) * 16 + v_d % 8 * 2;
+    const int v_up = G::kTileBytes + ((v_key + 8) * KC + ((v_d / 8) ^ G::swap(v_key + 8))) * 16 + v_d % 8 * 2;
+    [[maybe_unused]] const int v_dl = 4 * (lane & 3), v_last = G::kTileBytes + (v_key * KC + ((v_dl / 8) ^ G::swap(v_key))) * 16 + v_dl % 8 * 2,
+        v_last_up = G::kTileBytes + ((v_key + 8) * KC + ((v_dl / 8) ^ G::swap(v_key + 8))) * 16 + v_dl % 8 * 2;
+    // chunk `more` on from the place at an address, `more` a constant that shares no bit with the chunk there
+    auto chunk_on = [&](int at, int more) __attribute__((always_inline)) {
+        return (at ^ ((more & (kXor - 1)) * 16)) + (more & -kXor) * 16;
+    };
 
     f32x16 acc[DN];
-    float m = kSpanNone, l = 0.0f;
+    float m = kSpanNone, l = 0.0f, alpha = 1.0f;
     int spoiled = 0;   // this lane's query sees a value that is no number
 #pragma unroll
     for (int n = 0; n < DN; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[n][r] = 0.0f;
 
-    // S^T = K Q^T, p = 2^(c s - m), O^T += V^T P^T for the tile at `key0` in buffer `buf`;
-    // ct = c times the page's scale
-    auto consume = [&](auto end_c, int buf, int key0, float ct, const uint64_t* word) __attribute__((always_inline)) {
-        constexpr bool END = decltype(end_c)::value;
-        const char* const kt = smem + buf * G::kBufBytes;
-        f32x16 st[2];
+    constexpr int NQ = DK, NP = 2 * DN, NM = NQ + NP;   // matrix products of S^T, of O^T and of a step
+    constexpr int NA = NM / 4;                          // beside the maximum
+    constexpr int KR = G::kAhead;                       // operands of K read ahead
+    u32x4 kf[KR], vf[2][DN], pk[2][2];
+    f32x16 st[2];
+    auto read_k = [&](int buf, int sub, int s) __attribute__((always_inline)) {
+        kf[s % KR] = *(const u32x4*)(smem + chunk_on(buf + k_at, 2 * s) + 32 * sub * KC * 16);
+    };
+    auto read_v = [&](int buf, int sub, int h) __attribute__((always_inline)) {
+        const int u = h / DN, n = h % DN, rows = (32 * sub + 16 * u) * KC * 16;
+        // (the second 16 of the last 32 columns may be none of DP: then the first, for rows of O^T that are not stored)
+        int at = v_at, up = v_up;
+        if (32 * n + 32 > DP) at = v_last, up = v_last_up;
+        const u32x2 x = lds_read_tr(smem + chunk_on(buf + at, 4 * n) + rows), y = lds_read_tr(smem + chunk_on(buf + up, 4 * n) + rows);
+        vf[u][n] = u32x4{x[0], x[1], y[0], y[1]};
+    };
+    const f32x16 zero = {};
+    auto s_mfma = [&](int x, int s) __attribute__((always_inline)) { st[x] = mfma32x32x16<ET>(kf[s % KR], qreg[s], s == 0 ? zero : st[x]); };
+    auto o_mfma = [&](int x, int h) __attribute__((always_inline)) {
+        acc[h % DN] = mfma32x32x16<ET>(vf[h / DN][h % DN], pk[x][h / DN], acc[h % DN]);
+    };
+    // The scores of the sub-tile at `key0` that this lane's query does not see, as minus infinity
+    auto mask = [&](int x, int key0, const uint64_t* word) __attribute__((always_inline)) {
+        const uint32_t seen = span_seen(key0, hi, lo, sinks);
+        span_hide(st[x], seen >> (4 * half));
+        // a query that sees a key whose V is no number has no number to give
+        if (seen & (uint32_t)(*word >> (key0 & 32))) spoiled = 1;
+    };
+    // m moved for st[x], where it has to be, and what that makes of the sums so far
+    auto look = [&](int x, float ct) __attribute__((always_inline)) {
+        float p = st[x][0], q = st[x][1];
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) st[sub][r] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < DK; ++s)
-                st[sub] = mfma32x32x16<ET>(*(const u32x4*)(kt + k_off[s] + 32 * sub * KC * 16), qreg[s], st[sub]);
+        for (int r = 2; r < 14; r += 4) {
+            p = fmaxf(fmaxf(p, st[x][r]), st[x][r + 1]);
+            q = fmaxf(fmaxf(q, st[x][r + 2]), st[x][r + 3]);
         }
-        uint32_t seen = ~0u;
-        if constexpr (END) {
-            seen = 0;
+        p = fmaxf(fmaxf(p, st[x][14]), st[x][15]);
+        const float mx = half_max(fmaxf(p, q)) * ct;
+        const float m_new = mx - m > kSpanLimit ? mx - kSpanBias : m;
+        alpha = fast_exp2(m - m_new);
+        l *= alpha;
+        m = m_new;
+    };
+    // The weights of st[x] as a list of operations, 2 scores at a time, each stage one unit behind the one before:
+    // c s - m, 2^, rounding and the row sum
+    constexpr int kOps = 8 * 6;
+    auto weights = [&](int x, int i, float ct) __attribute__((always_inline)) {
+        int at = 0;
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = key0 + 32 * sub + 8 * (r >> 2) + 4 * half + (r & 3);
-                    const bool in = key < hi && (key >= lo || key < sinks);
-                    seen |= in ? 1u << (16 * sub + r) : 0u;
-                    if (!in) st[sub][r] = -__builtin_inff();
-                }
+        for (int t = 0; t < 10; ++t) {
+            if (t < 8) {
+                if (i == at) st[x][2 * t] = fmaf(st[x][2 * t], ct, -m);
+                if (i == at + 1) st[x][2 * t + 1] = fmaf(st[x][2 * t + 1], ct, -m);
+                at += 2;
+            }
+            if (t >= 1 && t < 9) {
+                if (i == at) st[x][2 * t - 2] = fast_exp2(st[x][2 * t - 2]);
+                if (i == at + 1) st[x][2 * t - 1] = fast_exp2(st[x][2 * t - 1]);
+                at += 2;
+            }
+            if (t >= 2) {
+                const int w = t - 2;
+                if (i == at) pk[x][w / 4][w % 4] = pack2<ET>(st[x][2 * w], st[x][2 * w + 1]);
+                if (i == at + 1) l = add_pair<ET>(pk[x][w / 4][w % 4], l);
+                at += 2;
+            }
         }
-        float mx = fmaxf(st[0][0], st[1][0]);
+    };
+    // Step of sub-tile SUB at `key0` (`end`: key by key), of the buffer at buf; next is the next tile's.
+    auto step = [&](auto sub_c, int buf, int next, bool end, int key0, const uint64_t* word, float ct) __attribute__((always_inline)) {
+        constexpr int X = decltype(sub_c)::value, Y = 1 - X;
+        auto product = [&](int g) __attribute__((always_inline)) {
+            // S^T and O^T in turn: each is a chain on one accumulator, which two in a row would wait on
+            const int q = (g * NQ + NM - 1) / NM, h = g - q;
+            if ((g + 1) * NQ > q * NM) {
+                s_mfma(Y, q);
+                __builtin_amdgcn_sched_barrier(0);   // (the operand's registers are free now)
+                // (of sub-tile p + 1, or of the one after: X 0 has p + 1 in its own tile)
+                if (q + KR < NQ) read_k(X == 0 ? buf : next, Y, q + KR);
+                else read_k(next, X, q + KR - NQ);
+            } else {
+                o_mfma(Y, h);
+                __builtin_amdgcn_sched_barrier(0);
+                read_v(buf, X, h);
+            }
+        };
+        if (end) mask(X, key0, word);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, fmaxf(st[0][r], st[1][r]));
-        mx = half_max(mx);
-        mx = mx == -__builtin_inff() ? mx : mx * ct;   // (ct may be 0)
-        if (__any(mx - m > kSpanLimit)) {
-            const float m_new = fmaxf(m, mx - kSpanBias);
-            const float alpha = fast_exp2(m - m_new);
+        for (int g = 0; g < NA; ++g) {
+            product(g);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        look(X, ct);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = NA; g < NM; ++g) {
+            product(g);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = (g - NA) * kOps / (NM - NA); i < (g - NA + 1) * kOps / (NM - NA); ++i) weights(X, i, ct);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        computed_here(pk[X][0]);
+        computed_here(pk[X][1]);
+        computed_here(l);
+        // the products of the sub-tile before were for the m before
+        if (__any(alpha != 1.0f)) {
 #pragma unroll
             for (int n = 0; n < DN; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[n][r] *= alpha;
-            l *= alpha;
-            m = m_new;
-        }
-        u32x4 pk[2][2];
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            float p[16];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                p[r] = fast_exp2(fmaf(st[sub][r], ct, -m));
-                if (END) p[r] = seen >> (16 * sub + r) & 1 ? p[r] : 0.0f;
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    pk[sub][u][w] = pack2<ET>(p[8 * u + 2 * w], p[8 * u + 2 * w + 1]);
-                    l = add_pair<ET>(pk[sub][u][w], l);
-                }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int n = 0; n < DN; ++n) {
-                    const int at = (32 * sub + 16 * u) * KC * 16;
-                    const u32x2 x = lds_read_tr(kt + v_off[n] + at), y = lds_read_tr(kt + v_hi[n] + at);
-                    acc[n] = mfma32x32x16<ET>(u32x4{x[0], x[1], y[0], y[1]}, pk[sub][u], acc[n]);
-                }
-        }
-        if constexpr (END) {
-            const uint64_t keys = *word;
-            if (keys) {   // a query that sees one of them has no number to give
-#pragma unroll
-                for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if ((seen >> (16 * sub + r) & 1) && (keys >> (32 * sub + 8 * (r >> 2) + 4 * half + (r & 3)) & 1))
-                            spoiled = 1;
-            }
         }
     };
-    std::integral_constant<bool, false> whole_c;
-    std::integral_constant<bool, true> end_c;
+    std::integral_constant<int, 0> c0;
+    std::integral_constant<int, 1> c1;
 
-    int page = 0;
-    i = next_tile(i, &page);
-    int buf = 0, now = 0;   // buffer and word of this tile
-    float kscale = 1.0f, vscale = 1.0f;
-    auto scales = [&](int page) __attribute__((always_inline)) {
-        if constexpr (PAGED) {
-            kscale = a.ks[(size_t)page * a.Hk + hk];
-            vscale = a.vs[(size_t)page * a.Hk + hk];
+    // ---- the stream: tile c is used, the next one lies in LDS, the one after that is on its way
+    Tile t0 = next_tile(), t1{-1, 0, 1.0f, 1.0f}, t2;
+    if (t0.t >= 0) {
+        load(t0, 0);
+        store(t0, 0, &bad[0]);
+        t1 = next_tile();
+        if (t1.t >= 0) {
+            load(t1, 1);
+            store(t1, 1, &bad[1]);
         }
-    };
-    if (i < i_end) {
-        load(tiles.at(i), page, 0);
-        scales(page);
-        store(tiles.at(i), vscale, 0, &bad[0]);
-    }
-    while (i < i_end) {
-        const int t = tiles.at(i);
-        const float ct = a.c * kscale;
-        // this tile is in LDS for every wave, and the other buffer free
         wait_copies<0>();
         __syncthreads();
-        const int next = now == 2 ? 0 : now + 1, after = next == 2 ? 0 : next + 1;
-        if (tid == 0) bad[after] = 0;
-        const bool block_end = !block.all(t * TK, TK);
-        if (!PAGED && block_end) {
-            scan(buf, &bad[now]);
-            __syncthreads();
+        // the first sub-tile's scores; nothing before it
+#pragma unroll
+        for (int s = 0; s < KR; ++s) read_k(0, 0, s);
+#pragma unroll
+        for (int s = 0; s < NQ; ++s) {
+            s_mfma(0, s);
+            if (s + KR < NQ) read_k(0, 0, s + KR);
         }
-        i = next_tile(i + 1, &page);
-        if (i < i_end) {
-            load(tiles.at(i), page, buf ^ 1);
-            scales(page);
+#pragma unroll
+        for (int s = 0; s < KR; ++s) read_k(0, 1, s);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            pk[1][u] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int n = 0; n < DN; ++n) vf[u][n] = u32x4{0u, 0u, 0u, 0u};
         }
-        if (!idle && !run.none(t * TK, TK)) {
-            if (run.all(t * TK, TK)) {
-                consume(whole_c, buf, t * TK, ct, &bad[now]);
-                if (block_end && bad[now] != 0) spoiled = 1;   // (its queries see all of the tile)
-            } else {
-                consume(end_c, buf, t * TK, ct, &bad[now]);
+        int buf = 0, c = 0;
+        for (;;) {
+            const int buf1 = buf == 2 ? 0 : buf + 1, buf2 = buf1 == 2 ? 0 : buf1 + 1;
+            uint64_t* const word = &bad[c & 3];
+            if (c > 0) {   // the next tile is in LDS for every wave, and the buffer of the one before this free
+                wait_copies<0>();
+                __syncthreads();
             }
+            if (!PAGED && !block.has(t0.t)) {
+                scan(buf, word);
+                __syncthreads();
+            }
+            if (tid == 0) bad[(c + 3) & 3] = 0;
+            t2 = next_tile();
+            if (t2.t >= 0) load(t2, buf2);
+            const bool end = !whole.has(t0.t) || (!block.has(t0.t) && *word != 0);
+            const float ct = PAGED ? fmaxf(a.c * t0.ks, __FLT_MIN__) : a.c;   // (minus infinity times it stays that)
+            step(c0, buf * G::kBufBytes, buf1 * G::kBufBytes, end, t0.t * TK, word, ct);
+            step(c1, buf * G::kBufBytes, buf1 * G::kBufBytes, end, t0.t * TK + 32, word, ct);
+            if (PAGED && t2.t >= 0) store(t2, buf2, &bad[(c + 2) & 3]);
+            if (t1.t < 0) break;
+            t0 = t1;
+            t1 = t2;
+            buf = buf1;
+            ++c;
         }
-        if (PAGED && i < i_end) store(tiles.at(i), vscale, buf ^ 1, &bad[next]);
-        buf ^= 1;
-        now = next;
+#pragma unroll
+        for (int h = 0; h < NP; ++h) o_mfma(1, h);
     }
 
-    if (idle) return;
-    const float sum = half_sum(l);
     // (this file's floats are taken for numbers by the compiler: no number is made of bits)
-    spoiled |= __shfl_xor(spoiled, 32, 64);
+    const float sum = half_sum(l);
+    if (!valid) return;
     if (a.splits > 1) {
-        if (!valid) return;
         const size_t at = ((size_t)split * a.B * a.Hk + bh) * R + row;
         float* const o = a.part + at * D;
 #pragma unroll
@@ -406,7 +522,6 @@ __global__ __launch_bounds__(SpanTile<DP>::kThreads, SpanTile<DP>::kWavesPerSimd
         }
         return;
     }
-    if (!valid) return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // 0 where no key is seen
     const uint32_t nan = spoiled ? 0x7fff7fffu : 0u;     // (no number in both types)
     uint16_t* const o = a.out + b * a.ob + head * a.oh + token * a.ol;
@@ -419,12 +534,12 @@ __global__ __launch_bounds__(SpanTile<DP>::kThreads, SpanTile<DP>::kWavesPerSimd
                                                                 pack2<ET>(acc[n][4 * g + 2] * inv, acc[n][4 * g + 3] * inv) | nan};
 }
 
-template <int ET, int DP, bool PAGED>
+template <int ET, int DP, int NW, bool PAGED>
 hipError_t launch_span_tile(const SpanKernel& a, hipStream_t stream) {
-    using G = SpanTile<DP>;
+    using G = SpanTile<DP, NW>;
     const long long wgs = (long long)a.B * a.Hk * a.splits * a.row_blocks;
     if (!grid_fits(wgs, G::kThreads)) return kGridTooLarge;
-    auto kern = span_tile_kernel<ET, DP, PAGED>;
+    auto kern = span_tile_kernel<ET, DP, NW, PAGED>;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
     if (attr != hipSuccess) return attr;
@@ -438,7 +553,8 @@ template <int ET, bool PAGED, int... I>
 hipError_t span_dispatch(const SpanKernel& a, hipStream_t stream, std::integer_sequence<int, I...>) {
     hipError_t r = hipErrorInvalidValue;
     const int dp = (a.D + 15) / 16 * 16;
-    ((dp == 32 + 16 * I ? (void)(r = launch_span_tile<ET, 32 + 16 * I, PAGED>(a, stream)) : (void)0), ...);
+    ((dp == 32 + 16 * I ? (void)(r = a.block == 256 ? launch_span_tile<ET, 32 + 16 * I, 8, PAGED>(a, stream)
+                                                    : launch_span_tile<ET, 32 + 16 * I, 4, PAGED>(a, stream)) : (void)0), ...);
     return r;
 }
 using SpanWidths = std::make_integer_sequence<int, 9>;   // 32, 48, ..., 160

@@ -1,5 +1,6 @@
 // attn_span.hip -- how a call of attn_span.h is cut up, its entry point, and the join of the
 // parts of its keys.
+#include "attn_geom.h"
 #include "attn_span_seq.h"
 
 namespace sdattn {
@@ -58,9 +59,11 @@ SpanPlan span_plan(const SpanArgs& a) {
     const int G = a.H / a.Hk;
     const long long rows = (long long)a.Lq * G;
     p.single = rows <= kSpanRows;
-    const int block = p.single ? kSpanRows : 128, tile = p.single ? 32 : 64;
+    const long long heads = (long long)a.B * a.Hk;
+    p.block = p.single ? kSpanRows : a.D > 80 || heads * ((rows + 255) / 256) >= 2 * kCus ? 256 : 128;
+    const int block = p.block, tile = p.single ? 32 : 64;
     p.row_blocks = (int)((rows + block - 1) / block);
-    const long long wgs = (long long)a.B * a.Hk * p.row_blocks;
+    const long long wgs = heads * p.row_blocks;
     // the most tiles that a block can see
     long long tiles = ((long long)a.Lk + tile - 1) / tile;
     if (a.window > 0) {
@@ -68,8 +71,9 @@ SpanPlan span_plan(const SpanArgs& a) {
         const long long seen = ((long long)a.sinks + tile - 1) / tile + ((long long)a.window + spread) / tile + 2;
         if (seen < tiles) tiles = seen;
     }
-    const long long most = tiles / (p.single ? 16 : 8), enough = (p.single ? 1024 : 512) / wgs;
-    p.splits = (int)(enough < most ? enough : most);
+    // workgroups that the card holds at once
+    const long long most = tiles / (p.single ? 16 : 8), room = p.single ? 1024 : p.block == 256 ? kCus : 2 * kCus;
+    p.splits = (int)(room / wgs < most ? room / wgs : most);
     if (p.splits < 1) p.splits = 1;
     if (p.splits > 1) {
         const __int128 bytes = (__int128)p.splits * a.B * a.Hk * rows * (a.D + 2) * 4;
@@ -96,8 +100,9 @@ hipError_t launch_span(const SpanArgs& s) {
     a.B = s.B, a.Hk = s.Hk, a.G = s.H / s.Hk, a.Lq = s.Lq, a.Lk = s.Lk, a.D = s.D;
     a.pages = s.pages, a.slots = s.slots;
     a.frame = s.frame, a.window = s.window, a.sinks = s.sinks;
-    a.row_blocks = p.row_blocks, a.splits = p.splits;
-    a.c = (s.scale < 0 ? -s.scale : s.scale) * kLog2e, a.neg = s.scale < 0;
+    a.block = p.block, a.row_blocks = p.row_blocks, a.splits = p.splits;
+    a.zero = s.scale == 0.0f, a.neg = s.scale < 0;
+    a.c = a.zero ? 1.0f : (a.neg ? -s.scale : s.scale) * kLog2e;
     const hipStream_t stream = (hipStream_t)s.stream;
     const bool f16 = s.dtype == kF16;
     hipError_t r;

@@ -76,6 +76,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
         u32x4 w = {0u, 0u, 0u, 0u};
         if (d0 < D) w = *(const u32x4*)(a.q + b * a.qb + head * a.qh + token * a.ql + d0);
         if (a.neg) w ^= 0x80008000u;
+        if (a.zero) w = u32x4{0u, 0u, 0u, 0u};
         qreg[s] = w;
     }
 
@@ -195,17 +196,10 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             }
             st = mfma32x32x16<ET>(w, qreg[s], st);
         }
-        uint32_t seen = ~0u;
-        [[maybe_unused]] uint32_t keys = 0;   // whose V holds no number
         if constexpr (END) {
-            seen = 0;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int key = key0 + 8 * (r >> 2) + 4 * half + (r & 3);
-                const bool in = key < hi && (key >= lo || key < sinks);
-                seen |= in ? 1u << r : 0u;
-                if (!in) st[r] = -__builtin_inff();
-            }
+            const uint32_t seen = span_seen(key0, hi, lo, sinks);
+            span_hide(st, seen >> (4 * half));
+            uint32_t keys = 0;   // whose V holds no number
             // such values as zeros, and those of keys past the end
             char* const vt = (char*)kt + G::kCopies * 1024;
             if constexpr (PAGED) {
@@ -226,14 +220,14 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             }
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) keys |= (uint32_t)__shfl_xor((int)keys, o, 64);
+            if (keys & seen) spoiled = 1;   // a query that sees one of them has no number to give
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
         float mx = st[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, st[r]);
-        mx = half_max(mx);
-        mx = mx == -__builtin_inff() ? mx : mx * ct;
+        mx = half_max(mx) * ct;
         if (__any(mx - m > kSpanLimit)) {
             const float m_new = fmaxf(m, mx - kSpanBias);
             const float alpha = fast_exp2(m - m_new);
@@ -248,7 +242,6 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             p[r] = fast_exp2(fmaf(st[r], ct, -m));
-            if (END) p[r] = seen >> r & 1 ? p[r] : 0.0f;
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -270,13 +263,6 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
                     w = u32x4{x[0], x[1], y[0], y[1]};
                 }
                 acc[n] = mfma32x32x16<ET>(w, pk, acc[n]);
-            }
-        }
-        if constexpr (END) {
-            if (keys) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if ((seen >> r & 1) && (keys >> (8 * (r >> 2) + 4 * half + (r & 3)) & 1)) spoiled = 1;
             }
         }
     };
@@ -311,7 +297,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             }
             const int t = tile_of(i);
             if (PAGED && slot_page[slot] < 0) return;
-            const float ct = PAGED ? a.c * slot_ks[slot] : a.c;
+            const float ct = fmaxf(PAGED ? a.c * slot_ks[slot] : a.c, __FLT_MIN__);   // (minus infinity times it stays that)
             if (run.all(t * TK, TK)) use(whole_c, buf0 + slot * G::kBufBytes, t * TK, ct, slot_vs[slot]);
             else use(end_c, buf0 + slot * G::kBufBytes, t * TK, ct, slot_vs[slot]);
         });
@@ -320,7 +306,6 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
     // ---- the waves' parts: O [row][D], then m, l
     constexpr int kO = D + 4;
     l = half_sum(l);
-    spoiled |= __shfl_xor(spoiled, 32, 64);
     __syncthreads();   // every wave is done with its buffers
     float* const parts = (float*)smem;
     if (l32 < R) {

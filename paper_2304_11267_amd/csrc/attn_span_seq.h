@@ -25,9 +25,10 @@ struct SpanKernel {
     int B, Hk, G, Lq, Lk, D;
     int pages, slots;
     int frame, window, sinks;
-    int row_blocks, splits;
-    float c;                   // |scale| log2(e)
+    int block, row_blocks, splits;   // rows of a workgroup, blocks of them, parts of their keys
+    float c;                   // |scale| log2(e); with scale 0, 1 and Q is taken for zeros
     int neg;                   // scale < 0
+    int zero;                  // scale = 0
 };
 
 // A sequence's place: what is on the device is taken as it is and kept in bounds.
