@@ -79,9 +79,11 @@ __device__ __forceinline__ bool bad8(u32x4 w) {
 
 // ---------------------------------------------------------------- the tiled kernel
 
-// Workgroups of NW waves of 32 rows.  K and V tiles of 64 keys lie as 16-bit values in a ring of three LDS
-// buffers, rows of DP values whose 16-byte chunks are permuted where rows would share banks (chunk c of row
-// r in the place of c ^ swap(r)).
+// Workgroups of NW waves of 32 rows: four, and two workgroups a CU, whose waves share the SIMDs without waiting for
+// each other at barriers (eight waves of one workgroup, D = 128: one of a SIMD's two ends its tile first, and the
+// other's products then have no exponentials beside them); eight past D = 128, where registers and LDS leave no room for that.  K and V tiles
+// of 64 keys lie as 16-bit values in LDS buffers, two or three of K and two of V, rows of DP values whose 16-byte chunks are permuted
+// where rows would share banks (chunk c of row r in the place of c ^ swap(r)).
 //
 // The pass is one stream over 32-key sub-tiles p = 0, 1, ...: step p issues
 //   S^T = K Q^T of sub-tile p + 1,  the weights 2^(c s - m) of p,  O^T += V^T P^T of p - 1
@@ -98,10 +100,11 @@ struct SpanTile {
     static constexpr int DK = DP / 16;                         // 16-deep steps of S
     static constexpr int DN = (DP + 31) / 32;                  // 32-row tiles of O^T
     static constexpr int kTileBytes = kSpanTile * DP * 2;
-    static constexpr int kBufBytes = 2 * kTileBytes;
-    static constexpr int kBufs = 3;
-    static constexpr int kLdsBytes = kBufs * kBufBytes + 32;   // and four words of keys
-    static constexpr int kAhead = DP <= 128 ? DK : DP == 144 ? 3 : 5; static_assert(DK % kAhead == 0, "a step ends where the ring does");          // operands of K read ahead of their products (what registers there are)
+    // operands of K read ahead of their products: a sub-tile's, or what registers there are
+    static constexpr int kAhead = DP <= 128 ? DK : DP == 144 ? 3 : 5;
+    static_assert(DK % kAhead == 0, "a step ends where the ring does");
+    static constexpr int kBufsK = kAhead == DK ? 2 : 3;        // (with fewer, a tile's K is read while it is used)
+    static constexpr int kLdsBytes = (kBufsK + 2) * kTileBytes + 32;   // K, V, and four words of keys
     static __device__ __forceinline__ int swap(int row) { return kSwap > 1 ? row / (16 / kSwap) & (kSwap - 1) : 0; }
 };
 
@@ -118,7 +121,7 @@ __device__ __forceinline__ SpanWhole span_whole(const SpanRun& r) {
 template <int ET, int DP, int NW, bool PAGED>
 __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_kernel(const SpanKernel a) {
     using G = SpanTile<DP, NW>;
-    constexpr int DK = G::DK, DN = G::DN, KC = G::KC, TK = kSpanTile;
+    constexpr int DK = G::DK, DN = G::DN, KC = G::KC, TK = kSpanTile, NKB = G::kBufsK;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x;
     const int lane = lane_id(), l32 = lane & 31, half = lane >> 5;
@@ -165,9 +168,9 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     const uint32_t lds0 = lds_offset(smem);
     // keys of tile c whose V is no number, in word c % 4: cleared three tiles before it is written, so that no
     // barrier is needed for it
-    uint64_t* const bad = (uint64_t*)(smem + G::kBufs * G::kBufBytes);
-    // 16-bit tensors: 1 KB copies, 2 KC of them over the waves
-    constexpr int kCopies = (2 * KC + NW - 1) / NW;
+    uint64_t* const bad = (uint64_t*)(smem + (NKB + 2) * G::kTileBytes);
+    // 16-bit tensors: 1 KB copies, KC of them over the waves
+    constexpr int kCopies = (KC + NW - 1) / NW;
     [[maybe_unused]] const char* Kb = nullptr;
     [[maybe_unused]] const char* Vb = nullptr;
     [[maybe_unused]] const uint32_t row_bytes = (uint32_t)a.kl * 2;
@@ -185,14 +188,14 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
                 place[p][e] = r < TK ? (r * KC + (c ^ G::swap(r))) * 16 : -1;
             }
         if (D != DP) {   // values past D are never written and meet zeros of Q
-            for (int z = tid; z < G::kBufs * G::kBufBytes / 16; z += G::kThreads) *(u32x4*)(smem + z * 16) = u32x4{0u, 0u, 0u, 0u};
+            for (int z = tid; z < (NKB + 2) * G::kTileBytes / 16; z += G::kThreads) *(u32x4*)(smem + z * 16) = u32x4{0u, 0u, 0u, 0u};
         }
     } else {
         Kb = a.k + 2 * (b * a.kb + hk * a.kh);
         Vb = a.v + 2 * (b * a.kb + hk * a.kh);
 #pragma unroll
         for (int p = 0; p < kCopies; ++p) {
-            const int ci = wave + p * NW, q = (ci >= KC ? ci - KC : ci) * 64 + lane, r = q / KC;
+            const int q = (wave + p * NW) * 64 + lane, r = q / KC;
             int c = (q - r * KC) ^ G::swap(r);
             if (DP != D) c = min(c, D / 8 - 1);
             copy_off[p] = (uint32_t)r * row_bytes + c * 16;
@@ -243,38 +246,46 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
         }
         return x;
     };
-    auto load = [&](const Tile& x, int buf) __attribute__((always_inline)) {
+    // A tile of K or of V, from `from` (its batch item's and head's, or the pages), into buffer buf; pages: into
+    // registers, as codes.
+    auto load = [&](const Tile& x, const char* from, u32x4 (&raw)[kPieces], int buf) __attribute__((always_inline)) {
         if constexpr (PAGED) {
-            const size_t at = ((size_t)x.page * a.Hk + hk) * TK * D;
+            const char* const at = from + ((size_t)x.page * a.Hk + hk) * TK * D;
 #pragma unroll
-            for (int p = 0; p < kPieces; ++p) {
-                if (place[p][0] >= 0) {
-                    kraw[p] = *(const u32x4*)(a.k + at + (p * G::kThreads + tid) * 16);
-                    vraw[p] = *(const u32x4*)(a.v + at + (p * G::kThreads + tid) * 16);
-                }
-            }
+            for (int p = 0; p < kPieces; ++p)
+                if (place[p][0] >= 0) raw[p] = *(const u32x4*)(at + (p * G::kThreads + tid) * 16);
         } else {
-            const char *Kt = Kb + (long long)x.t * TK * row_bytes, *Vt = Vb + (long long)x.t * TK * row_bytes;
+            const char* const at = from + (long long)x.t * TK * row_bytes;
             const int last = seq.n - 1 - x.t * TK;   // keys past the last one repeat it
 #pragma unroll
             for (int p = 0; p < kCopies; ++p) {
                 const int ci = wave + p * NW;
-                if (ci < 2 * KC) {
+                if (ci < KC) {
                     uint32_t off = copy_off[p];
                     if (last < TK - 1) {
-                        const int r = ((ci >= KC ? ci - KC : ci) * 64 + lane) / KC;
+                        const int r = (ci * 64 + lane) / KC;
                         if (r > last) off -= (uint32_t)(r - last) * row_bytes;
                     }
-                    copy16_to_lds(ci >= KC ? Vt : Kt, off, lds0 + buf * G::kBufBytes + ci * 1024);
+                    copy16_to_lds(at, off, lds0 + buf * G::kTileBytes + ci * 1024);
                 }
             }
         }
     };
-    // pages: the codes read by load as 16-bit values (V times its scale) in buffer `buf`
-    auto store = [&](const Tile& x, int buf, uint64_t* word) __attribute__((always_inline)) {
+    auto load_k = [&](const Tile& x, int buf) __attribute__((always_inline)) { load(x, PAGED ? a.k : Kb, kraw, buf); };
+    auto load_v = [&](const Tile& x, int buf) __attribute__((always_inline)) { load(x, PAGED ? a.v : Vb, vraw, NKB + buf); };
+    // pages: the codes read by load as 16-bit values in buffer buf, V's times its scale
+    auto store_k = [&](int buf) __attribute__((always_inline)) {
         if constexpr (PAGED) {
-            char* const kt = smem + buf * G::kBufBytes;
-            char* const vt = kt + G::kTileBytes;
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (place[p][e] >= 0)
+                        *(u32x4*)(smem + buf * G::kTileBytes + place[p][e]) = decode8<ET>(kraw[p][2 * e], kraw[p][2 * e + 1], 1.0f);
+        }
+    };
+    auto store_v = [&](const Tile& x, int buf, uint64_t* word) __attribute__((always_inline)) {
+        if constexpr (PAGED) {
             const bool end = !block.has(x.t);
 #pragma unroll
             for (int p = 0; p < kPieces; ++p)
@@ -282,7 +293,6 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
                 for (int e = 0; e < 2; ++e) {
                     if (place[p][e] < 0) continue;
                     uint32_t lo4 = vraw[p][2 * e], hi4 = vraw[p][2 * e + 1];
-                    *(u32x4*)(kt + place[p][e]) = decode8<ET>(kraw[p][2 * e], kraw[p][2 * e + 1], 1.0f);
                     if (end) {
                         const int r = place[p][e] / (KC * 16);
                         // a code that is no number: 0x7f or 0xff
@@ -291,13 +301,13 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
                         if (nan || x.t * TK + r >= seq.n) lo4 = hi4 = 0;
                         if (nan) atomicOr((unsigned long long*)word, 1ull << r);
                     }
-                    *(u32x4*)(vt + place[p][e]) = decode8<ET>(lo4, hi4, x.vs);
+                    *(u32x4*)(smem + (NKB + buf) * G::kTileBytes + place[p][e]) = decode8<ET>(lo4, hi4, x.vs);
                 }
         }
     };
     // 16-bit tensors: chunks of V in an end tile that hold no number, as zeros, with their keys
     auto scan = [&](int buf, uint64_t* word) __attribute__((always_inline)) {
-        char* const vt = smem + buf * G::kBufBytes + G::kTileBytes;
+        char* const vt = smem + (NKB + buf) * G::kTileBytes;
         for (int q = tid; q < TK * KC; q += G::kThreads) {
             if (bad8<ET>(*(const u32x4*)(vt + q * 16))) {
                 *(u32x4*)(vt + q * 16) = u32x4{0u, 0u, 0u, 0u};
@@ -311,10 +321,10 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     constexpr int kXor = G::kSwap;   // a power of two: bits below it are a chunk's in its group
     const int k_at = (l32 * KC + (half ^ G::swap(l32))) * 16;
     const int v_key = 4 * (lane >> 5) + ((lane & 15) >> 2), v_d = 16 * (lane >> 4 & 1) + 4 * (lane & 3);
-    const int v_at = G::kTileBytes + (v_key * KC + ((v_d / 8) ^ G::swap(v_key))) * 16 + v_d % 8 * 2;
-    const int v_up = G::kTileBytes + ((v_key + 8) * KC + ((v_d / 8) ^ G::swap(v_key + 8))) * 16 + v_d % 8 * 2;
-    [[maybe_unused]] const int v_dl = 4 * (lane & 3), v_last = G::kTileBytes + (v_key * KC + ((v_dl / 8) ^ G::swap(v_key))) * 16 + v_dl % 8 * 2,
-        v_last_up = G::kTileBytes + ((v_key + 8) * KC + ((v_dl / 8) ^ G::swap(v_key + 8))) * 16 + v_dl % 8 * 2;
+    const int v_at = NKB * G::kTileBytes + (v_key * KC + ((v_d / 8) ^ G::swap(v_key))) * 16 + v_d % 8 * 2;
+    const int v_up = NKB * G::kTileBytes + ((v_key + 8) * KC + ((v_d / 8) ^ G::swap(v_key + 8))) * 16 + v_d % 8 * 2;
+    [[maybe_unused]] const int v_dl = 4 * (lane & 3), v_last = NKB * G::kTileBytes + (v_key * KC + ((v_dl / 8) ^ G::swap(v_key))) * 16 + v_dl % 8 * 2,
+        v_last_up = NKB * G::kTileBytes + ((v_key + 8) * KC + ((v_dl / 8) ^ G::swap(v_key + 8))) * 16 + v_dl % 8 * 2;
     // chunk `more` on from the place at an address, `more` a constant that shares no bit with the chunk there
     auto chunk_on = [&](int at, int more) __attribute__((always_inline)) {
         return (at ^ ((more & (kXor - 1)) * 16)) + (more & -kXor) * 16;
@@ -396,8 +406,8 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
             }
         }
     };
-    // Step of sub-tile SUB at `key0` (`end`: key by key), of the buffer at buf; next is the next tile's.
-    auto step = [&](auto sub_c, int buf, int next, bool end, int key0, const uint64_t* word, float ct) __attribute__((always_inline)) {
+    // Step of sub-tile SUB at `key0` (`end`: key by key); its tile's V lies at vbuf and K at kbuf, the next one's K at next.
+    auto step = [&](auto sub_c, int vbuf, int kbuf, int next, bool end, int key0, const uint64_t* word, float ct) __attribute__((always_inline)) {
         constexpr int X = decltype(sub_c)::value, Y = 1 - X;
         auto product = [&](int g) __attribute__((always_inline)) {
             // S^T and O^T in turn: each is a chain on one accumulator, which two in a row would wait on
@@ -406,12 +416,12 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
                 s_mfma(Y, q);
                 __builtin_amdgcn_sched_barrier(0);   // (the operand's registers are free now)
                 // (of sub-tile p + 1, or of the one after: X 0 has p + 1 in its own tile)
-                if (q + KR < NQ) read_k(X == 0 ? buf : next, Y, q + KR);
+                if (q + KR < NQ) read_k(X == 0 ? kbuf : next, Y, q + KR);
                 else read_k(next, X, q + KR - NQ);
             } else {
                 o_mfma(Y, h);
                 __builtin_amdgcn_sched_barrier(0);
-                read_v(buf, X, h);
+                read_v(vbuf, X, h);
             }
         };
         if (end) mask(X, key0, word);
@@ -445,15 +455,19 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     std::integral_constant<int, 0> c0;
     std::integral_constant<int, 1> c1;
 
-    // ---- the stream: tile c is used, the next one lies in LDS, the one after that is on its way
-    Tile t0 = next_tile(), t1{-1, 0, 1.0f, 1.0f}, t2;
+    // ---- the stream.  While tile c is used its V and the next one's K are read from LDS (its own K is in
+    // registers by then), and the next one's V and the K of the one after that are on their way.
+    const Tile none{-1, 0, 1.0f, 1.0f};
+    Tile t0 = next_tile(), t1 = none, t2;
     if (t0.t >= 0) {
-        load(t0, 0);
-        store(t0, 0, &bad[0]);
+        load_k(t0, 0);
+        load_v(t0, 0);
+        store_k(0);
+        store_v(t0, 0, &bad[0]);
         t1 = next_tile();
         if (t1.t >= 0) {
-            load(t1, 1);
-            store(t1, 1, &bad[1]);
+            load_k(t1, 1);
+            store_k(1);
         }
         wait_copies<0>();
         __syncthreads();
@@ -473,31 +487,32 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
 #pragma unroll
             for (int n = 0; n < DN; ++n) vf[u][n] = u32x4{0u, 0u, 0u, 0u};
         }
-        int buf = 0, c = 0;
-        for (;;) {
-            const int buf1 = buf == 2 ? 0 : buf + 1, buf2 = buf1 == 2 ? 0 : buf1 + 1;
+        for (int c = 0, kbuf = 0;; ++c) {
+            const int knext = kbuf + 1 == NKB ? 0 : kbuf + 1, kfree = NKB == 2 ? kbuf : knext + 1 == NKB ? 0 : knext + 1;
+            const int even = c & 1;
             uint64_t* const word = &bad[c & 3];
-            if (c > 0) {   // the next tile is in LDS for every wave, and the buffer of the one before this free
-                wait_copies<0>();
-                __syncthreads();
-            }
+            // the tiles to read are in LDS for every wave, and the other buffers free
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_copies<0>();
+            __syncthreads();
             if (!PAGED && !block.has(t0.t)) {
-                scan(buf, word);
+                scan(even, word);
                 __syncthreads();
             }
             if (tid == 0) bad[(c + 3) & 3] = 0;
-            t2 = next_tile();
-            if (t2.t >= 0) load(t2, buf2);
+            t2 = t1.t >= 0 ? next_tile() : none;
+            if (t1.t >= 0) load_v(t1, even ^ 1);
+            if (t2.t >= 0) load_k(t2, kfree);
             const bool end = !whole.has(t0.t) || (!block.has(t0.t) && *word != 0);
             const float ct = PAGED ? fmaxf(a.c * t0.ks, __FLT_MIN__) : a.c;   // (minus infinity times it stays that)
-            step(c0, buf * G::kBufBytes, buf1 * G::kBufBytes, end, t0.t * TK, word, ct);
-            step(c1, buf * G::kBufBytes, buf1 * G::kBufBytes, end, t0.t * TK + 32, word, ct);
-            if (PAGED && t2.t >= 0) store(t2, buf2, &bad[(c + 2) & 3]);
+            step(c0, even * G::kTileBytes, kbuf * G::kTileBytes, knext * G::kTileBytes, end, t0.t * TK, word, ct);
+            step(c1, even * G::kTileBytes, kbuf * G::kTileBytes, knext * G::kTileBytes, end, t0.t * TK + 32, word, ct);
             if (t1.t < 0) break;
+            store_v(t1, even ^ 1, &bad[(c + 1) & 3]);
+            if (t2.t >= 0) store_k(kfree);
             t0 = t1;
             t1 = t2;
-            buf = buf1;
-            ++c;
+            kbuf = knext;
         }
 #pragma unroll
         for (int h = 0; h < NP; ++h) o_mfma(1, h);
@@ -553,8 +568,7 @@ template <int ET, bool PAGED, int... I>
 hipError_t span_dispatch(const SpanKernel& a, hipStream_t stream, std::integer_sequence<int, I...>) {
     hipError_t r = hipErrorInvalidValue;
     const int dp = (a.D + 15) / 16 * 16;
-    ((dp == 32 + 16 * I ? (void)(r = a.block == 256 ? launch_span_tile<ET, 32 + 16 * I, 8, PAGED>(a, stream)
-                                                    : launch_span_tile<ET, 32 + 16 * I, 4, PAGED>(a, stream)) : (void)0), ...);
+    ((dp == 32 + 16 * I ? (void)(r = launch_span_tile<ET, 32 + 16 * I, (16 * I + 32 > kSpanNarrow ? 8 : 4), PAGED>(a, stream)) : (void)0), ...);
     return r;
 }
 using SpanWidths = std::make_integer_sequence<int, 9>;   // 32, 48, ..., 160

@@ -60,8 +60,7 @@ SpanPlan span_plan(const SpanArgs& a) {
     const long long rows = (long long)a.Lq * G;
     p.single = rows <= kSpanRows;
     const long long heads = (long long)a.B * a.Hk;
-    p.block = p.single ? kSpanRows : a.D > 80 || heads * ((rows + 255) / 256) >= 2 * kCus ? 256 : 128;
-    const int block = p.block, tile = p.single ? 32 : 64;
+    const int block = p.single ? kSpanRows : a.D > kSpanNarrow ? 256 : 128, tile = p.single ? 32 : 64;
     p.row_blocks = (int)((rows + block - 1) / block);
     const long long wgs = heads * p.row_blocks;
     // the most tiles that a block can see
@@ -72,7 +71,7 @@ SpanPlan span_plan(const SpanArgs& a) {
         if (seen < tiles) tiles = seen;
     }
     // workgroups that the card holds at once
-    const long long most = tiles / (p.single ? 16 : 8), room = p.single ? 1024 : p.block == 256 ? kCus : 2 * kCus;
+    const long long most = tiles / (p.single ? 16 : 8), room = p.single ? 1024 : a.D > kSpanNarrow ? kCus : 2 * kCus;
     p.splits = (int)(room / wgs < most ? room / wgs : most);
     if (p.splits < 1) p.splits = 1;
     if (p.splits > 1) {
@@ -100,7 +99,7 @@ hipError_t launch_span(const SpanArgs& s) {
     a.B = s.B, a.Hk = s.Hk, a.G = s.H / s.Hk, a.Lq = s.Lq, a.Lk = s.Lk, a.D = s.D;
     a.pages = s.pages, a.slots = s.slots;
     a.frame = s.frame, a.window = s.window, a.sinks = s.sinks;
-    a.block = p.block, a.row_blocks = p.row_blocks, a.splits = p.splits;
+    a.row_blocks = p.row_blocks, a.splits = p.splits;
     a.zero = s.scale == 0.0f, a.neg = s.scale < 0;
     a.c = a.zero ? 1.0f : (a.neg ? -s.scale : s.scale) * kLog2e;
     const hipStream_t stream = (hipStream_t)s.stream;

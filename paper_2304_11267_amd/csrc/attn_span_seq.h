@@ -8,6 +8,7 @@
 namespace sdattn {
 
 constexpr int kSpanRows = 32;          // most rows of a key head for attn_span_row.h
+constexpr int kSpanNarrow = 128;       // widest heads that the tiled kernel takes in blocks of 128 rows, not 256
 constexpr float kSpanNone = -1e30f;    // the exponent's reference before the first key
 
 struct SpanKernel {
@@ -25,7 +26,7 @@ struct SpanKernel {
     int B, Hk, G, Lq, Lk, D;
     int pages, slots;
     int frame, window, sinks;
-    int block, row_blocks, splits;   // rows of a workgroup, blocks of them, parts of their keys
+    int row_blocks, splits;    // blocks of rows, parts of their keys
     float c;                   // |scale| log2(e); with scale 0, 1 and Q is taken for zeros
     int neg;                   // scale < 0
     int zero;                  // scale = 0

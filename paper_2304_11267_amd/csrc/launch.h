@@ -269,7 +269,7 @@ struct SpanArgs {
 // afterwards through the workspace.
 struct SpanPlan {
     bool single;           // few rows: attn_span_row.h
-    int block, row_blocks, splits;
+    int row_blocks, splits;
     long long workspace;   // bytes; -1: too large
 };
 SpanPlan span_plan(const SpanArgs& a);
