@@ -7,47 +7,120 @@ namespace sdattn {
 
 namespace {
 
-// 8 values of a row a thread: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, in the order of
-// the splits.  A split without keys has l = 0, and its O is not written.
+// O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s for a row of part s's sums O_s, l_s and reference m_s, always
+// in the same order.  A part without keys has l = 0.
+struct SpanJoin {
+    const float* part;   // of a row: O_s
+    const float* ml;
+    uint16_t* out;
+    size_t apart;        // rows from one part to the next
+    bool live;
+};
+__device__ __forceinline__ SpanJoin span_join_row(const SpanKernel& a, long long at) {
+    const int R = a.Lq * a.G;
+    const size_t rows = (size_t)a.B * a.Hk * R;
+    const int bh = (int)(at / R), row = (int)(at - (long long)bh * R), b = bh / a.Hk, hk = bh - b * a.Hk;
+    const int token = row / a.G, head = hk * a.G + row - token * a.G;
+    return SpanJoin{a.part + at * a.D, a.part + a.splits * rows * a.D + at * 2,
+                    a.out + b * a.ob + head * a.oh + token * a.ol, rows, token < span_seq(a, b).count};
+}
+template <int ET>
+__device__ __forceinline__ void span_join_store(uint16_t* out, const float* o, float sum) {
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    *(u32x4*)out = u32x4{pack2<ET>(o[0] * inv, o[1] * inv), pack2<ET>(o[2] * inv, o[3] * inv),
+                         pack2<ET>(o[4] * inv, o[5] * inv), pack2<ET>(o[6] * inv, o[7] * inv)};
+}
+
+// Many rows and two or three parts: 8 values of a row a thread.
 template <int ET>
 __global__ __launch_bounds__(256) void span_join_kernel(const SpanKernel a) {
     const int pieces = a.D / 8;
-    const long long R = (long long)a.Lq * a.G, rows = a.B * (long long)a.Hk * R;
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long at = id / pieces;
-    if (at >= rows) return;
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, at = id / pieces;
+    if (at >= (long long)a.B * a.Hk * a.Lq * a.G) return;
     const int d = (int)(id - at * pieces) * 8;
-    const long long bh = at / R;
-    const int row = (int)(at - bh * R), b = (int)(bh / a.Hk), hk = (int)(bh - (long long)b * a.Hk);
-    const int token = row / a.G, head = hk * a.G + row % a.G;
-    if (token >= span_seq(a, b).count) return;
-    const float* const ml = a.part + (size_t)a.splits * rows * a.D + at * 2;
-    float top = kSpanNone;
+    const SpanJoin r = span_join_row(a, at);
+    if (!r.live) return;
+    float top = kSpanNone, sum = 0.0f, o[8];
     for (int s = 0; s < a.splits; ++s)
-        if (ml[s * rows * 2 + 1] != 0.0f) top = fmaxf(top, ml[s * rows * 2]);
-    float sum = 0.0f, o[8];
+        if (r.ml[s * r.apart * 2 + 1] != 0.0f) top = fmaxf(top, r.ml[s * r.apart * 2]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+#pragma unroll 2
     for (int s = 0; s < a.splits; ++s) {
-        const float ls = ml[s * rows * 2 + 1];
-        if (ls == 0.0f) continue;
-        const float w = fast_exp2(ml[s * rows * 2] - top);
-        const float* const p = a.part + ((size_t)s * rows + at) * a.D + d;
+        const float l = r.ml[s * r.apart * 2 + 1], w = l == 0.0f ? 0.0f : fast_exp2(r.ml[s * r.apart * 2] - top);
+        const float* const p = r.part + s * r.apart * a.D + d;
         const f32x4 x = *(const f32x4*)p, y = *(const f32x4*)(p + 4);
-        sum = fmaf(w, ls, sum);
+        sum = fmaf(w, l, sum);
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = fmaf(w, x[e], o[e]), o[4 + e] = fmaf(w, y[e], o[4 + e]);
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    *(u32x4*)(a.out + b * a.ob + head * a.oh + token * a.ol + d) =
-        u32x4{pack2<ET>(o[0] * inv, o[1] * inv), pack2<ET>(o[2] * inv, o[3] * inv), pack2<ET>(o[4] * inv, o[5] * inv),
-              pack2<ET>(o[6] * inv, o[7] * inv)};
+    span_join_store<ET>(r.out + d, o, sum);
+}
+
+// Few rows and many parts: a wave for a row's 64 values from 64 blockIdx.y on, 8 of them a lane, every eighth part,
+// all of them on their way at once.  (64 parts and more: in runs.)
+template <int ET>
+__global__ __launch_bounds__(64) void span_join_wide_kernel(const SpanKernel a) {
+    constexpr int kRun = 64;
+    const int lane = lane_id(), g = lane >> 3, d = blockIdx.y * 64 + (lane & 7) * 8;
+    const SpanJoin r = span_join_row(a, blockIdx.x);
+    if (!r.live) return;
+    const bool in = d < a.D;
+    float m = kSpanNone, sum = 0.0f, o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+    for (int s0 = 0; s0 < a.splits; s0 += kRun) {
+        const int s = s0 + lane;
+        float ms = kSpanNone, ls = 0.0f;
+        if (s < a.splits) ms = r.ml[s * r.apart * 2], ls = r.ml[s * r.apart * 2 + 1];
+        f32x4 x[kRun / 8][2];
+#pragma unroll
+        for (int i = 0; i < kRun / 8; ++i) {
+            const int p = s0 + 8 * i + g;
+            x[i][0] = x[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (p < a.splits && in) {
+                const float* const q = r.part + p * r.apart * a.D + d;
+                x[i][0] = *(const f32x4*)q;
+                x[i][1] = *(const f32x4*)(q + 4);
+            }
+        }
+        float top = fmaxf(m, ls == 0.0f ? kSpanNone : ms);
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
+        const float w = ls == 0.0f ? 0.0f : fast_exp2(ms - top), before = fast_exp2(m - top);
+        m = top;
+        float part = w * ls;
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) part += __shfl_xor(part, k, 64);
+        sum = fmaf(sum, before, part);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= before;
+#pragma unroll
+        for (int i = 0; i < kRun / 8; ++i) {
+            const float f = __shfl(w, 8 * i + g, 64);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[i][0][e], o[e]), o[4 + e] = fmaf(f, x[i][1][e], o[4 + e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int k = 8; k < 64; k <<= 1) o[e] += __shfl_xor(o[e], k, 64);
+    if (g == 0 && in) span_join_store<ET>(r.out + d, o, sum);
 }
 
 }  // namespace
 
 static hipError_t launch_span_join(const SpanKernel& a, int type, hipStream_t stream) {
-    const long long threads = (long long)a.B * a.Hk * a.Lq * a.G * (a.D / 8);
+    const long long rows = (long long)a.B * a.Hk * a.Lq * a.G;
+    if (a.splits > 3) {
+        const int blocks = (a.D + 63) / 64;
+        if (!grid_fits(rows * blocks, 64)) return kGridTooLarge;
+        auto k = type == kF16 ? span_join_wide_kernel<kF16> : span_join_wide_kernel<kBF16>;
+        hipLaunchKernelGGL(k, dim3((unsigned)rows, (unsigned)blocks), dim3(64), 0, stream, a);
+        return hipGetLastError();
+    }
+    const long long threads = rows * (a.D / 8);
     if (!grid_fits((threads + 255) / 256, 256)) return kGridTooLarge;
     auto k = type == kF16 ? span_join_kernel<kF16> : span_join_kernel<kBF16>;
     hipLaunchKernelGGL(k, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a);
@@ -75,7 +148,7 @@ SpanPlan span_plan(const SpanArgs& a) {
     p.splits = (int)(room / wgs < most ? room / wgs : most);
     if (p.splits < 1) p.splits = 1;
     if (p.splits > 1) {
-        const __int128 bytes = (__int128)p.splits * a.B * a.Hk * rows * (a.D + 2) * 4;
+        const __int128 bytes = (__int128)p.splits * heads * rows * (a.D + 2) * 4;
         p.workspace = bytes < ((__int128)1 << 62) ? (long long)bytes : -1;
     }
     return p;

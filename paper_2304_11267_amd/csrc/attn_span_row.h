@@ -34,7 +34,7 @@ struct SpanRow {
     static constexpr int kCopies = (kTileBytes + 1023) / 1024;       // 1 KB each
     static constexpr int kBufBytes = 2 * kCopies * 1024;
     static constexpr int kRoom = 160 * 1024 - 2048;
-    static constexpr int kWaves = 4 * 2 * kBufBytes <= kRoom ? 4 : 3;
+    static constexpr int kWaves = 8 * 2 * kBufBytes <= kRoom ? 8 : 4 * 2 * kBufBytes <= kRoom ? 4 : 3;
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kFit = kRoom / (kWaves * kBufBytes);
     static constexpr int kBufs = kFit > 4 ? 4 : kFit;                // tiles in LDS or on their way
@@ -196,33 +196,43 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             }
             st = mfma32x32x16<ET>(w, qreg[s], st);
         }
+        [[maybe_unused]] u32x4 hold[2] = {{~0u, ~0u, ~0u, ~0u}, {~0u, ~0u, ~0u, ~0u}};   // of 2 keys each: those that count
         if constexpr (END) {
             const uint32_t seen = span_seen(key0, hi, lo, sinks);
             span_hide(st, seen >> (4 * half));
-            uint32_t keys = 0;   // whose V holds no number
-            // such values as zeros, and those of keys past the end
-            char* const vt = (char*)kt + G::kCopies * 1024;
-            if constexpr (PAGED) {
-                for (int q = lane; q < G::kTileBytes / 8; q += 64) {
-                    const int r = q / (D / 8);
-                    const uint64_t w = *(const uint64_t*)(vt + q * 8), n7 = (w & 0x7f7f7f7f7f7f7f7full) + 0x0101010101010101ull;
-                    const bool nan = (n7 & 0x8080808080808080ull) != 0;   // 0x7f or 0xff
-                    if (nan || key0 + r >= seq.n) *(uint64_t*)(vt + q * 8) = 0;
-                    if (nan) keys |= 1u << r;
+            if (a.Lq == 1) {
+                // all queries see the same: values of keys that they do not see are zeros, whatever they hold
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int k = 16 * (i >> 2) + 8 * (i >> 1 & 1) + 4 * half + 2 * (i & 1);
+                    hold[i >> 2][i & 3] = (seen >> k & 1 ? 0xffffu : 0u) | (seen >> k & 2 ? 0xffff0000u : 0u);
                 }
             } else {
-                for (int q = lane; q < G::kTileBytes / 16; q += 64) {
-                    if (bad8<ET>(*(const u32x4*)(vt + q * 16))) {
-                        *(u32x4*)(vt + q * 16) = u32x4{0u, 0u, 0u, 0u};
-                        keys |= 1u << (q / G::KC);
+                // values that are no numbers as zeros, with their keys, and those of keys past the end
+                uint32_t keys = 0;
+                char* const vt = (char*)kt + G::kCopies * 1024;
+                if constexpr (PAGED) {
+                    for (int q = lane; q < G::kTileBytes / 8; q += 64) {
+                        const int r = q / (D / 8);
+                        const uint64_t w = *(const uint64_t*)(vt + q * 8), n7 = (w & 0x7f7f7f7f7f7f7f7full) + 0x0101010101010101ull;
+                        const bool nan = (n7 & 0x8080808080808080ull) != 0;   // 0x7f or 0xff
+                        if (nan || key0 + r >= seq.n) *(uint64_t*)(vt + q * 8) = 0;
+                        if (nan) keys |= 1u << r;
+                    }
+                } else {
+                    for (int q = lane; q < G::kTileBytes / 16; q += 64) {
+                        if (bad8<ET>(*(const u32x4*)(vt + q * 16))) {
+                            *(u32x4*)(vt + q * 16) = u32x4{0u, 0u, 0u, 0u};
+                            keys |= 1u << (q / G::KC);
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) keys |= (uint32_t)__shfl_xor((int)keys, o, 64);
-            if (keys & seen) spoiled = 1;   // a query that sees one of them has no number to give
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+                for (int o = 1; o < 64; o <<= 1) keys |= (uint32_t)__shfl_xor((int)keys, o, 64);
+                if (keys & seen) spoiled = 1;   // a query that sees one of them has no number to give
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
         }
         float mx = st[0];
 #pragma unroll
@@ -262,6 +272,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
                     const u32x2 x = lds_read_tr(kt + v_off[n] + at), y = lds_read_tr(kt + v_hi[n] + at);
                     w = u32x4{x[0], x[1], y[0], y[1]};
                 }
+                if constexpr (END) w &= hold[u];
                 acc[n] = mfma32x32x16<ET>(w, pk, acc[n]);
             }
         }

@@ -196,6 +196,7 @@ hipError_t gated_launch(const GatedKernel& a, void* stream) {
 
 template <int ET, bool WIDE>
 hipError_t gated_pick(const GatedKernel& a, void* stream) {
+    // Many tokens: a wave each; few or wide ones: a workgroup each.
     const int pieces = a.C / 8;
     if (pieces <= 64) return gated_launch<ET, WIDE, 64, 1>(a, stream);
     if (a.M >= 1024) {

@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const CacheK
 
 // 64 tokens of a sequence, one key head of K or V: the codes' values in 16 bits; zeros for
 // positions without a page.
-template <int ET>
+template <int ET, int CH>
 __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(const CacheKernel a) {
     const int D = a.D, pieces = D / 8;
     const long long item = blockIdx.x;
@@ -198,18 +198,26 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(const CacheKe
         scale[i] = there ? a.scales[which][at] : -1.0f;
     }
     uint16_t* y = a.y[which] + b * a.sb + h * a.sh + (long long)l0 * a.sl;
-    for (int c = threadIdx.x; c < rows * pieces; c += kCacheThreads) {
-        const int row = c / pieces, d = (c - row * pieces) * 8;
-        const int i = row >= split ? 1 : 0;
-        const int at = i ? row - split : kPage - split + row;
-        const float s = i ? scale[1] : scale[0];
+    u32x2 w[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = i * kCacheThreads + (int)threadIdx.x, row = c / pieces, d = (c - row * pieces) * 8;
+        const bool second = row >= split;
+        w[i] = u32x2{0u, 0u};
+        if (row < rows && (second ? scale[1] : scale[0]) >= 0.0f)
+            w[i] = *(const u32x2*)((second ? codes[1] + (size_t)(row - split) * D : codes[0] + (size_t)(kPage - split + row) * D) + d);
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = i * kCacheThreads + (int)threadIdx.x, row = c / pieces, d = (c - row * pieces) * 8;
+        if (row >= rows) continue;
+        const float s = row >= split ? scale[1] : scale[0];
         u32x4 o = {0u, 0u, 0u, 0u};
         if (s >= 0.0f) {
-            const u32x2 w = *(const u32x2*)((i ? codes[1] : codes[0]) + (size_t)at * D + d);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                o[2 * j] = pack2<ET>(__builtin_amdgcn_cvt_f32_fp8((int)w[j], 0) * s, __builtin_amdgcn_cvt_f32_fp8((int)w[j], 1) * s);
-                o[2 * j + 1] = pack2<ET>(__builtin_amdgcn_cvt_f32_fp8((int)w[j], 2) * s, __builtin_amdgcn_cvt_f32_fp8((int)w[j], 3) * s);
+                o[2 * j] = pack2<ET>(__builtin_amdgcn_cvt_f32_fp8((int)w[i][j], 0) * s, __builtin_amdgcn_cvt_f32_fp8((int)w[i][j], 1) * s);
+                o[2 * j + 1] = pack2<ET>(__builtin_amdgcn_cvt_f32_fp8((int)w[i][j], 2) * s, __builtin_amdgcn_cvt_f32_fp8((int)w[i][j], 3) * s);
             }
         }
         *(u32x4*)(y + row * a.sl + d) = o;
@@ -244,6 +252,14 @@ hipError_t write_e(const CacheArgs& c) {
     return hipGetLastError();
 }
 
+template <int ET>
+hipError_t read_e(const CacheKernel& a, long long wgs, void* stream) {
+    const int ch = (8 * a.D + kCacheThreads - 1) / kCacheThreads;
+    auto k = ch <= 2 ? cache_read_kernel<ET, 2> : ch <= 3 ? cache_read_kernel<ET, 3> : ch <= 4 ? cache_read_kernel<ET, 4> : cache_read_kernel<ET, 8>;
+    hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(kCacheThreads), 0, (hipStream_t)stream, a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_cache_write(const CacheArgs& c) { return c.dtype == kF16 ? write_e<kF16>(c) : write_e<kBF16>(c); }
@@ -254,9 +270,7 @@ hipError_t launch_cache_read(const CacheArgs& c) {
     a.blocks = (c.L + kPage - 1) / kPage;
     const long long wgs = 2LL * c.B * a.blocks * c.Hk;
     if (!grid_fits(wgs, kCacheThreads)) return kGridTooLarge;
-    auto k = c.dtype == kF16 ? cache_read_kernel<kF16> : cache_read_kernel<kBF16>;
-    hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(kCacheThreads), 0, (hipStream_t)c.stream, a);
-    return hipGetLastError();
+    return c.dtype == kF16 ? read_e<kF16>(a, wgs, c.stream) : read_e<kBF16>(a, wgs, c.stream);
 }
 
 }  // namespace sdattn
