@@ -104,7 +104,12 @@ struct SpanTile {
     static constexpr int kAhead = DP <= 128 ? DK : DP == 144 ? 3 : 5;
     static_assert(DK % kAhead == 0, "a step ends where the ring does");
     static constexpr int kBufsK = kAhead == DK ? 2 : 3;        // (with fewer, a tile's K is read while it is used)
-    static constexpr int kLdsBytes = (kBufsK + 2) * kTileBytes + 32;   // K, V, and four words of keys
+    // With columns to spare in the last 32 rows of O^T, one of them is of ones: the row sum of the weights comes out
+    // of the matrix core.  Its lanes read a constant block: a one and zeros, where 16 rows of a tile begin.
+    static constexpr bool kOnes = DP % 32 == 16;
+    static constexpr int kWords = (kBufsK + 2) * kTileBytes;   // after K and V: four words of keys,
+    static constexpr int kConst = kWords + 32;                 // and the constant block
+    static constexpr int kLdsBytes = kConst + (kOnes ? 3 * 16 * DP * 2 + 16 : 0);
     static __device__ __forceinline__ int swap(int row) { return kSwap > 1 ? row / (16 / kSwap) & (kSwap - 1) : 0; }
 };
 
@@ -128,35 +133,39 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int D = a.D;
 
+    // Blocks of the last rows, which see most, first and of the next head last: neighbours of a CU's first round
+    // meet others in its second.
     int item = xcd_remap(blockIdx.x, gridDim.x);
-    const int rb = a.row_blocks - 1 - item % a.row_blocks;   // the last rows, which see most, first
-    item /= a.row_blocks;
-    const int split = item % a.splits;
-    const int bh = item / a.splits, b = bh / a.Hk, hk = bh - b * a.Hk;
-    const SpanSeq seq = span_seq(a, b);
-    const int R = a.Lq * a.G, r0 = rb * G::kRows;
-    // tokens of this block and of this wave, the ones past `count` left out
-    const int token0 = r0 / a.G, token1 = min((r0 + G::kRows - 1) / a.G, seq.count - 1);
-    if (token0 >= seq.count) return;
-    const int w0 = r0 + 32 * wave;
-    const int wtoken0 = min(w0 / a.G, token1), wtoken1 = max(min((w0 + 31) / a.G, seq.count - 1), wtoken0);
-    const SpanTiles tiles = span_tiles(a, seq, token0, token1, TK);
-    const SpanWhole block = span_whole(span_run(a, seq, token0, token1));
-    const SpanWhole whole = span_whole(span_run(a, seq, wtoken0, wtoken1));
-
-    // this lane's row
-    const int row = w0 + l32, token = min(row / a.G, seq.count - 1), head = hk * a.G + row % a.G;
-    const bool valid = row / a.G < seq.count && row < R;
-    const int hi = span_hi(a, seq, token), lo = span_lo(a, hi), sinks = a.sinks;
+    const int turn = item / a.row_blocks;
+    int rb = item - turn * a.row_blocks;
+    if (!(turn & 1)) rb = a.row_blocks - 1 - rb;
+    const int bh = turn / a.splits, split = turn - bh * a.splits, b = bh / a.Hk, hk = bh - b * a.Hk;
+    auto token_of = [&](int row) __attribute__((always_inline)) { return a.G == 1 ? row : row / a.G; };
+    // this lane's row, and its query, which waits for nothing
+    const int R = a.Lq * a.G, r0 = rb * G::kRows, w0 = r0 + 32 * wave;
+    const int row = min(w0 + l32, R - 1), token = token_of(row), head = hk * a.G + row - token * a.G;
     u32x4 qreg[DK];
 #pragma unroll
     for (int s = 0; s < DK; ++s) {
         const int d0 = 16 * s + 8 * half;
-        u32x4 w = {0u, 0u, 0u, 0u};
-        if (valid && d0 < D) w = *(const u32x4*)(a.q + b * a.qb + head * a.qh + token * a.ql + d0);
-        if (a.neg) w ^= 0x80008000u;   // a negative scale (exact)
-        if (a.zero) w = u32x4{0u, 0u, 0u, 0u};
-        qreg[s] = w;
+        qreg[s] = u32x4{0u, 0u, 0u, 0u};
+        if (d0 < D) qreg[s] = *(const u32x4*)(a.q + b * a.qb + head * a.qh + token * a.ql + d0);
+    }
+    const SpanSeq seq = span_seq(a, b);
+    // tokens of this block and of this wave, the ones past `count` left out
+    const int token0 = token_of(r0), token1 = min(token_of(r0 + G::kRows - 1), seq.count - 1);
+    if (token0 >= seq.count) return;
+    const int wtoken0 = min(token_of(w0), token1), wtoken1 = max(min(token_of(w0 + 31), seq.count - 1), wtoken0);
+    const SpanTiles tiles = span_tiles(a, seq, token0, token1, TK);
+    const SpanWhole block = span_whole(span_run(a, seq, token0, token1));
+    const SpanWhole whole = span_whole(span_run(a, seq, wtoken0, wtoken1));
+
+    const bool valid = token < seq.count && w0 + l32 < R;
+    const int hi = span_hi(a, seq, min(token, seq.count - 1)), lo = span_lo(a, hi), sinks = a.sinks;
+#pragma unroll
+    for (int s = 0; s < DK; ++s) {
+        if (a.neg) qreg[s] ^= 0x80008000u;   // a negative scale (exact)
+        if (a.zero) qreg[s] = u32x4{0u, 0u, 0u, 0u};
     }
 
     // this split's tiles
@@ -168,7 +177,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     const uint32_t lds0 = lds_offset(smem);
     // keys of tile c whose V is no number, in word c % 4: cleared three tiles before it is written, so that no
     // barrier is needed for it
-    uint64_t* const bad = (uint64_t*)(smem + (NKB + 2) * G::kTileBytes);
+    uint64_t* const bad = (uint64_t*)(smem + G::kWords);
     // 16-bit tensors: 1 KB copies, KC of them over the waves
     constexpr int kCopies = (KC + NW - 1) / NW;
     [[maybe_unused]] const char* Kb = nullptr;
@@ -202,6 +211,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
         }
     }
     if (tid < 4) bad[tid] = 0;
+    if (G::kOnes && tid < 4) *(u32x4*)(smem + G::kConst + tid * 16 * DP * 2) = u32x4{(uint32_t)from_float<ET>(1.0f), 0u, 0u, 0u};
     __syncthreads();
 
     // Pages and scales of places `base` .. base + 63 of the list of tiles, one a lane.
@@ -323,8 +333,9 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     const int v_key = 4 * (lane >> 5) + ((lane & 15) >> 2), v_d = 16 * (lane >> 4 & 1) + 4 * (lane & 3);
     const int v_at = NKB * G::kTileBytes + (v_key * KC + ((v_d / 8) ^ G::swap(v_key))) * 16 + v_d % 8 * 2;
     const int v_up = NKB * G::kTileBytes + ((v_key + 8) * KC + ((v_d / 8) ^ G::swap(v_key + 8))) * 16 + v_d % 8 * 2;
-    [[maybe_unused]] const int v_dl = 4 * (lane & 3), v_last = NKB * G::kTileBytes + (v_key * KC + ((v_dl / 8) ^ G::swap(v_key))) * 16 + v_dl % 8 * 2,
-        v_last_up = NKB * G::kTileBytes + ((v_key + 8) * KC + ((v_dl / 8) ^ G::swap(v_key + 8))) * 16 + v_dl % 8 * 2;
+    // the last 32 columns, of which DP has 16: past D the constant block, the one at D
+    const int c_d = 32 * (DN - 1) + v_d, c_mask = G::kOnes && c_d >= D ? 0 : -1;
+    const int c_at = c_mask ? v_at + 64 * (DN - 1) : G::kConst + (c_d == D ? 0 : 8), c_up = c_mask ? v_up + 64 * (DN - 1) : c_at;
     // chunk `more` on from the place at an address, `more` a constant that shares no bit with the chunk there
     auto chunk_on = [&](int at, int more) __attribute__((always_inline)) {
         return (at ^ ((more & (kXor - 1)) * 16)) + (more & -kXor) * 16;
@@ -348,10 +359,10 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     };
     auto read_v = [&](int buf, int sub, int h) __attribute__((always_inline)) {
         const int u = h / DN, n = h % DN, rows = (32 * sub + 16 * u) * KC * 16;
-        // (the second 16 of the last 32 columns may be none of DP: then the first, for rows of O^T that are not stored)
-        int at = v_at, up = v_up;
-        if (32 * n + 32 > DP) at = v_last, up = v_last_up;
-        const u32x2 x = lds_read_tr(smem + chunk_on(buf + at, 4 * n) + rows), y = lds_read_tr(smem + chunk_on(buf + up, 4 * n) + rows);
+        const bool ones = G::kOnes && n == DN - 1;   // (kXor is 2 or 4 then: 4 n is added)
+        const char* const xp = smem + (ones ? (buf & c_mask) + c_at : chunk_on(buf + v_at, 4 * n)) + rows;
+        const char* const yp = smem + (ones ? (buf & c_mask) + c_up : chunk_on(buf + v_up, 4 * n)) + rows;
+        const u32x2 x = lds_read_tr(xp), y = lds_read_tr(yp);
         vf[u][n] = u32x4{x[0], x[1], y[0], y[1]};
     };
     const f32x16 zero = {};
@@ -376,14 +387,17 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
         }
         p = fmaxf(fmaxf(p, st[x][14]), st[x][15]);
         const float mx = half_max(fmaxf(p, q)) * ct;
-        const float m_new = mx - m > kSpanLimit ? mx - kSpanBias : m;
-        alpha = fast_exp2(m - m_new);
-        l *= alpha;
-        m = m_new;
+        alpha = 1.0f;
+        if (__any(mx - m > kSpanLimit)) {
+            const float m_new = fmaxf(m, mx - kSpanBias);
+            alpha = fast_exp2(m - m_new);
+            if (!G::kOnes) l *= alpha;
+            m = m_new;
+        }
     };
     // The weights of st[x] as a list of operations, 2 scores at a time, each stage one unit behind the one before:
     // c s - m, 2^, rounding and the row sum
-    constexpr int kOps = 8 * 6;
+    constexpr int kOut = G::kOnes ? 1 : 2, kOps = 8 * (4 + kOut);
     auto weights = [&](int x, int i, float ct) __attribute__((always_inline)) {
         int at = 0;
 #pragma unroll
@@ -401,8 +415,8 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
             if (t >= 2) {
                 const int w = t - 2;
                 if (i == at) pk[x][w / 4][w % 4] = pack2<ET>(st[x][2 * w], st[x][2 * w + 1]);
-                if (i == at + 1) l = add_pair<ET>(pk[x][w / 4][w % 4], l);
-                at += 2;
+                if (!G::kOnes && i == at + 1) l = add_pair<ET>(pk[x][w / 4][w % 4], l);
+                at += kOut;
             }
         }
     };
@@ -443,7 +457,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
         }
         computed_here(pk[X][0]);
         computed_here(pk[X][1]);
-        computed_here(l);
+        if (!G::kOnes) computed_here(l);
         // the products of the sub-tile before were for the m before
         if (__any(alpha != 1.0f)) {
 #pragma unroll
@@ -519,7 +533,14 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     }
 
     // (this file's floats are taken for numbers by the compiler: no number is made of bits)
-    const float sum = half_sum(l);
+    float sum;
+    if constexpr (G::kOnes) {
+        const float own = D == DP ? acc[DN - 1][8] : acc[DN - 1][4];   // column D, row 16 or 8 of the tile: lanes below 32
+        const float other = half_partner(own, half);
+        sum = half ? other : own;
+    } else {
+        sum = half_sum(l);
+    }
     if (!valid) return;
     if (a.splits > 1) {
         const size_t at = ((size_t)split * a.B * a.Hk + bh) * R + row;

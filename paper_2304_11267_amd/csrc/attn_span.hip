@@ -143,9 +143,14 @@ SpanPlan span_plan(const SpanArgs& a) {
         const long long seen = ((long long)a.sinks + tile - 1) / tile + ((long long)a.window + spread) / tile + 2;
         if (seen < tiles) tiles = seen;
     }
-    // workgroups that the card holds at once
-    const long long most = tiles / (p.single ? 16 : 8), room = p.single ? 1024 : a.D > kSpanNarrow ? kCus : 2 * kCus;
-    p.splits = (int)(room / wgs < most ? room / wgs : most);
+    // Parts, so that there are as many workgroups as the card holds at once.  Joining them costs a launch: with few rows
+    // four us, so from 48 tiles on, and eight at least a part.  (us; none, parts of 4 / 8 / 16 / 32 tiles: 16 heads over 2048
+    // keys D = 64 10.4, 8.5 / 9.6 / 10.3 / 12.1; 4096 16.3, 11.9 / 9.7 / 10.6 / 11.9; 8192 D = 128 55.9, 20.3 / 20.3 / 17.0 / 17.6;
+    // 64 windows of 35 tiles 7.9, 15.4 / 9.9 / 11.2; 256 or 512 workgroups: 128 heads over 4096 keys in pages, D = 80 22.6 /
+    // 27.5, 8 over 32768 D = 128 19.7 / 23.6, 64 of 11000 to 32768 80.6 / 78.0.)
+    const long long most = p.single && tiles < 48 ? 1 : tiles / 8, room = p.single || a.D > kSpanNarrow ? kCus : 2 * kCus;
+    const long long enough = p.single ? (room + wgs / 2) / wgs : room / wgs;
+    p.splits = (int)(enough < most ? enough : most);
     if (p.splits < 1) p.splits = 1;
     if (p.splits > 1) {
         const __int128 bytes = (__int128)p.splits * heads * rows * (a.D + 2) * 4;
