@@ -14,6 +14,7 @@
 // r / G, so keys are read once for all of them.
 #pragma once
 
+#include "attn_geom.h"
 #include "attn_span_seq.h"
 
 namespace sdattn {
@@ -133,12 +134,13 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int D = a.D;
 
-    // Blocks of the last rows, which see most, first and of the next head last: neighbours of a CU's first round
-    // meet others in its second.
+    // Blocks of the last rows, which see most, first; where all workgroups are on the card at once, for the next head
+    // last, so that the two of a CU differ (causal, 16 heads of 4096 tokens D = 40 77 -> 65 us; 8192 tokens D = 128, four
+    // rounds, 307 -> 374).
     int item = xcd_remap(blockIdx.x, gridDim.x);
     const int turn = item / a.row_blocks;
     int rb = item - turn * a.row_blocks;
-    if (!(turn & 1)) rb = a.row_blocks - 1 - rb;
+    if (!(turn & 1) || gridDim.x > 2 * kCus) rb = a.row_blocks - 1 - rb;
     const int bh = turn / a.splits, split = turn - bh * a.splits, b = bh / a.Hk, hk = bh - b * a.Hk;
     auto token_of = [&](int row) __attribute__((always_inline)) { return a.G == 1 ? row : row / a.G; };
     // this lane's row, and its query, which waits for nothing
@@ -387,13 +389,10 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
         }
         p = fmaxf(fmaxf(p, st[x][14]), st[x][15]);
         const float mx = half_max(fmaxf(p, q)) * ct;
-        alpha = 1.0f;
-        if (__any(mx - m > kSpanLimit)) {
-            const float m_new = fmaxf(m, mx - kSpanBias);
-            alpha = fast_exp2(m - m_new);
-            if (!G::kOnes) l *= alpha;
-            m = m_new;
-        }
+        const float m_new = mx - m > kSpanLimit ? mx - kSpanBias : m;
+        alpha = fast_exp2(m - m_new);
+        if (!G::kOnes) l *= alpha;
+        m = m_new;
     };
     // The weights of st[x] as a list of operations, 2 scores at a time, each stage one unit behind the one before:
     // c s - m, 2^, rounding and the row sum
