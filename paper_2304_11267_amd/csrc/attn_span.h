@@ -102,7 +102,7 @@ struct SpanTile {
     static constexpr int DN = (DP + 31) / 32;                  // 32-row tiles of O^T
     static constexpr int kTileBytes = kSpanTile * DP * 2;
     // operands of K read ahead of their products: a sub-tile's, or what registers there are
-    static constexpr int kAhead = DP <= 128 ? DK : DP == 144 ? 3 : 5;
+    static constexpr int kAhead = NW == 4 || DP <= 112 ? DK : DP == 144 ? 3 : 2;
     static_assert(DK % kAhead == 0, "a step ends where the ring does");
     static constexpr int kBufsK = kAhead == DK ? 2 : 3;        // (with fewer, a tile's K is read while it is used)
     // With columns to spare in the last 32 rows of O^T, one of them is of ones: the row sum of the weights comes out
@@ -588,7 +588,7 @@ template <int ET, bool PAGED, int... I>
 hipError_t span_dispatch(const SpanKernel& a, hipStream_t stream, std::integer_sequence<int, I...>) {
     hipError_t r = hipErrorInvalidValue;
     const int dp = (a.D + 15) / 16 * 16;
-    ((dp == 32 + 16 * I ? (void)(r = launch_span_tile<ET, 32 + 16 * I, (16 * I + 32 > kSpanNarrow ? 8 : 4), PAGED>(a, stream)) : (void)0), ...);
+    ((dp == 32 + 16 * I ? (void)(r = launch_span_tile<ET, 32 + 16 * I, span_block(32 + 16 * I, PAGED) / 32, PAGED>(a, stream)) : (void)0), ...);
     return r;
 }
 using SpanWidths = std::make_integer_sequence<int, 9>;   // 32, 48, ..., 160

@@ -133,7 +133,7 @@ SpanPlan span_plan(const SpanArgs& a) {
     const long long rows = (long long)a.Lq * G;
     p.single = rows <= kSpanRows;
     const long long heads = (long long)a.B * a.Hk;
-    const int block = p.single ? kSpanRows : a.D > kSpanNarrow ? 256 : 128, tile = p.single ? 32 : 64;
+    const int block = p.single ? kSpanRows : span_block((a.D + 15) / 16 * 16, a.slots > 0), tile = p.single ? 32 : 64;
     p.row_blocks = (int)((rows + block - 1) / block);
     const long long wgs = heads * p.row_blocks;
     // the most tiles that a block can see
@@ -148,7 +148,7 @@ SpanPlan span_plan(const SpanArgs& a) {
     // keys D = 64 10.4, 8.5 / 9.6 / 10.3 / 12.1; 4096 16.3, 11.9 / 9.7 / 10.6 / 11.9; 8192 D = 128 55.9, 20.3 / 20.3 / 17.0 / 17.6;
     // 64 windows of 35 tiles 7.9, 15.4 / 9.9 / 11.2; 256 or 512 workgroups: 128 heads over 4096 keys in pages, D = 80 22.6 /
     // 27.5, 8 over 32768 D = 128 19.7 / 23.6, 64 of 11000 to 32768 80.6 / 78.0.)
-    const long long most = p.single && tiles < 48 ? 1 : tiles / 8, room = p.single || a.D > kSpanNarrow ? kCus : 2 * kCus;
+    const long long most = p.single && tiles < 48 ? 1 : tiles / 8, room = p.single || block == 256 ? kCus : 2 * kCus;
     const long long enough = p.single ? (room + wgs / 2) / wgs : room / wgs;
     p.splits = (int)(enough < most ? enough : most);
     if (p.splits < 1) p.splits = 1;

@@ -8,7 +8,9 @@
 namespace sdattn {
 
 constexpr int kSpanRows = 32;          // most rows of a key head for attn_span_row.h
-constexpr int kSpanNarrow = 128;       // widest heads that the tiled kernel takes in blocks of 128 rows, not 256
+// Rows of a block of the tiled kernel for heads of D (a multiple of 16).  Wide heads have no registers for the codes of
+// pages beside 128 rows.
+constexpr int span_block(int D, bool paged) { return D > (paged ? 96 : 128) ? 256 : 128; }
 constexpr float kSpanNone = -1e30f;    // the exponent's reference before the first key
 
 struct SpanKernel {

@@ -257,7 +257,7 @@ struct SpanArgs {
     const int* counts;    // [B] or null
     void* out;            // like q, by y_heads
     void* workspace;
-    int B, H, Hk, Lq, Lk, D;   // pages: Lk = 64 slots
+    int B, H, Hk, Lq, Lk, D;   // pages: Lk = 64 slots, else slots = 0
     int pages, slots;
     int frame, window, sinks;
     float scale;
