@@ -162,7 +162,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     const SpanWhole block = span_whole(span_run(a, seq, token0, token1));
     const SpanWhole whole = span_whole(span_run(a, seq, wtoken0, wtoken1));
 
-    const bool valid = token < seq.count && w0 + l32 < R;
+    const bool valid = token < seq.count && w0 + l32 < R, live = w0 < R && token_of(w0) < seq.count;
     const int hi = span_hi(a, seq, min(token, seq.count - 1)), lo = span_lo(a, hi), sinks = a.sinks;
 #pragma unroll
     for (int s = 0; s < DK; ++s) {
@@ -518,8 +518,10 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
             if (t2.t >= 0) load_k(t2, kfree);
             const bool end = !whole.has(t0.t) || (!block.has(t0.t) && *word != 0);
             const float ct = PAGED ? fmaxf(a.c * t0.ks, __FLT_MIN__) : a.c;   // (minus infinity times it stays that)
-            step(c0, even * G::kTileBytes, kbuf * G::kTileBytes, knext * G::kTileBytes, end, t0.t * TK, word, ct);
-            step(c1, even * G::kTileBytes, kbuf * G::kTileBytes, knext * G::kTileBytes, end, t0.t * TK + 32, word, ct);
+            if (live) {   // (waves without rows copy tiles for the others)
+                step(c0, even * G::kTileBytes, kbuf * G::kTileBytes, knext * G::kTileBytes, end, t0.t * TK, word, ct);
+                step(c1, even * G::kTileBytes, kbuf * G::kTileBytes, knext * G::kTileBytes, end, t0.t * TK + 32, word, ct);
+            }
             if (t1.t < 0) break;
             store_v(t1, even ^ 1, &bad[(c + 1) & 3]);
             if (t2.t >= 0) store_k(kfree);
