@@ -333,8 +333,8 @@ int sdattn_gated_norm(const void *x, const void *r, const void *gate, const void
  * Codes are rounded to nearest even: a value is off by at most 2^-4 of itself, or 2^(e - 10)
  * (once more for each time that its page is coded anew, where that takes it below 2^(e - 6)).  Finite values past 1.875 * 2^15
  * (fp16) or 1.875 * 2^127 (bf16) are held as that; NaN and infinities come back as NaN and do not count for
- * the scale.  A page that is written belongs to one item: two that write to the same page in one call
- * leave it unspecified.
+ * the scale.  A page that is written to has one place in the table: a call that writes to it through two leaves it
+ * unspecified.
  *
  * sdattn_cache_read gives the values of positions starts[b] + l, l < counts[b], back in 16 bits
  * (zeros for what is not there); rows of k and v from counts[b] on are left as they were.
@@ -364,7 +364,8 @@ int sdattn_cache_read(const void *k_pages, const void *v_pages, const float *k_s
  *   hi = min(n, (floor(p / frame) + 1) * frame), or n with frame = 0;  lo = hi - window, or 0 with window = 0
  * it sees key j where j < hi, and j >= lo or j < sinks: everything up to the end of its frame of `frame`
  * tokens (1: up to itself; 0: the whole sequence), of that the last `window` keys (0: all) and
- * the first `sinks`.  Keys that it does not see have no influence, whatever their values.
+ * the first `sinks`.  Keys that it does not see have no influence, whatever their values; of those that it
+ * sees, a value of V that is infinite or no number makes that of its own column, one of K a row of no numbers.
  *
  *   q, out  token rows of H heads of D values in `x_layout` and `y_layout`, [B, Lq tokens]; rows from
  *           counts[b] on are left as they were

@@ -68,14 +68,50 @@ __device__ __forceinline__ void span_hide(f32x16& st, uint32_t seen) {
     }
 }
 
-// whether any of 8 16-bit values is infinite or no number
+// The bits of those 16-bit values of two that are infinite or no number.
 template <int ET>
-__device__ __forceinline__ bool bad8(u32x4 w) {
+__device__ __forceinline__ uint32_t bad2(uint32_t w) {
     constexpr uint32_t kInf = ET == kF16 ? 0x7c00u : 0x7f80u;
-    bool bad = false;
+    return ((w & kInf) == kInf ? 0xffffu : 0u) | ((w & (kInf << 16)) == (kInf << 16) ? 0xffff0000u : 0u);
+}
+// The bits of those codes of four that are no number (0x7f and 0xff).
+__device__ __forceinline__ uint32_t bad_codes(uint32_t c) { return (((c & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 255u; }
+
+// Values of V that are no numbers, or infinite, are zeros in the products of a tile that not all queries see whole: a
+// weight of 0 would not keep them out.  For the queries that do see one, this adds it to the sums (acc as the
+// products leave it), at the end, where key by key costs no time that counts: `vt` is the tile's first row in memory,
+// `row` bytes from one to the next, `seen` this lane's keys of the 32.
+template <int ET, bool PAGED, int DN>
+__device__ __forceinline__ void span_add_bad(f32x16 (&acc)[DN], const char* vt, long long row, uint32_t seen, int D, int half) {
+    for (uint32_t left = seen; __any(left != 0); left &= left - 1) {
+        if (!left) continue;
+        const char* const v = vt + (__ffs((int)left) - 1) * row;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bad = bad || (w[i] & kInf) == kInf || (w[i] & (kInf << 16)) == (kInf << 16);
-    return bad;
+        for (int n = 0; n < DN; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int d = 32 * n + 8 * g + 4 * half;
+                if (d >= D) continue;
+                uint32_t w[2];
+                if constexpr (PAGED) {
+                    const uint32_t c = bad_codes(*(const uint32_t*)(v + d));   // (the type's no number is all ones too)
+                    w[0] = (c & 0xff ? 0xffffu : 0u) | (c & 0xff00 ? 0xffff0000u : 0u);
+                    w[1] = (c & 0xff0000 ? 0xffffu : 0u) | (c & 0xff000000u ? 0xffff0000u : 0u);
+                } else {
+                    const u32x2 x = *(const u32x2*)(v + 2 * d);
+                    w[0] = x[0] & bad2<ET>(x[0]), w[1] = x[1] & bad2<ET>(x[1]);
+                }
+                if (!(w[0] | w[1])) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x = to_float<ET>((uint16_t)(w[e >> 1] >> (16 * (e & 1))));
+                    computed_here(x);   // (this file's floats are taken for numbers: neither side of the sum is known to be one)
+                    x += acc[n][4 * g + e];
+                    computed_here(x);
+                    acc[n][4 * g + e] = x;
+                }
+            }
+    }
 }
 
 // ---------------------------------------------------------------- the tiled kernel
@@ -172,8 +208,8 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
 
     // this split's tiles
     const int per = (tiles.count + a.splits - 1) / a.splits;
-    int i = split * per;
-    const int i_end = min(i + per, tiles.count);
+    const int i_begin = split * per, i_end = min(i_begin + per, tiles.count);
+    int i = i_begin;
 
     // ---- tiles into LDS
     const uint32_t lds0 = lds_offset(smem);
@@ -307,22 +343,24 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
                     uint32_t lo4 = vraw[p][2 * e], hi4 = vraw[p][2 * e + 1];
                     if (end) {
                         const int r = place[p][e] / (KC * 16);
-                        // a code that is no number: 0x7f or 0xff
-                        const uint64_t w = lo4 | (uint64_t)hi4 << 32, n7 = (w & 0x7f7f7f7f7f7f7f7full) + 0x0101010101010101ull;
-                        const bool nan = (n7 & 0x8080808080808080ull) != 0;
-                        if (nan || x.t * TK + r >= seq.n) lo4 = hi4 = 0;
-                        if (nan) atomicOr((unsigned long long*)word, 1ull << r);
+                        const uint32_t lob = bad_codes(lo4), hib = bad_codes(hi4);
+                        if (lob | hib) atomicOr((unsigned long long*)word, 1ull << r);
+                        const bool past = x.t * TK + r >= seq.n;
+                        lo4 = past ? 0 : lo4 & ~lob;
+                        hi4 = past ? 0 : hi4 & ~hib;
                     }
                     *(u32x4*)(smem + (NKB + buf) * G::kTileBytes + place[p][e]) = decode8<ET>(lo4, hi4, x.vs);
                 }
         }
     };
-    // 16-bit tensors: chunks of V in an end tile that hold no number, as zeros, with their keys
+    // 16-bit tensors: values of V in an end tile that are no numbers, as zeros, with their keys
     auto scan = [&](int buf, uint64_t* word) __attribute__((always_inline)) {
         char* const vt = smem + (NKB + buf) * G::kTileBytes;
         for (int q = tid; q < TK * KC; q += G::kThreads) {
-            if (bad8<ET>(*(const u32x4*)(vt + q * 16))) {
-                *(u32x4*)(vt + q * 16) = u32x4{0u, 0u, 0u, 0u};
+            const u32x4 w = *(const u32x4*)(vt + q * 16);
+            const u32x4 b = {bad2<ET>(w[0]), bad2<ET>(w[1]), bad2<ET>(w[2]), bad2<ET>(w[3])};
+            if (b[0] | b[1] | b[2] | b[3]) {
+                *(u32x4*)(vt + q * 16) = w & ~b;
                 atomicOr((unsigned long long*)word, 1ull << (q / KC));
             }
         }
@@ -376,7 +414,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
     auto mask = [&](int x, int key0, const uint64_t* word) __attribute__((always_inline)) {
         const uint32_t seen = span_seen(key0, hi, lo, sinks);
         span_hide(st[x], seen >> (4 * half));
-        // a query that sees a key whose V is no number has no number to give
+        // a query that sees a key of which a V is no number
         if (seen & (uint32_t)(*word >> (key0 & 32))) spoiled = 1;
     };
     // m moved for st[x], where it has to be, and what that makes of the sums so far
@@ -532,8 +570,22 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
 #pragma unroll
         for (int h = 0; h < NP; ++h) o_mfma(1, h);
     }
+    if (__any(spoiled)) {
+        for (int at = i_begin; at < i_end; ++at) {
+            const int t = tiles.at(at);
+            if (block.has(t)) continue;   // (of these the values went into the products)
+            const char* vt = Vb + (long long)t * TK * row_bytes;
+            if constexpr (PAGED) {
+                const int page = a.table[(size_t)b * a.slots + t];
+                if (page < 0 || page >= a.pages) continue;
+                vt = a.v + ((size_t)page * a.Hk + hk) * TK * D;
+            }
+            const long long bytes = PAGED ? D : row_bytes;
+            for (int k = 0; k < TK; k += 32)
+                span_add_bad<ET, PAGED, DN>(acc, vt + k * bytes, bytes, span_seen(t * TK + k, hi, lo, sinks), D, half);
+        }
+    }
 
-    // (this file's floats are taken for numbers by the compiler: no number is made of bits)
     float sum;
     if constexpr (G::kOnes) {
         const float own = D == DP ? acc[DN - 1][8] : acc[DN - 1][4];   // column D, row 16 or 8 of the tile: lanes below 32
@@ -555,20 +607,19 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
         if (half == 0) {
             float* const ml = a.part + (size_t)a.splits * a.B * a.Hk * R * D + at * 2;
             ml[0] = m;
-            ((uint32_t*)ml)[1] = spoiled ? 0x7fc00000u : __float_as_uint(sum);
+            ml[1] = sum;
         }
         return;
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // 0 where no key is seen
-    const uint32_t nan = spoiled ? 0x7fff7fffu : 0u;     // (no number in both types)
     uint16_t* const o = a.out + b * a.ob + head * a.oh + token * a.ol;
 #pragma unroll
     for (int n = 0; n < DN; ++n)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
             if (32 * n + 8 * g < D)
-                *(u32x2*)(o + 32 * n + 8 * g + 4 * half) = u32x2{pack2<ET>(acc[n][4 * g] * inv, acc[n][4 * g + 1] * inv) | nan,
-                                                                pack2<ET>(acc[n][4 * g + 2] * inv, acc[n][4 * g + 3] * inv) | nan};
+                *(u32x2*)(o + 32 * n + 8 * g + 4 * half) = u32x2{pack2<ET>(acc[n][4 * g] * inv, acc[n][4 * g + 1] * inv),
+                                                                pack2<ET>(acc[n][4 * g + 2] * inv, acc[n][4 * g + 3] * inv)};
 }
 
 template <int ET, int DP, int NW, bool PAGED>

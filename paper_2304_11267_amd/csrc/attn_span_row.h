@@ -208,28 +208,30 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
                     hold[i >> 2][i & 3] = (seen >> k & 1 ? 0xffffu : 0u) | (seen >> k & 2 ? 0xffff0000u : 0u);
                 }
             } else {
-                // values that are no numbers as zeros, with their keys, and those of keys past the end
+                // values that are no numbers as zeros, and those of keys past the end; added afterwards where they are seen
                 uint32_t keys = 0;
                 char* const vt = (char*)kt + G::kCopies * 1024;
                 if constexpr (PAGED) {
                     for (int q = lane; q < G::kTileBytes / 8; q += 64) {
                         const int r = q / (D / 8);
-                        const uint64_t w = *(const uint64_t*)(vt + q * 8), n7 = (w & 0x7f7f7f7f7f7f7f7full) + 0x0101010101010101ull;
-                        const bool nan = (n7 & 0x8080808080808080ull) != 0;   // 0x7f or 0xff
-                        if (nan || key0 + r >= seq.n) *(uint64_t*)(vt + q * 8) = 0;
-                        if (nan) keys |= 1u << r;
+                        const u32x2 w = *(const u32x2*)(vt + q * 8), bad = {bad_codes(w[0]), bad_codes(w[1])};
+                        if (key0 + r >= seq.n) *(u32x2*)(vt + q * 8) = u32x2{0u, 0u};
+                        else if (bad[0] | bad[1]) *(u32x2*)(vt + q * 8) = w & ~bad;
+                        if (bad[0] | bad[1]) keys |= 1u << r;
                     }
                 } else {
                     for (int q = lane; q < G::kTileBytes / 16; q += 64) {
-                        if (bad8<ET>(*(const u32x4*)(vt + q * 16))) {
-                            *(u32x4*)(vt + q * 16) = u32x4{0u, 0u, 0u, 0u};
+                        const u32x4 w = *(const u32x4*)(vt + q * 16);
+                        const u32x4 bad = {bad2<ET>(w[0]), bad2<ET>(w[1]), bad2<ET>(w[2]), bad2<ET>(w[3])};
+                        if (bad[0] | bad[1] | bad[2] | bad[3]) {
+                            *(u32x4*)(vt + q * 16) = w & ~bad;
                             keys |= 1u << (q / G::KC);
                         }
                     }
                 }
 #pragma unroll
                 for (int o = 1; o < 64; o <<= 1) keys |= (uint32_t)__shfl_xor((int)keys, o, 64);
-                if (keys & seen) spoiled = 1;   // a query that sees one of them has no number to give
+                if (keys & seen) spoiled = 1;
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();
             }
@@ -314,6 +316,20 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
         });
     }
 
+    if (__any(spoiled)) {
+        for (int i = 0; i < mine; ++i) {
+            const int t = tile_of(i);
+            if (run.all(t * TK, TK)) continue;   // (of these the values went into the products)
+            const char* vt = a.v + 2 * (b * a.kb + hk * a.kh + (long long)t * TK * a.kl);
+            if constexpr (PAGED) {
+                const int page = a.table[(size_t)b * a.slots + t / (kCachePage / TK)];
+                if (page < 0 || page >= a.pages) continue;
+                vt = a.v + (((size_t)page * a.Hk + hk) * kCachePage + t % (kCachePage / TK) * TK) * D;
+            }
+            span_add_bad<ET, PAGED, DN>(acc, vt, PAGED ? D : 2 * a.kl, span_seen(t * TK, hi, lo, sinks), D, half);
+        }
+    }
+
     // ---- the waves' parts: O [row][D], then m, l
     constexpr int kO = D + 4;
     l = half_sum(l);
@@ -330,7 +346,6 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
         if (half == 0) {
             o[D] = m;
             o[D + 1] = l;
-            ((int*)o)[D + 2] = spoiled;
         }
     }
     __syncthreads();
@@ -340,7 +355,6 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
         if (r / a.G >= seq.count) break;   // (rows of later tokens follow)
         const float* const o = parts + r * kO;
         float top = kSpanNone, sum = 0.0f;
-        int bad = 0;
 #pragma unroll
         for (int w = 0; w < G::kWaves; ++w) top = fmaxf(top, o[w * kSpanRows * kO + D]);
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -349,7 +363,6 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             const float* const ow = o + w * kSpanRows * kO;
             const float f = fast_exp2(ow[D] - top);
             sum = fmaf(ow[D + 1], f, sum);
-            bad |= ((const int*)ow)[D + 2];
             const f32x4 x = *(const f32x4*)(ow + d);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], f, v[e]);
@@ -360,14 +373,13 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             if (d == 0) {
                 float* const ml = a.part + a.splits * rows * D + at * 2;
                 ml[0] = top;
-                ((uint32_t*)ml)[1] = bad ? 0x7fc00000u : __float_as_uint(sum);
+                ml[1] = sum;
             }
         } else {
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            const uint32_t nan = bad ? 0x7fff7fffu : 0u;
             const int tk = r / a.G;
             *(u32x2*)(a.out + b * a.ob + (hk * a.G + r - tk * a.G) * a.oh + tk * a.ol + d) =
-                u32x2{pack2<ET>(v[0] * inv, v[1] * inv) | nan, pack2<ET>(v[2] * inv, v[3] * inv) | nan};
+                u32x2{pack2<ET>(v[0] * inv, v[1] * inv), pack2<ET>(v[2] * inv, v[3] * inv)};
         }
     }
 }

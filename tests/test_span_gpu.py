@@ -226,6 +226,59 @@ def test_no_numbers_where_nothing_is_seen(what, Lq):
             assert not torch.isfinite(a[:, :, first:, 3]).any()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [40, 64, 128, 136])
+@pytest.mark.parametrize("Lq", [1, 7, 150, 260])
+def test_infinite_values_and_no_numbers_reach_their_columns(Lq, D, dtype):
+    """A value of V that is no number, or infinite, makes that of its column for the queries that see it: what else
+    they give, and what the others give, is as with a zero there."""
+    import torch
+    Lk, H = 260, 2
+    inf, nan = float("inf"), float("nan")
+    # (key, column, value): two infinities of one column meet at key 258
+    odd = [(30, 3, inf), (130, 3, inf), (131, 8, -inf), (200, 8, -inf), (129, 17, nan), (210, D - 1, inf), (255, 9, inf), (258, 9, -inf)]
+    for rule in ((1, 0, 0), (1, 64, 0), (1, 40, 31), (0, 100, 33)):
+        def own(q, k, v):
+            for key, col, x in odd:
+                v[:, :, key, col] = x
+
+        def none(q, k, v):
+            for key, col, x in odd:
+                v[:, :, key, col] = 0
+        got = window(1, H, 1, Lq, Lk, D, *rule, dtype=dtype, tweak=own, check=False).float()
+        want = window(1, H, 1, Lq, Lk, D, *rule, dtype=dtype, tweak=none, check=False).float()
+        see = torch.from_numpy(ref.seen([Lk - Lq], [Lq], Lq, Lk, *rule)[0]).cuda()
+        for key, col, x in odd:
+            want[:, :, see[:, key], col] += x
+        assert torch.equal(torch.nan_to_num(got, 1e5, 2e5, -2e5), torch.nan_to_num(want, 1e5, 2e5, -2e5)), rule
+
+
+@pytest.mark.parametrize("Lq", [1, 7, 150])
+def test_codes_of_no_numbers_reach_their_columns(Lq):
+    """As above, for a cache, in which infinities are no numbers."""
+    import torch
+    n, H, D, dtype = 260, 2, 64, "bf16"
+    odd = [(30, 3), (130, 3), (131, 8), (200, 8), (129, 17), (210, 63), (258, 9)]
+    g = op.generator(4)
+    k, v, q = (op.randn(g, 1, h, l, D, dtype=dtype) for h, l in ((1, n), (1, n), (H, Lq)))
+    k[:], table = 0.5 * k, i32([[2, 0, 3, 1, 4]])
+    for rule in ((1, 0, 0), (1, 64, 0), (1, 40, 31), (0, 100, 33)):
+        outs = []
+        for x in (0.0, float("nan")):
+            for key, col in odd:
+                v[:, :, key, col] = x
+            c = [torch.zeros(5, 1, 64, D, dtype=torch.uint8, device="cuda") for _ in range(2)]
+            c += [torch.ones(5, 1, device="cuda") for _ in range(2)]
+            sd.cache_write(k, v, *c, table, i32([0]))
+            ws = torch.empty(max(16, sd.cache_forward_workspace(1, H, 1, Lq, D, 5, *rule)), dtype=torch.uint8, device="cuda")
+            outs.append(sd.cache_forward(q, *c, table, i32([n - Lq]), torch.empty_like(q), 0.125, H, workspace=ws, frame=rule[0],
+                                         window=rule[1], sinks=rule[2]).float())
+        see = torch.from_numpy(ref.seen([n - Lq], [Lq], Lq, n, *rule)[0]).cuda()
+        for key, col in odd:
+            outs[0][:, :, see[:, key], col] = float("nan")
+        assert torch.equal(torch.nan_to_num(outs[1], 1e5), torch.nan_to_num(outs[0], 1e5)), rule
+
+
 def test_no_numbers_in_the_cache():
     """A token of no numbers in the cache: rows before it as without it, and a window leaves it behind."""
     import torch
