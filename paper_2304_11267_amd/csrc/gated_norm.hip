@@ -5,8 +5,8 @@
 // gamma + beta (population variance), over a token's C channels; gate, scale and shift one
 // vector for each group of tokens.
 //
-// Its bound is memory: x and r read once, h and y written once.  A token belongs to one wave,
-// or to a workgroup of four where tokens are few or wide, and stays in registers
+// Its bound is memory: x and r read once, h and y written once.  A token belongs to a run
+// of 8 to 64 lanes, or to a workgroup of four waves where tokens are few or wide, and stays in registers
 // from the reads to the writes; sums are fp32, of deviations from the mean where there is one,
 // and each output is rounded once.
 #include "device.h"
@@ -42,14 +42,16 @@ template <int CTRL>
 __device__ __forceinline__ float gn_moved(float v) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
 }
-// sum over a wave, in every lane
-__device__ __forceinline__ float gn_wave_sum(float v) {
+// sum over each run of LANES (8 to 64), in every lane of it
+template <int LANES>
+__device__ __forceinline__ float gn_lane_sum(float v) {
     v += gn_moved<0xb1>(v);
     v += gn_moved<0x4e>(v);
     v += gn_moved<0x141>(v);
-    v += gn_moved<0x140>(v);
-    v += __shfl_xor(v, 16, 64);
-    return half_sum(v);
+    if constexpr (LANES > 8) v += gn_moved<0x140>(v);
+    if constexpr (LANES > 16) v += __shfl_xor(v, 16, 64);
+    if constexpr (LANES > 32) v = half_sum(v);
+    return v;
 }
 
 template <int ET>
@@ -65,17 +67,20 @@ __device__ __forceinline__ void gn_widen(u32x4 w, float* f) {
 template <int ET, bool WIDE, int TEAM, int CH>
 __global__ __launch_bounds__(kGnThreads) void gated_norm_kernel(const GatedKernel a) {
     constexpr int kTeams = kGnThreads / TEAM;
+    constexpr bool kEarly = CH <= 2;   // the vectors have registers of their own from the start
     __shared__ float sums[2][kGnThreads / 64];
     const int t = threadIdx.x % TEAM;
-    const int m = blockIdx.x * kTeams + (TEAM == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : 0);
+    int m = blockIdx.x * kTeams + threadIdx.x / TEAM;
+    if (TEAM >= 64) m = __builtin_amdgcn_readfirstlane(m);
     if (m >= a.M) return;   // (teams of four waves: never)
     const int C = a.C, pieces = C / 8;
     const int b = m / a.L, g = (m - b * a.L) / a.per_group;
     const long long mod = (long long)b * a.mod_batch + g;
+    const size_t row = (size_t)m * C;
 
     int turn = 0;
     auto team_sum = [&](float v) __attribute__((always_inline)) {
-        v = gn_wave_sum(v);
+        v = gn_lane_sum<(TEAM > 64 ? 64 : TEAM)>(v);
         if constexpr (TEAM > 64) {
             if (threadIdx.x % 64 == 0) sums[turn][threadIdx.x / 64] = v;
             __syncthreads();
@@ -114,52 +119,76 @@ __global__ __launch_bounds__(kGnThreads) void gated_norm_kernel(const GatedKerne
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[i][e] *= rstd;
     };
-    // f = op(f, v) for a vector v of channels, in every piece of this thread
-    auto with = [&](float (&f)[CH][8], const uint16_t* v, auto op) __attribute__((always_inline)) {
+    // this thread's pieces of 16-bit values at v
+    auto fetch = [&](u32x4 (&w)[CH], const uint16_t* v) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int c = i * TEAM + t;
-            if (c >= pieces) continue;
+            w[i] = u32x4{0u, 0u, 0u, 0u};
+            if (c < pieces) w[i] = *(const u32x4*)(v + c * 8);
+        }
+    };
+    // the vectors of channels that this call has
+    enum { kGammaR, kGate, kGamma, kBeta, kScale, kShift, kVectors };
+    const bool pre = a.pre != kNormNone;
+    const uint16_t* const at[kVectors] = {a.r && a.post != kNormNone ? a.gamma_r : nullptr, a.r && a.gate ? a.gate + mod * a.sg : nullptr,
+                                          a.y && pre ? a.gamma : nullptr, a.y && pre ? a.beta : nullptr,
+                                          a.y && a.scale ? a.scale + mod * a.ss : nullptr, a.y && a.shift ? a.shift + mod * a.st : nullptr};
+    u32x4 early[kEarly ? (int)kVectors : 1][CH];
+    // f = op(f, vector) in every piece of this thread
+    auto with = [&](float (&f)[CH][8], int n, auto op) __attribute__((always_inline)) {
+        if (!at[n]) return;
+        if constexpr (!kEarly) fetch(early[0], at[n]);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
             float w[8];
-            gn_widen<ET>(*(const u32x4*)(v + c * 8), w);
+            gn_widen<ET>(early[kEarly ? n : 0][i], w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[i][e] = op(f[i][e], w[e]);
         }
     };
+    const auto times = [](float v, float w) { return v * w; };
+    const auto plus = [](float v, float w) { return v + w; };
+
+    // everything on its way
+    u32x4 rw[CH], xw[WIDE ? 2 : 1][CH];
+    if (a.r) fetch(rw, a.r + row);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = i * TEAM + t;
+#pragma unroll
+        for (int k = 0; k < (WIDE ? 2 : 1); ++k) {
+            xw[k][i] = u32x4{0u, 0u, 0u, 0u};
+            if (c < pieces) xw[k][i] = *(const u32x4*)((const char*)a.x + (row + c * 8) * (WIDE ? 4 : 2) + 16 * k);
+        }
+    }
+    if constexpr (kEarly) {
+#pragma unroll
+        for (int n = 0; n < kVectors; ++n)
+            if (at[n]) fetch(early[n], at[n]);
+    }
 
     float f[CH][8];
-    const size_t row = (size_t)m * C;
     if (a.r) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int c = i * TEAM + t;
-            u32x4 w = {0u, 0u, 0u, 0u};
-            if (c < pieces) w = *(const u32x4*)(a.r + row + c * 8);
-            gn_widen<ET>(w, f[i]);
-        }
+        for (int i = 0; i < CH; ++i) gn_widen<ET>(rw[i], f[i]);
         normed(f, a.post);
-        if (a.post != kNormNone && a.gamma_r) with(f, a.gamma_r, [](float v, float g) { return v * g; });
-        if (a.gate) with(f, a.gate + mod * a.sg, [](float v, float g) { return v * g; });
+        with(f, kGammaR, times);
+        with(f, kGate, times);
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = i * TEAM + t;
         float w[8];
-        if (c >= pieces) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[i][e] = 0.0f;
-            continue;
-        }
         if constexpr (WIDE) {
-            const f32x4 lo = *(const f32x4*)((const float*)a.x + row + c * 8), hi = *(const f32x4*)((const float*)a.x + row + c * 8 + 4);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = lo[e], w[4 + e] = hi[e];
+            for (int e = 0; e < 8; ++e) w[e] = __uint_as_float(xw[e / 4][i][e % 4]);
         } else {
-            gn_widen<ET>(*(const u32x4*)((const uint16_t*)a.x + row + c * 8), w);
+            gn_widen<ET>(xw[0][i], w);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[i][e] = a.r ? fmaf(a.skip, w[e], f[i][e]) : a.skip * w[e];
-        if (a.h) {
+        if (a.h && c < pieces) {
             if constexpr (WIDE) {
                 *(f32x4*)((float*)a.h + row + c * 8) = f32x4{f[i][0], f[i][1], f[i][2], f[i][3]};
                 *(f32x4*)((float*)a.h + row + c * 8 + 4) = f32x4{f[i][4], f[i][5], f[i][6], f[i][7]};
@@ -168,15 +197,17 @@ __global__ __launch_bounds__(kGnThreads) void gated_norm_kernel(const GatedKerne
                                                                 pack2<ET>(f[i][4], f[i][5]), pack2<ET>(f[i][6], f[i][7])};
             }
         }
+        if (c >= pieces) {   // (a norm without a number, times a zero)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[i][e] = 0.0f;
+        }
     }
     if (!a.y) return;
     normed(f, a.pre);
-    if (a.pre != kNormNone) {
-        if (a.gamma) with(f, a.gamma, [](float v, float g) { return v * g; });
-        if (a.beta) with(f, a.beta, [](float v, float g) { return v + g; });
-    }
-    if (a.scale) with(f, a.scale + mod * a.ss, [](float v, float g) { return fmaf(v, g, v); });
-    if (a.shift) with(f, a.shift + mod * a.st, [](float v, float g) { return v + g; });
+    with(f, kGamma, times);
+    with(f, kBeta, plus);
+    with(f, kScale, [](float v, float w) { return fmaf(v, w, v); });
+    with(f, kShift, plus);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = i * TEAM + t;
@@ -196,8 +227,13 @@ hipError_t gated_launch(const GatedKernel& a, void* stream) {
 
 template <int ET, bool WIDE>
 hipError_t gated_pick(const GatedKernel& a, void* stream) {
-    // Many tokens: a wave each; few or wide ones: a workgroup each.
+    // A piece a thread and as many threads as there are pieces, down to 8 (16000 tokens of 64 channels 9.8 us with a wave
+    // each, 4.7; 16384 of 160 10.6, 7.1, 16 threads with two pieces 7.3); past 64 a wave with more
+    // where tokens are many, else four waves (512 tokens of 1280 5.4 us, 4.5).
     const int pieces = a.C / 8;
+    if (pieces <= 8) return gated_launch<ET, WIDE, 8, 1>(a, stream);
+    if (pieces <= 16) return gated_launch<ET, WIDE, 16, 1>(a, stream);
+    if (pieces <= 32) return gated_launch<ET, WIDE, 32, 1>(a, stream);
     if (pieces <= 64) return gated_launch<ET, WIDE, 64, 1>(a, stream);
     if (a.M >= 1024) {
         if (pieces <= 128) return gated_launch<ET, WIDE, 64, 2>(a, stream);

@@ -92,6 +92,15 @@ def test_widths(C, M):
     check(inputs(*M, C, dtype="bf16", wide=C % 16 == 0), "rms", "layer", 1.0, "bf16")
 
 
+@pytest.mark.parametrize("C", [24, 64, 72, 128, 136, 160, 256, 264, 320])
+@pytest.mark.parametrize("M,groups", [((1, 1), 1), ((3, 21), 7), ((2, 1100), 2)])
+def test_narrow_tokens(C, M, groups):
+    """Several tokens a wave, of different groups and batch items."""
+    for dtype, wide, norm_r in (("f16", False, "layer"), ("bf16", True, "rms")):
+        t = inputs(*M, C, groups=groups, dtype=dtype, wide=wide)
+        check(t, norm_r, "layer", 0.75, dtype)
+
+
 @pytest.mark.parametrize("missing", ["r", "gate", "scale", "shift", "gamma_r", "gamma", "beta", "all"])
 def test_missing_parts(missing):
     t = inputs(2, 4, 320, 2)
