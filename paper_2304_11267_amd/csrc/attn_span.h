@@ -116,7 +116,7 @@ __device__ __forceinline__ void span_add_bad(f32x16 (&acc)[DN], const char* vt, 
 
 // ---------------------------------------------------------------- the tiled kernel
 
-// Workgroups of NW waves of 32 rows: four, and two workgroups a CU, whose waves share the SIMDs without waiting for
+// Workgroups of NW waves of 32 rows: four, and two or three workgroups a CU, whose waves share the SIMDs without waiting for
 // each other at barriers (eight waves of one workgroup, D = 128: one of a SIMD's two ends its tile first, and the
 // other's products then have no exponentials beside them); eight past D = 128, where registers and LDS leave no room for that.  K and V tiles
 // of 64 keys lie as 16-bit values in LDS buffers, two or three of K and two of V, rows of DP values whose 16-byte chunks are permuted
@@ -134,6 +134,11 @@ __device__ __forceinline__ void span_add_bad(f32x16 (&acc)[DN], const char* vt, 
 // reaches 1300.  4096 tokens of D = 40, windows of 1024 and 77: 29.6 us; a tile takes 1.1 us of it on two
 // workgroups of a CU, of which the products alone are 0.58, the exponentials and sums 0.3 to 0.4, copies and LDS reads
 // the rest.  Pages, 1350 tokens over 6750 keys, D = 128: 136 us and a join of 7.6.
+
+// Waves of a SIMD that the registers are cut for: three where that costs none (D = 40 in pages, 2665 tokens of 16 sequences
+// 99 -> 83 us; D = 64, 64 heads of 4096 tokens 370 -> 345; 64 in pages spills, 99 -> 101).
+constexpr int span_waves(int DP, bool paged) { return DP <= 48 || (DP == 64 && !paged) ? 3 : 2; }
+
 template <int DP, int NW>
 struct SpanTile {
     static constexpr int kThreads = 64 * NW, kRows = 32 * NW;
@@ -167,7 +172,7 @@ __device__ __forceinline__ SpanWhole span_whole(const SpanRun& r) {
 }
 
 template <int ET, int DP, int NW, bool PAGED>
-__global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_kernel(const SpanKernel a) {
+__global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)) void span_tile_kernel(const SpanKernel a) {
     using G = SpanTile<DP, NW>;
     constexpr int DK = G::DK, DN = G::DN, KC = G::KC, TK = kSpanTile, NKB = G::kBufsK;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -350,8 +355,8 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), 2) void span_tile_ker
                     if (end) {
                         const int r = place[p][e] / (KC * 16);
                         const uint32_t lob = bad_codes(lo4), hib = bad_codes(hi4);
-                        if (lob | hib) atomicOr((unsigned long long*)word, 1ull << r);
-                        const bool past = x.t * TK + r >= seq.n;
+                        const bool past = x.t * TK + r >= seq.n;   // (whatever the page holds there; nobody sees it)
+                        if ((lob | hib) && !past) atomicOr((unsigned long long*)word, 1ull << r);
                         lo4 = past ? 0 : lo4 & ~lob;
                         hi4 = past ? 0 : hi4 & ~hib;
                     }

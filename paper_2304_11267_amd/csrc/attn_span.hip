@@ -1,5 +1,7 @@
 // attn_span.hip -- how a call of attn_span.h is cut up, its entry point, and the join of the
 // parts of its keys.
+#include <cmath>
+
 #include "attn_geom.h"
 #include "attn_span_seq.h"
 
@@ -129,6 +131,31 @@ static hipError_t launch_span_join(const SpanKernel& a, int type, hipStream_t st
     return hipGetLastError();
 }
 
+// In how many parts a block's keys are cheapest, by the time of a part's tiles one after another and of the join: 4.5 us
+// for its launch, and each part's rows through memory.  A tile's time, in us: for few rows its bytes at what one CU reads
+// alone, 50 KB a us, and 0.12 at least; else what a workgroup of few takes (paged, D = 128 1.6 to 2.3; 16-bit, D = 128 / 64 / 40
+// 1.3 / 0.94 / 0.8), or 1.6 times that where two share a CU.
+static int span_parts(const SpanArgs& a, bool single, int block, long long tiles, long long wgs, long long rows) {
+    const double tile = single ? fmax(32.0 * 2 * a.D * (a.slots > 0 ? 1 : 2) / 50e3, 0.12)
+                      : block == 256 ? 1.0 + 0.01 * a.D : (0.55 + 0.006 * a.D) * (a.slots > 0 ? 1.25 : 1.0);
+    const double part = (double)rows * a.D * 8 / 4e6 + 0.1;
+    const long long most = tiles / (single ? 4 : 2);
+    int best = 1;
+    double least = (double)tiles * tile * (!single && block == 128 && wgs > kCus ? 1.6 : 1.0);
+    auto consider = [&](long long room, double slower) {
+        const double ideal = sqrt((double)tiles * tile * slower / part);
+        long long s = single ? (room + wgs / 2) / wgs : room / wgs;
+        if (s > most) s = most;
+        if ((double)s > ideal) s = (long long)ideal;
+        if (s < 2) return;
+        const double t = (double)((tiles + s - 1) / s) * tile * slower + 4.5 + (double)s * part;
+        if (t < least) least = t, best = (int)s;
+    };
+    consider(kCus, 1.0);
+    if (!single && block == 128) consider(2 * kCus, 1.6);
+    return best;
+}
+
 SpanPlan span_plan(const SpanArgs& a) {
     SpanPlan p{};
     const int G = a.H / a.Hk;
@@ -145,15 +172,7 @@ SpanPlan span_plan(const SpanArgs& a) {
         const long long seen = ((long long)a.sinks + tile - 1) / tile + ((long long)a.window + spread) / tile + 2;
         if (seen < tiles) tiles = seen;
     }
-    // Parts, so that there are as many workgroups as the card holds at once.  Joining them costs a launch: with few rows
-    // four us, so from 48 tiles on, and eight at least a part.  (us; none, parts of 4 / 8 / 16 / 32 tiles: 16 heads over 2048
-    // keys D = 64 10.4, 8.5 / 9.6 / 10.3 / 12.1; 4096 16.3, 11.9 / 9.7 / 10.6 / 11.9; 8192 D = 128 55.9, 20.3 / 20.3 / 17.0 / 17.6;
-    // 64 windows of 35 tiles 7.9, 15.4 / 9.9 / 11.2; 256 or 512 workgroups: 128 heads over 4096 keys in pages, D = 80 22.6 /
-    // 27.5, 8 over 32768 D = 128 19.7 / 23.6, 64 of 11000 to 32768 80.6 / 78.0.)
-    const long long most = p.single && tiles < 48 ? 1 : tiles / 8, room = p.single || block == 256 ? kCus : 2 * kCus;
-    const long long enough = p.single ? (room + wgs / 2) / wgs : room / wgs;
-    p.splits = (int)(enough < most ? enough : most);
-    if (p.splits < 1) p.splits = 1;
+    p.splits = span_parts(a, p.single, block, tiles, wgs, rows * heads);
     if (p.splits > 1) {
         const __int128 bytes = (__int128)p.splits * heads * rows * (a.D + 2) * 4;
         p.workspace = bytes < ((__int128)1 << 62) ? (long long)bytes : -1;

@@ -409,3 +409,22 @@ def test_another_stream_and_native_marshalling(monkeypatch):
     c = [window(2, 4, 2, Lq, 3000, 64, 1, 2000, 7) for Lq in (1, 90)]
     c1 = [cached(2, 4, 2, Lq, 64, 2900, 1, 2000, 7) for Lq in (1, 90)]
     assert all(torch.equal(p, q) and torch.equal(p, r) for p, q, r in zip(a, b, c)) and all(torch.equal(p, q) for p, q in zip(c0, c1))
+
+
+@pytest.mark.parametrize("D", [40, 64, 128, 160])
+def test_few_tiles_in_parts(D):
+    """Few blocks of rows over few tiles, in parts of two or three; one token over wide heads, whose parts are short."""
+    for dtype, rule in (("f16", (1, 0, 0)), ("bf16", (1, 150, 70)), ("f16", (0, 0, 0)), ("bf16", (100, 300, 0))):
+        window(1, 2, 1, 310, 863, D, *rule, dtype=dtype)
+        cached(1, 2, 1, 310, D, 553, *rule, dtype=dtype)
+        window(1, 4, 1, 1, 1389, D, *rule, dtype=dtype)
+        cached(2, 4, 1, 1, D, 1388, *rule, dtype=dtype, starts=[1388, 3])
+
+
+def test_what_a_page_holds_behind_the_sequence():
+    """Codes that are no numbers, or large ones, behind the last token: the same bits."""
+    import torch
+    for Lq in (1, 9, 70):
+        for D in (40, 128):
+            a, b = (cached(2, 8, 2, Lq, D, 3, spoil=s) for s in (True, False))
+            assert torch.equal(a, b)
