@@ -131,40 +131,22 @@ static hipError_t launch_span_join(const SpanKernel& a, int type, hipStream_t st
     return hipGetLastError();
 }
 
-// In how many parts a block's keys are cheapest, by the time of a part's tiles one after another and of the join: 4.5 us
-// for its launch, and each part's rows through memory.  A tile's time, in us: for few rows its bytes at what one CU reads
-// alone, 50 KB a us, and 0.12 at least; else what a workgroup of few takes (paged, D = 128 1.6 to 2.3; 16-bit, D = 128 / 64 / 40
-// 1.3 / 0.94 / 0.8), or 1.6 times that where two share a CU.
-static int span_parts(const SpanArgs& a, bool single, int block, long long tiles, long long wgs, long long rows) {
-    const double tile = single ? fmax(32.0 * 2 * a.D * (a.slots > 0 ? 1 : 2) / 50e3, 0.12)
-                      : block == 256 ? 1.0 + 0.01 * a.D : (0.55 + 0.006 * a.D) * (a.slots > 0 ? 1.25 : 1.0);
-    const double part = (double)rows * a.D * 8 / 4e6 + 0.1;
-    const long long most = tiles / (single ? 4 : 2);
-    int best = 1;
-    double least = (double)tiles * tile * (!single && block == 128 && wgs > kCus ? 1.6 : 1.0);
-    auto consider = [&](long long room, double slower) {
-        const double ideal = sqrt((double)tiles * tile * slower / part);
-        long long s = single ? (room + wgs / 2) / wgs : room / wgs;
-        if (s > most) s = most;
-        if ((double)s > ideal) s = (long long)ideal;
-        if (s < 2) return;
-        const double t = (double)((tiles + s - 1) / s) * tile * slower + 4.5 + (double)s * part;
-        if (t < least) least = t, best = (int)s;
-    };
-    consider(kCus, 1.0);
-    if (!single && block == 128) consider(2 * kCus, 1.6);
-    return best;
-}
+// A way to cut a call up, and the time that it is taken for, in us.
+struct SpanWay {
+    int row_blocks, splits;
+    double time;
+};
 
-SpanPlan span_plan(const SpanArgs& a) {
-    SpanPlan p{};
+// By the time of a part's tiles one after another and of the join: 4.5 us for its launch, and each part's rows through
+// memory.  A tile's time, in us: for few rows its bytes at what one CU reads alone, 50 KB a us, and 0.12 at least; else
+// what a workgroup of few takes (paged, D = 128 1.6 to 2.3; 16-bit, D = 128 / 64 / 40 1.3 / 0.94 / 0.8),
+// or 1.6 times that where two share a CU.
+static SpanWay span_way(const SpanArgs& a, bool single) {
     const int G = a.H / a.Hk;
-    const long long rows = (long long)a.Lq * G;
-    p.single = rows <= kSpanRows;
-    const long long heads = (long long)a.B * a.Hk;
-    const int block = p.single ? kSpanRows : span_block((a.D + 15) / 16 * 16, a.slots > 0), tile = p.single ? 32 : 64;
-    p.row_blocks = (int)((rows + block - 1) / block);
-    const long long wgs = heads * p.row_blocks;
+    const long long rows = (long long)a.Lq * G, heads = (long long)a.B * a.Hk;
+    const int block = single ? kSpanRows : span_block((a.D + 15) / 16 * 16, a.slots > 0), tile = single ? 32 : 64;
+    SpanWay w{(int)((rows + block - 1) / block), 1, 0.0};
+    const long long wgs = heads * w.row_blocks;
     // the most tiles that a block can see
     long long tiles = ((long long)a.Lk + tile - 1) / tile;
     if (a.window > 0) {
@@ -172,7 +154,40 @@ SpanPlan span_plan(const SpanArgs& a) {
         const long long seen = ((long long)a.sinks + tile - 1) / tile + ((long long)a.window + spread) / tile + 2;
         if (seen < tiles) tiles = seen;
     }
-    p.splits = span_parts(a, p.single, block, tiles, wgs, rows * heads);
+    const double cost = single ? fmax(32.0 * 2 * a.D * (a.slots > 0 ? 1 : 2) / 50e3, 0.12)
+                      : block == 256 ? 1.0 + 0.01 * a.D : (0.55 + 0.006 * a.D) * (a.slots > 0 ? 1.25 : 1.0);
+    const double part = (double)rows * heads * a.D * 8 / 4e6 + 0.1;
+    const bool pairs = !single && block == 128;   // two workgroups a CU
+    const long long most = tiles / (single ? 4 : 2);
+    auto rounds = [&](long long room) { return (double)((wgs + room - 1) / room); };
+    w.time = pairs && wgs > kCus ? rounds(2 * kCus) * (double)tiles * cost * 1.6 : rounds(kCus) * (double)tiles * cost;
+    auto consider = [&](long long room, double slower) {
+        const double ideal = sqrt((double)tiles * cost * slower / part);
+        long long s = single ? (room + wgs / 2) / wgs : room / wgs;
+        if (s > most) s = most;
+        if ((double)s > ideal) s = (long long)ideal;
+        if (s < 2) return;
+        const double t = (double)((tiles + s - 1) / s) * cost * slower + 4.5 + (double)s * part;
+        if (t < w.time) w.time = t, w.splits = (int)s;
+    };
+    consider(kCus, 1.0);
+    if (pairs) consider(2 * kCus, 1.6);
+    return w;
+}
+
+SpanPlan span_plan(const SpanArgs& a) {
+    const long long rows = (long long)a.Lq * (a.H / a.Hk), heads = (long long)a.B * a.Hk;
+    SpanPlan p{};
+    SpanWay w = span_way(a, true);
+    p.single = true;
+    if (rows > kSpanRows) {
+        // Blocks of 32 rows whose eight waves share out the keys, where there is a CU for each (110 calls drawn at random, at
+        // most 3000 such blocks: 13.7 us in the geometric mean, 16.0 tiled; where there are up to 512 blocks 14.0, all 16.7; 754 tokens of
+        // 8 heads D = 80, windows of 162, 19.5 -> 9.0; 29 tokens of two heads 7.6 -> 8.4).
+        const SpanWay tiled = span_way(a, false);
+        if (heads * w.row_blocks > kCus || tiled.time < w.time) w = tiled, p.single = false;
+    }
+    p.row_blocks = w.row_blocks, p.splits = w.splits;
     if (p.splits > 1) {
         const __int128 bytes = (__int128)p.splits * heads * rows * (a.D + 2) * 4;
         p.workspace = bytes < ((__int128)1 << 62) ? (long long)bytes : -1;

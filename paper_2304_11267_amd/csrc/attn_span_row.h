@@ -1,8 +1,8 @@
-// attn_span_row.h -- the attention of attn_span.h for at most 32 rows of a key head (the query heads of one
-// new token, or of a few).
+// attn_span_row.h -- the attention of attn_span.h in blocks of at most 32 rows of a key head (the query heads of one
+// new token, or of a few), for calls that have a CU for each block.
 //
-// What counts is reading the visible keys and values once.  A workgroup takes one (batch item, key head), or a
-// part of its keys, and each of its waves every fourth tile of 32 of them, through a ring of LDS buffers
+// What counts is reading the visible keys and values once.  A workgroup takes one block, or a
+// part of its keys, and each of its waves every eighth tile of 32 of them (wide heads: every fourth or third), through a ring of LDS buffers
 // of its own: direct global->LDS copies of the tiles to come are in flight while one is used, and no
 // wave waits for another before the end.  The page and the scales of a wave's tiles lie in its
 // lanes, 64 tiles at a time.  Codes stay codes in LDS; a lane turns the 8 that it needs for a matrix product
@@ -64,12 +64,15 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
     const int lane = lane_id(), l32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-    const int split = blockIdx.x % a.splits;
-    const int bh = blockIdx.x / a.splits, b = bh / a.Hk, hk = bh - b * a.Hk;
+    // (blocks of one head on one XCD, whose L2 they share)
+    const int item = a.row_blocks > 1 ? xcd_remap(blockIdx.x, gridDim.x) : (int)blockIdx.x, list = item / a.splits;
+    const int split = item - list * a.splits;
+    const int bh = list / a.row_blocks, b = bh / a.Hk, hk = bh - b * a.Hk;
     const SpanSeq seq = span_seq(a, b);
-    if (seq.count == 0) return;
-    const int R = a.Lq * a.G;
-    const int row = min(l32, R - 1);
+    const int R = a.Lq * a.G, r0 = (list - bh * a.row_blocks) * kSpanRows;
+    const int token0 = r0 / a.G, token1 = min(min(r0 + kSpanRows - 1, R - 1) / a.G, seq.count - 1);
+    if (token0 >= seq.count) return;
+    const int row = min(r0 + l32, R - 1);
     const int token = min(row / a.G, seq.count - 1), head = hk * a.G + row % a.G;
 
     u32x4 qreg[DK];
@@ -83,8 +86,8 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
         qreg[s] = w;
     }
 
-    const SpanTiles tiles = span_tiles(a, seq, 0, seq.count - 1, TK);
-    const SpanRun run = span_run(a, seq, 0, seq.count - 1);
+    const SpanTiles tiles = span_tiles(a, seq, token0, token1, TK);
+    const SpanRun run = span_run(a, seq, token0, token1);
     const int hi = span_hi(a, seq, token), lo = span_lo(a, hi), sinks = a.sinks;
     // this split's tiles, and of these every kWaves-th
     const int per = (tiles.count + a.splits - 1) / a.splits;
@@ -338,7 +341,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
     l = half_sum(l);
     __syncthreads();   // every wave is done with its buffers
     float* const parts = (float*)smem;
-    if (l32 < R) {
+    if (r0 + l32 < R) {
         float* const o = parts + (wave * kSpanRows + l32) * kO;
 #pragma unroll
         for (int n = 0; n < DN; ++n)
@@ -353,9 +356,9 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
     }
     __syncthreads();
     const size_t rows = (size_t)a.B * a.Hk * R;
-    for (int z = tid; z < R * (D / 4); z += G::kThreads) {
-        const int r = z / (D / 4), d = (z - r * (D / 4)) * 4;
-        if (r / a.G >= seq.count) break;   // (rows of later tokens follow)
+    for (int z = tid; z < min(R - r0, kSpanRows) * (D / 4); z += G::kThreads) {
+        const int r = z / (D / 4), d = (z - r * (D / 4)) * 4, tk = (r0 + r) / a.G;
+        if (tk >= seq.count) break;   // (rows of later tokens follow)
         const float* const o = parts + r * kO;
         float top = kSpanNone, sum = 0.0f;
 #pragma unroll
@@ -371,7 +374,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], f, v[e]);
         }
         if (a.splits > 1) {
-            const size_t at = (split * rows + (size_t)bh * R + r);
+            const size_t at = (split * rows + (size_t)bh * R + r0 + r);
             *(f32x4*)(a.part + at * D + d) = v;
             if (d == 0) {
                 float* const ml = a.part + a.splits * rows * D + at * 2;
@@ -380,8 +383,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             }
         } else {
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            const int tk = r / a.G;
-            *(u32x2*)(a.out + b * a.ob + (hk * a.G + r - tk * a.G) * a.oh + tk * a.ol + d) =
+            *(u32x2*)(a.out + b * a.ob + (hk * a.G + r0 + r - tk * a.G) * a.oh + tk * a.ol + d) =
                 u32x2{pack2<ET>(v[0] * inv, v[1] * inv), pack2<ET>(v[2] * inv, v[3] * inv)};
         }
     }
@@ -390,7 +392,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
 template <int ET, int D, bool PAGED>
 hipError_t launch_span_row_d(const SpanKernel& a, hipStream_t stream) {
     using G = SpanRow<D, PAGED>;
-    const long long wgs = (long long)a.B * a.Hk * a.splits;
+    const long long wgs = (long long)a.B * a.Hk * a.row_blocks * a.splits;
     if (!grid_fits(wgs, G::kThreads)) return kGridTooLarge;
     auto kern = span_row_kernel<ET, D, PAGED>;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),

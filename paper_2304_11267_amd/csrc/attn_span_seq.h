@@ -7,7 +7,7 @@
 
 namespace sdattn {
 
-constexpr int kSpanRows = 32;          // most rows of a key head for attn_span_row.h
+constexpr int kSpanRows = 32;          // rows of a block of attn_span_row.h
 // Rows of a block of the tiled kernel for heads of D (a multiple of 16).  Wide heads have no registers for the codes of
 // pages beside 128 rows.
 constexpr int span_block(int D, bool paged) { return D > (paged ? 96 : 128) ? 256 : 128; }
@@ -28,7 +28,7 @@ struct SpanKernel {
     int B, Hk, G, Lq, Lk, D;
     int pages, slots;
     int frame, window, sinks;
-    int row_blocks, splits;    // blocks of rows, parts of their keys
+    int row_blocks, splits;    // blocks of a key head's rows, parts of their keys
     float c;                   // |scale| log2(e); with scale 0, 1 and Q is taken for zeros
     int neg;                   // scale < 0
     int zero;                  // scale = 0

@@ -268,7 +268,7 @@ struct SpanArgs {
 // How a call is cut up: blocks of query rows, and parts of each one's keys that are joined
 // afterwards through the workspace.
 struct SpanPlan {
-    bool single;           // few rows: attn_span_row.h
+    bool single;           // blocks of 32 rows: attn_span_row.h
     int row_blocks, splits;
     long long workspace;   // bytes; -1: too large
 };

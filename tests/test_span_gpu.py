@@ -428,3 +428,15 @@ def test_what_a_page_holds_behind_the_sequence():
         for D in (40, 128):
             a, b = (cached(2, 8, 2, Lq, D, 3, spoil=s) for s in (True, False))
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("D", [40, 72, 128, 160])
+@pytest.mark.parametrize("H,Hk", [(1, 1), (6, 2), (5, 1)])
+def test_blocks_of_32_rows(H, Hk, D):
+    """More rows than one block of 32 and few blocks: tokens whose heads lie in two blocks, ragged counts, parts of keys."""
+    for Lq in (12, 33, 70, 201):
+        for rule in ((1, 0, 0), (1, 45, 9), (0, 0, 0), (16, 64, 40)):
+            window(2, H, Hk, Lq, Lq + 90, D, *rule, starts=[90, 17], counts=[Lq, Lq - 5], x_rows=D == 72, y_rows=D != 72)
+            cached(2, H, Hk, Lq, D, 90, *rule, dtype="bf16", starts=[90, 64], counts=[Lq - 9, Lq], x_rows=D != 72, missing=[(0, 0)])
+        cached(1, H, Hk, Lq, D, 9000, 1, 0, 0)
+        window(1, H, Hk, Lq, 9000, D, 1, 8000, 100, dtype="bf16")
