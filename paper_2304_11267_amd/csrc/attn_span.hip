@@ -134,6 +134,7 @@ static hipError_t launch_span_join(const SpanKernel& a, int type, hipStream_t st
 // A way to cut a call up, and the time that it is taken for, in us.
 struct SpanWay {
     int row_blocks, splits;
+    long long tiles;   // the most that a block can see
     double time;
 };
 
@@ -145,7 +146,7 @@ static SpanWay span_way(const SpanArgs& a, bool single) {
     const int G = a.H / a.Hk;
     const long long rows = (long long)a.Lq * G, heads = (long long)a.B * a.Hk;
     const int block = single ? kSpanRows : span_block((a.D + 15) / 16 * 16, a.slots > 0), tile = single ? 32 : 64;
-    SpanWay w{(int)((rows + block - 1) / block), 1, 0.0};
+    SpanWay w{(int)((rows + block - 1) / block), 1, 0, 0.0};
     const long long wgs = heads * w.row_blocks;
     // the most tiles that a block can see
     long long tiles = ((long long)a.Lk + tile - 1) / tile;
@@ -154,6 +155,7 @@ static SpanWay span_way(const SpanArgs& a, bool single) {
         const long long seen = ((long long)a.sinks + tile - 1) / tile + ((long long)a.window + spread) / tile + 2;
         if (seen < tiles) tiles = seen;
     }
+    w.tiles = tiles;
     const double cost = single ? fmax(32.0 * 2 * a.D * (a.slots > 0 ? 1 : 2) / 50e3, 0.12)
                       : block == 256 ? 1.0 + 0.01 * a.D : (0.55 + 0.006 * a.D) * (a.slots > 0 ? 1.25 : 1.0);
     const double part = (double)rows * heads * a.D * 8 / 4e6 + 0.1;
@@ -188,6 +190,7 @@ SpanPlan span_plan(const SpanArgs& a) {
         if (heads * w.row_blocks > kCus || tiled.time < w.time) w = tiled, p.single = false;
     }
     p.row_blocks = w.row_blocks, p.splits = w.splits;
+    p.part_tiles = (int)((w.tiles + w.splits - 1) / w.splits);
     if (p.splits > 1) {
         const __int128 bytes = (__int128)p.splits * heads * rows * (a.D + 2) * 4;
         p.workspace = bytes < ((__int128)1 << 62) ? (long long)bytes : -1;
@@ -213,7 +216,7 @@ hipError_t launch_span(const SpanArgs& s) {
     a.B = s.B, a.Hk = s.Hk, a.G = s.H / s.Hk, a.Lq = s.Lq, a.Lk = s.Lk, a.D = s.D;
     a.pages = s.pages, a.slots = s.slots;
     a.frame = s.frame, a.window = s.window, a.sinks = s.sinks;
-    a.row_blocks = p.row_blocks, a.splits = p.splits;
+    a.row_blocks = p.row_blocks, a.splits = p.splits, a.part_tiles = p.part_tiles;
     a.zero = s.scale == 0.0f, a.neg = s.scale < 0;
     a.c = a.zero ? 1.0f : (a.neg ? -s.scale : s.scale) * kLog2e;
     const hipStream_t stream = (hipStream_t)s.stream;

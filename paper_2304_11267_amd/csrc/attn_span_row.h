@@ -41,9 +41,10 @@ struct SpanRow {
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kFit = kRoom / (kWaves * kBufBytes);
     static constexpr int kBufs = kFit > 4 ? 4 : kFit;                // tiles in LDS or on their way
-    static constexpr int kRing = kWaves * kBufs * kBufBytes + 16;    // (a read of V's last 16 columns may end past a row)
-    static constexpr int kJoin = kWaves * kSpanRows * (D + 4) * 4;   // O of a row, then m and l
-    static constexpr int kLdsBytes = kRing > kJoin ? kRing : kJoin;
+    static constexpr int kRing = kBufs * kBufBytes;                  // of a wave
+    static constexpr int kJoin = kSpanRows * (D + 4) * 4;            // O of a row, then m and l
+    // (a read of V's last 16 columns may end past a row)
+    static constexpr int lds_bytes(int waves) { return kRing + 16 > kJoin ? waves * kRing + 16 : waves * kJoin; }
     static constexpr int kAhead = (kBufs - 1) * 2 * kCopies;         // copies in flight behind a tile that is used
     static_assert(kAhead < 64, "vmcnt");
     static __device__ __forceinline__ int swap(int row) { return kSwap > 1 ? row / (16 / kSwap) & (kSwap - 1) : 0; }
@@ -89,11 +90,13 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
     const SpanTiles tiles = span_tiles(a, seq, token0, token1, TK);
     const SpanRun run = span_run(a, seq, token0, token1);
     const int hi = span_hi(a, seq, token), lo = span_lo(a, hi), sinks = a.sinks;
-    // this split's tiles, and of these every kWaves-th
+    // this split's tiles, and of these every `waves`-th
     const int per = (tiles.count + a.splits - 1) / a.splits;
+    const int waves = a.waves;
     const int first = split * per + wave, last = min(split * per + per, tiles.count);
-    const int mine = first < last ? (last - first + G::kWaves - 1) / G::kWaves : 0;
-    auto tile_of = [&](int i) __attribute__((always_inline)) { return tiles.at(first + i * G::kWaves); };
+    const int left = first < last ? last - first + waves - 1 : 0;
+    const int mine = waves == 1 ? left : (int)__umulhi((uint32_t)left, a.per_wave);   // left / waves
+    auto tile_of = [&](int i) __attribute__((always_inline)) { return tiles.at(first + i * waves); };
 
     // pages: of this wave's tiles 64 k .. 64 k + 63, one a lane
     [[maybe_unused]] int pages = 0;
@@ -356,22 +359,29 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
     }
     __syncthreads();
     const size_t rows = (size_t)a.B * a.Hk * R;
-    for (int z = tid; z < min(R - r0, kSpanRows) * (D / 4); z += G::kThreads) {
+    for (int z = tid; z < min(R - r0, kSpanRows) * (D / 4); z += 64 * waves) {
         const int r = z / (D / 4), d = (z - r * (D / 4)) * 4, tk = (r0 + r) / a.G;
         if (tk >= seq.count) break;   // (rows of later tokens follow)
         const float* const o = parts + r * kO;
         float top = kSpanNone, sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < G::kWaves; ++w) top = fmaxf(top, o[w * kSpanRows * kO + D]);
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < G::kWaves; ++w) {
+        auto highest = [&](int w) __attribute__((always_inline)) { top = fmaxf(top, o[w * kSpanRows * kO + D]); };
+        auto add = [&](int w) __attribute__((always_inline)) {
             const float* const ow = o + w * kSpanRows * kO;
             const float f = fast_exp2(ow[D] - top);
             sum = fmaf(ow[D + 1], f, sum);
             const f32x4 x = *(const f32x4*)(ow + d);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], f, v[e]);
+        };
+        if (waves == G::kWaves) {
+#pragma unroll
+            for (int w = 0; w < G::kWaves; ++w) highest(w);
+#pragma unroll
+            for (int w = 0; w < G::kWaves; ++w) add(w);
+        } else {
+            for (int w = 0; w < waves; ++w) highest(w);
+            for (int w = 0; w < waves; ++w) add(w);
         }
         if (a.splits > 1) {
             const size_t at = (split * rows + (size_t)bh * R + r0 + r);
@@ -394,11 +404,22 @@ hipError_t launch_span_row_d(const SpanKernel& a, hipStream_t stream) {
     using G = SpanRow<D, PAGED>;
     const long long wgs = (long long)a.B * a.Hk * a.row_blocks * a.splits;
     if (!grid_fits(wgs, G::kThreads)) return kGridTooLarge;
+    // With more workgroups than CUs no more waves than there are tiles, or than a join of 16 values a thread takes, where
+    // two workgroups then fit a CU (a token of 64 sequences of 8 heads, one tile, D = 64: 9.9 -> 6.2 us; 8 tokens of 64
+    // sequences, 64 heads over 16, one tile, D = 128 32 -> 20).
+    SpanKernel k = a;
+    k.waves = G::kWaves;
+    if (wgs > kCus) {
+        const int rows = a.Lq * a.G < kSpanRows ? a.Lq * a.G : kSpanRows, join = (rows * (D / 4) + 255) / 256;
+        const int need = a.part_tiles > join ? a.part_tiles : join;
+        if (need < k.waves && G::lds_bytes(need) <= 80 * 1024) k.waves = need;
+    }
+    k.per_wave = (uint32_t)(((1ull << 32) + k.waves - 1) / k.waves);   // (exact up to 2^29 tiles)
     auto kern = span_row_kernel<ET, D, PAGED>;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, G::lds_bytes(G::kWaves));
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(G::kThreads), G::kLdsBytes, stream, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(64 * k.waves), G::lds_bytes(k.waves), stream, k);
     return hipGetLastError();
 }
 

@@ -270,6 +270,7 @@ struct SpanArgs {
 struct SpanPlan {
     bool single;           // blocks of 32 rows: attn_span_row.h
     int row_blocks, splits;
+    int part_tiles;        // the most tiles of a part
     long long workspace;   // bytes; -1: too large
 };
 SpanPlan span_plan(const SpanArgs& a);

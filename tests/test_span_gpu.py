@@ -440,3 +440,12 @@ def test_blocks_of_32_rows(H, Hk, D):
             cached(2, H, Hk, Lq, D, 90, *rule, dtype="bf16", starts=[90, 64], counts=[Lq - 9, Lq], x_rows=D != 72, missing=[(0, 0)])
         cached(1, H, Hk, Lq, D, 9000, 1, 0, 0)
         window(1, H, Hk, Lq, 9000, D, 1, 8000, 100, dtype="bf16")
+
+
+@pytest.mark.parametrize("D", [40, 64, 128, 160])
+def test_many_short_sequences(D):
+    """More blocks than CUs, of one tile or a few: workgroups of fewer waves."""
+    for Lq, keys in ((1, 1), (1, 20), (1, 64), (1, 130), (4, 40), (8, 8), (5, 97)):
+        counts = [Lq - b % 2 if Lq > 1 else 1 - b % 3 // 2 for b in range(40)]
+        window(40, 16, 8, Lq, max(keys, Lq), D, counts=counts, starts=[max(keys, Lq) - Lq - b % 3 for b in range(40)])
+        cached(40, 16, 8, Lq, D, max(keys - Lq, 0), dtype="bf16", counts=counts, starts=[max(keys - Lq - b % 5, 0) for b in range(40)])
