@@ -133,7 +133,7 @@ __device__ __forceinline__ void span_add_bad(f32x16 (&acc)[DN], const char* vt, 
 // frames of 1350 and the first: 890 to 930 us by the card, 880 to 920 TFLOP/s of the visible keys, where a library's product
 // reaches 1300.  4096 tokens of D = 40, windows of 1024 and 77: 29.6 us; a tile takes 1.1 us of it on two
 // workgroups of a CU, of which the products alone are 0.58, the exponentials and sums 0.3 to 0.4, copies and LDS reads
-// the rest.  Pages, 1350 tokens over 6750 keys, D = 128: 136 us and a join of 7.6.
+// the rest.  Pages, 1350 tokens over 6750 keys, D = 128: 132 us and a join of 7.6.
 
 // Waves of a SIMD that the registers are cut for: three where that costs none (D = 40 in pages, 2665 tokens of 16 sequences
 // 99 -> 83 us; D = 64, 64 heads of 4096 tokens 370 -> 345; 64 in pages spills, 99 -> 101).
