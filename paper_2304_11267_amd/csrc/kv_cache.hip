@@ -11,8 +11,8 @@
 // Both directions move bytes: 2 read and 1 written for a value, or the reverse.  A team of
 // threads takes one (page, key head) of K or V, holds its new values in registers between the
 // maximum and the codes, and writes 8 codes (8 bytes) at a time.  17550 tokens of 16 heads of 128: written in
-// 46 us, 4.66 TB/s where a copy reaches 5.14; eight sequences of 1365 to 4096 tokens, 8 heads of 80, read back in 20.3,
-// 4.37 TB/s; a token of each of 64 sequences 4.1, a launch and the chain from its place to its page's scale.
+// 46 us, 4.66 TB/s where a copy reaches 5.14; eight sequences of 1365 to 4096 tokens, 8 heads of 80, read back in 20.6,
+// 4.3 TB/s; a token of each of 64 sequences 4.1, a launch and the chain from its place to its page's scale.
 #include "device.h"
 #include "launch.h"
 
@@ -170,10 +170,11 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const CacheK
 
 // 64 tokens of a sequence, one key head of K or V: the codes' values in 16 bits; zeros for
 // positions without a page.
-template <int ET, int CH>
+template <int ET, int TEAM, int CH>
 __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(const CacheKernel a) {
-    const int D = a.D, pieces = D / 8;
-    const long long item = blockIdx.x;
+    const int D = a.D, pieces = D / 8, t = threadIdx.x % TEAM;
+    const long long item = (long long)blockIdx.x * (kCacheThreads / TEAM) + (TEAM == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : 0);
+    if (TEAM == 64 && item >= 2LL * a.B * a.blocks * a.Hk) return;
     const int h = (int)(item % a.Hk);
     long long rest = item / a.Hk;
     const int block = (int)(rest % a.blocks);
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(const CacheKe
     u32x2 w[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = i * kCacheThreads + (int)threadIdx.x, row = c / pieces, d = (c - row * pieces) * 8;
+        const int c = i * TEAM + t, row = c / pieces, d = (c - row * pieces) * 8;
         const bool second = row >= split;
         w[i] = u32x2{0u, 0u};
         if (row < rows && (second ? scale[1] : scale[0]) >= 0.0f)
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(const CacheKe
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = i * kCacheThreads + (int)threadIdx.x, row = c / pieces, d = (c - row * pieces) * 8;
+        const int c = i * TEAM + t, row = c / pieces, d = (c - row * pieces) * 8;
         if (row >= rows) continue;
         const float s = row >= split ? scale[1] : scale[0];
         u32x4 o = {0u, 0u, 0u, 0u};
@@ -238,26 +239,40 @@ CacheKernel kernel_args(const CacheArgs& c) {
     return a;
 }
 
+// Whether a wave takes a page's head, rather than four, which leave threads idle at D = 40 and 80 and wait for each other:
+// up to D = 80, with enough heads of pages (16 sequences of 8523 tokens, 5 heads of 40, written 56 -> 39 us and read 41 -> 31; 8 of
+// 4096, 8 heads of 64 27.9 -> 25 and 18.8 -> 16.4, 80 32 -> 29 and 20.9 -> 20.7, 96 34.2 -> 39.6; 96 heads of pages of 64
+// 4.8 -> 6.2, 1664 8.4 -> 8.6, 2080 of 40 8.5 -> 6.6).
+bool by_wave(long long items, int D) { return items >= 2048 && D <= 80; }
+
 template <int ET>
 hipError_t write_e(const CacheArgs& c) {
     CacheKernel a = kernel_args(c);
     a.x[0] = (const uint16_t*)c.k, a.x[1] = (const uint16_t*)c.v;
     a.blocks = (int)min((long long)c.slots, ((long long)c.L + 2 * kPage - 2) / kPage);   // L tokens may begin at a page's last
     const long long items = 2LL * c.B * a.blocks * c.Hk;
-    const bool one = c.L == 1;
-    const long long wgs = one ? (items + 3) / 4 : items;
+    const bool one = c.L == 1, wave = one || by_wave(items, c.D);
+    const long long wgs = wave ? (items + 3) / 4 : items;
     if (!grid_fits(wgs, kCacheThreads)) return kGridTooLarge;
     const int ch = (8 * c.D + kCacheThreads - 1) / kCacheThreads;   // 64 D values, 8 a piece
     auto k = one ? cache_write_kernel<ET, 64, 1>
-           : ch <= 2 ? cache_write_kernel<ET, 256, 2> : ch <= 4 ? cache_write_kernel<ET, 256, 4> : cache_write_kernel<ET, 256, 8>;
+           : wave ? (c.D <= 40 ? cache_write_kernel<ET, 64, 5> : c.D <= 64 ? cache_write_kernel<ET, 64, 8> : cache_write_kernel<ET, 64, 10>)
+           : ch <= 2 ? cache_write_kernel<ET, 256, 2> : ch <= 3 ? cache_write_kernel<ET, 256, 3> : ch <= 4 ? cache_write_kernel<ET, 256, 4>
+           : ch <= 5 ? cache_write_kernel<ET, 256, 5> : cache_write_kernel<ET, 256, 8>;
     hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(kCacheThreads), 0, (hipStream_t)c.stream, a);
     return hipGetLastError();
 }
 
 template <int ET>
-hipError_t read_e(const CacheKernel& a, long long wgs, void* stream) {
+hipError_t read_e(const CacheKernel& a, void* stream) {
     const int ch = (8 * a.D + kCacheThreads - 1) / kCacheThreads;
-    auto k = ch <= 2 ? cache_read_kernel<ET, 2> : ch <= 3 ? cache_read_kernel<ET, 3> : ch <= 4 ? cache_read_kernel<ET, 4> : cache_read_kernel<ET, 8>;
+    const long long items = 2LL * a.B * a.blocks * a.Hk;
+    const bool wave = by_wave(items, a.D);
+    const long long wgs = wave ? (items + 3) / 4 : items;
+    if (!grid_fits(wgs, kCacheThreads)) return kGridTooLarge;
+    auto k = wave ? (a.D <= 40 ? cache_read_kernel<ET, 64, 5> : a.D <= 64 ? cache_read_kernel<ET, 64, 8> : cache_read_kernel<ET, 64, 10>)
+           : ch <= 2 ? cache_read_kernel<ET, 256, 2> : ch <= 3 ? cache_read_kernel<ET, 256, 3>
+           : ch <= 4 ? cache_read_kernel<ET, 256, 4> : ch <= 5 ? cache_read_kernel<ET, 256, 5> : cache_read_kernel<ET, 256, 8>;
     hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(kCacheThreads), 0, (hipStream_t)stream, a);
     return hipGetLastError();
 }
@@ -270,9 +285,7 @@ hipError_t launch_cache_read(const CacheArgs& c) {
     CacheKernel a = kernel_args(c);
     a.y[0] = (uint16_t*)c.k, a.y[1] = (uint16_t*)c.v;
     a.blocks = (c.L + kPage - 1) / kPage;
-    const long long wgs = 2LL * c.B * a.blocks * c.Hk;
-    if (!grid_fits(wgs, kCacheThreads)) return kGridTooLarge;
-    return c.dtype == kF16 ? read_e<kF16>(a, wgs, c.stream) : read_e<kBF16>(a, wgs, c.stream);
+    return c.dtype == kF16 ? read_e<kF16>(a, c.stream) : read_e<kBF16>(a, c.stream);
 }
 
 }  // namespace sdattn

@@ -223,3 +223,42 @@ def test_replays():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(fresh, (*args, *out)))
+
+
+@pytest.mark.parametrize("layout", ["heads", "rows"])
+@pytest.mark.parametrize("D", [8, 40, 48, 64, 72, 80, 88, 160])
+def test_many_pages_are_as_few(D, layout):
+    """A call over many sequences gives what calls over some of them give, bit for bit, and back."""
+    import torch
+    B, Hk, L, slots = 64, 8, 70, 3
+    P = B * slots
+    g = op.generator(D)
+    lay = sd.LAYOUT_ROWS if layout == "rows" else sd.LAYOUT_HEADS
+    shape = (B, L, Hk * D) if layout == "rows" else (B, Hk, L, D)
+    k, v = (op.randn(g, *shape, dtype="bf16", sigma=s) for s in (1.0, 9.0))
+    table = torch.randperm(P, device="cuda", generator=g).to(torch.int32).view(B, slots)
+    starts = (torch.arange(B, device="cuda") * 7 % 100).to(torch.int32)
+    counts = (L - torch.arange(B, device="cuda") * 5 % 80).to(torch.int32)
+    caches, backs = [], []
+    for parts in (1, 16):
+        c = [torch.full((P, Hk, 64, D), 0x30, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        c += [torch.full((P, Hk), 2.0 ** -4, device="cuda") for _ in range(2)]
+        back = [torch.full(shape, 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        n = B // parts
+        for i in range(0, B, n):
+            s = slice(i, i + n)
+            sd.cache_write(k[s], v[s], *c, table[s], starts[s], counts=counts[s], layout=lay)
+        for i in range(0, B, n):
+            s = slice(i, i + n)
+            sd.cache_read(back[0][s], back[1][s], *c, table[s], starts[s], counts=counts[s], layout=lay)
+        caches.append(c)
+        backs.append(back)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*caches)) and all(torch.equal(a, b) for a, b in zip(*backs))
+    rows = backs[0][0].unflatten(2, (Hk, D)).transpose(1, 2) if layout == "rows" else backs[0][0]
+    x = k.unflatten(2, (Hk, D)).transpose(1, 2) if layout == "rows" else k
+    for b in (0, 1, 17, 63):
+        n = max(int(counts[b]), 0)
+        assert (rows[b, :, n:] == 7).all()
+        top = float(x[b].abs().max())
+        assert ((rows[b, :, :n].float() - x[b, :, :n].float()).abs() <= x[b, :, :n].float().abs() * 2.0 ** -4 + top * 2.0 ** -17 * 2).all()
