@@ -131,12 +131,13 @@ def test_launches_of_more_threads_than_32_bits(lib):  # noqa: F811
                  B=1, L=1 << 27, C=1024, batches=1, groups=1, sg=big(0), ss=big(0), st=big(0), skip=f32(1), norm_r=0, norm=1,
                  eps=f32(0), x_dtype=F16, dtype=F16)
     refused(lib.sdattn_gated_norm, gated, [(UNSUPPORTED, {})], lib)
-    cache = dict(zip(("k", "v", "kp", "vp", "ks", "vs", "table", "starts", "counts"), far), B=1 << 14, Hk=1 << 10, L=1, D=8, pages=4,
+    cache = dict(zip(("k", "v", "kp", "vp", "ks", "vs", "table", "starts", "counts"), far), B=1 << 14, Hk=1 << 10, L=1, D=88, pages=4,
                  slots=1, layout=ROWS, dtype=F16)
-    refused(lib.sdattn_cache_write, cache, [(UNSUPPORTED, dict(Hk=1 << 12)), (UNSUPPORTED, dict(L=2, Hk=1 << 10))], lib)
+    refused(lib.sdattn_cache_write, cache, [(UNSUPPORTED, dict(Hk=1 << 12)), (UNSUPPORTED, dict(L=2, Hk=1 << 10)),
+                                            (UNSUPPORTED, dict(L=2, Hk=1 << 12, D=8))], lib)
     read = {n: cache[n] for n in ("kp", "vp", "ks", "vs", "table", "starts", "counts", "k", "v")}
     read.update({n: cache[n] for n in ("B", "Hk", "L", "D", "pages", "slots", "layout", "dtype")})
-    refused(lib.sdattn_cache_read, read, [(UNSUPPORTED, {})], lib)
+    refused(lib.sdattn_cache_read, read, [(UNSUPPORTED, {}), (UNSUPPORTED, dict(Hk=1 << 12, D=8))], lib)
     window = dict(zip(("q", "k", "v", "starts", "counts", "out", "ws"), far), wsb=big(1 << 50), B=1 << 12, H=1 << 12, Hk=1 << 12, Lq=200,
                   Lk=1, D=32, frame=1, window=0, sinks=0, scale=f32(1), xl=HEADS, yl=HEADS, dtype=F16)
     refused(lib.sdattn_window_forward, window, [(UNSUPPORTED, {}), (UNSUPPORTED, dict(Lq=1, B=1 << 13))], lib)
