@@ -11,8 +11,8 @@
 // Both directions move bytes: 2 read and 1 written for a value, or the reverse.  A team of
 // threads takes one (page, key head) of K or V, holds its new values in registers between the
 // maximum and the codes, and writes 8 codes (8 bytes) at a time.  17550 tokens of 16 heads of 128: written in
-// 46 us, 4.66 TB/s where a copy reaches 5.14; eight sequences of 1365 to 4096 tokens, 8 heads of 80, read back in 20.6,
-// 4.3 TB/s; a token of each of 64 sequences 4.1, a launch and the chain from its place to its page's scale.
+// 46 us, 4.66 TB/s where a copy reaches 5.14; eight sequences of 1365 to 4096 tokens, 8 heads of 80, read back in 20.3,
+// 4.4 TB/s; a token of each of 64 sequences 4.1, a launch and the chain from its place to its page's scale.
 #include "device.h"
 #include "launch.h"
 
@@ -240,10 +240,10 @@ CacheKernel kernel_args(const CacheArgs& c) {
 }
 
 // Whether a wave takes a page's head, rather than four, which leave threads idle at D = 40 and 80 and wait for each other:
-// up to D = 80, with enough heads of pages (16 sequences of 8523 tokens, 5 heads of 40, written 56 -> 39 us and read 41 -> 31; 8 of
-// 4096, 8 heads of 64 27.9 -> 25 and 18.8 -> 16.4, 80 32 -> 29 and 20.9 -> 20.7, 96 34.2 -> 39.6; 96 heads of pages of 64
+// up to D = 80 (reading: 64), with enough heads of pages (16 sequences of 8523 tokens, 5 heads of 40, written 56 -> 39 us and read 41 -> 31; 8 of
+// 4096, 8 heads of 64 27.9 -> 25 and 18.8 -> 16.4, 80 32 -> 29 and, from HBM, 20.3 -> 20.8, 96 34.2 -> 39.6; 96 heads of pages of 64
 // 4.8 -> 6.2, 1664 8.4 -> 8.6, 2080 of 40 8.5 -> 6.6).
-bool by_wave(long long items, int D) { return items >= 2048 && D <= 80; }
+bool by_wave(long long items, int D, int most) { return items >= 2048 && D <= most; }
 
 template <int ET>
 hipError_t write_e(const CacheArgs& c) {
@@ -251,7 +251,7 @@ hipError_t write_e(const CacheArgs& c) {
     a.x[0] = (const uint16_t*)c.k, a.x[1] = (const uint16_t*)c.v;
     a.blocks = (int)min((long long)c.slots, ((long long)c.L + 2 * kPage - 2) / kPage);   // L tokens may begin at a page's last
     const long long items = 2LL * c.B * a.blocks * c.Hk;
-    const bool one = c.L == 1, wave = one || by_wave(items, c.D);
+    const bool one = c.L == 1, wave = one || by_wave(items, c.D, 80);
     const long long wgs = wave ? (items + 3) / 4 : items;
     if (!grid_fits(wgs, kCacheThreads)) return kGridTooLarge;
     const int ch = (8 * c.D + kCacheThreads - 1) / kCacheThreads;   // 64 D values, 8 a piece
@@ -267,10 +267,10 @@ template <int ET>
 hipError_t read_e(const CacheKernel& a, void* stream) {
     const int ch = (8 * a.D + kCacheThreads - 1) / kCacheThreads;
     const long long items = 2LL * a.B * a.blocks * a.Hk;
-    const bool wave = by_wave(items, a.D);
+    const bool wave = by_wave(items, a.D, 64);
     const long long wgs = wave ? (items + 3) / 4 : items;
     if (!grid_fits(wgs, kCacheThreads)) return kGridTooLarge;
-    auto k = wave ? (a.D <= 40 ? cache_read_kernel<ET, 64, 5> : a.D <= 64 ? cache_read_kernel<ET, 64, 8> : cache_read_kernel<ET, 64, 10>)
+    auto k = wave ? (a.D <= 40 ? cache_read_kernel<ET, 64, 5> : cache_read_kernel<ET, 64, 8>)
            : ch <= 2 ? cache_read_kernel<ET, 256, 2> : ch <= 3 ? cache_read_kernel<ET, 256, 3>
            : ch <= 4 ? cache_read_kernel<ET, 256, 4> : ch <= 5 ? cache_read_kernel<ET, 256, 5> : cache_read_kernel<ET, 256, 8>;
     hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(kCacheThreads), 0, (hipStream_t)stream, a);
