@@ -116,11 +116,12 @@ __device__ __forceinline__ void span_add_bad(f32x16 (&acc)[DN], const char* vt, 
 
 // ---------------------------------------------------------------- the tiled kernel
 
-// Workgroups of NW waves of 32 rows: four, and two or three workgroups a CU, whose waves share the SIMDs without waiting for
-// each other at barriers (eight waves of one workgroup, D = 128: one of a SIMD's two ends its tile first, and the
-// other's products then have no exponentials beside them); eight past D = 128, where registers and LDS leave no room for that.  K and V tiles
-// of 64 keys lie as 16-bit values in LDS buffers, two or three of K and two of V, rows of DP values whose 16-byte chunks are permuted
-// where rows would share banks (chunk c of row r in the place of c ^ swap(r)).
+// Workgroups of NW waves of 32 rows: four, and two or three workgroups a CU, whose waves share the SIMDs without
+// waiting for each other at barriers (eight waves of one workgroup, D = 128: one of a SIMD's two ends its tile first, and
+// the other's products then have no exponentials beside them); eight past D = 128, and over pages past 96, where registers
+// and LDS leave no room for that.  K and V tiles of 64 keys lie as 16-bit values in LDS buffers, two or three of K and two
+// of V, rows of DP values whose 16-byte chunks are permuted where rows would share banks (chunk c of row r in the place of
+// c ^ swap(r)).
 //
 // The pass is one stream over 32-key sub-tiles p = 0, 1, ...: step p issues
 //   S^T = K Q^T of sub-tile p + 1,  the weights 2^(c s - m) of p,  O^T += V^T P^T of p - 1

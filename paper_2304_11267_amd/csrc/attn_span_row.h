@@ -2,8 +2,8 @@
 // new token, or of a few), for calls that have a CU for each block.
 //
 // What counts is reading the visible keys and values once.  A workgroup takes one block, or a
-// part of its keys, and each of its waves every eighth tile of 32 of them (wide heads: every fourth or third), through a ring of LDS buffers
-// of its own: direct global->LDS copies of the tiles to come are in flight while one is used, and no
+// part of its keys, and each of its waves every eighth tile of 32 of them (wide heads: every fourth or third),
+// through a ring of LDS buffers of its own: direct global->LDS copies of the tiles to come are in flight while one is used, and no
 // wave waits for another before the end.  The page and the scales of a wave's tiles lie in its
 // lanes, 64 tiles at a time.  Codes stay codes in LDS; a lane turns the 8 that it needs for a matrix product
 // into 16-bit values on their way there (4 instructions), V's through the transposing read of bytes
