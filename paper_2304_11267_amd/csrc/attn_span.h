@@ -27,6 +27,13 @@ constexpr int kSpanTile = 64;          // keys of a tile: a page of the cache
 // and few tiles move it (fp16 holds values below 2^16).
 constexpr float kSpanBias = 8.0f;
 constexpr float kSpanLimit = 15.0f;
+// c s - m is one operation, exact in c s, where m came from a c s that was rounded.  Up to 2^23 that is a quarter of an octave
+// of a weight at most; from 2^28 on a row's largest weight would be anything from 0 to infinity.  Rows whose m has
+// been past 2^23 are computed again at the end (span_again); the largest |m| is noted where m is moved.  (A row whose m is
+// infinite is one of no numbers already.)
+constexpr float kSpanFar = 8388608.0f;
+__device__ __forceinline__ bool span_far(float worst, float m) { return worst >= kSpanFar && m <= __FLT_MAX__; }
+__device__ __forceinline__ float span_worst(float worst, float m) { return fmaxf(worst, m == kSpanNone ? 0.0f : fabsf(m)); }
 
 // 8 codes as 8 values of the 16-bit type times s, a power of two (v_cvt_scalef32_pk_f16_fp8 /
 // _bf16_fp8)
@@ -114,6 +121,86 @@ __device__ __forceinline__ void span_add_bad(f32x16 (&acc)[DN], const char* vt, 
     }
 }
 
+// A row whose scores are far from zero, by a wave, key by key: its largest score, rounded as all of them are, and then
+// the weights and sums relative to it, in 32 bits.  `row` is its query, [lo, hi) and a.sinks what it sees, tile_of(i) the i-th
+// of n tiles of TK keys.  What comes here is far from what a model makes: the time does not count.
+struct SpanAgain {
+    float o[3], m, l;   // of the columns lane + 64 i
+};
+template <int ET, bool PAGED, int TK, typename F>
+__device__ __forceinline__ SpanAgain span_again(const SpanKernel& a, int b, int hk, const uint16_t* row, int hi, int lo, int n, F tile_of) {
+    const int lane = lane_id();
+    const long long bytes = PAGED ? a.D : 2 * a.kl;   // from one key to the next
+    auto scores = [&](auto use) __attribute__((always_inline)) {
+        for (int i = 0; i < n; ++i) {
+            const int t = tile_of(i), key = t * TK + lane;
+            long long at = 2 * (b * a.kb + hk * a.kh + (long long)t * TK * a.kl);
+            float ct = a.c, vs = 1.0f;
+            if constexpr (PAGED) {
+                const int page = a.table[(size_t)b * a.slots + t / (kCachePage / TK)];
+                if (page < 0 || page >= a.pages) continue;
+                at = (((long long)page * a.Hk + hk) * kCachePage + t % (kCachePage / TK) * TK) * a.D;
+                ct = __builtin_amdgcn_fmed3f(ct * a.ks[(size_t)page * a.Hk + hk], __FLT_MIN__, __FLT_MAX__);
+                vs = a.vs[(size_t)page * a.Hk + hk];
+            }
+            const bool seen = lane < TK && key < hi && (key >= lo || key < a.sinks);
+            float x = 0.0f;
+            if (seen) {
+                const char* const k = a.k + at + lane * bytes;
+                for (int d = 0; d < a.D; d += 8) {
+                    u32x4 q = *(const u32x4*)(row + d), w;
+                    if (a.neg) q ^= 0x80008000u;
+                    if (a.zero) q = u32x4{0u, 0u, 0u, 0u};
+                    if constexpr (PAGED) {
+                        const u32x2 c = *(const u32x2*)(k + d);
+                        w = decode8<ET>(c[0], c[1], 1.0f);
+                    } else {
+                        w = *(const u32x4*)(k + 2 * d);
+                    }
+                    x = dot8<ET>(w, q, x);
+                }
+                x *= ct;
+                computed_here(x);   // (rounded)
+            }
+            use(seen, x, a.v + at, vs);
+        }
+    };
+    float top = -__builtin_inff();
+    bool bad = false;   // no number, or infinite and not below zero
+    scores([&](bool seen, float x, const char*, float) __attribute__((always_inline)) {
+        if (!seen) return;
+        top = fmaxf(top, x);
+        bad |= __float_as_uint(x) != 0xff800000u && (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
+    });
+    if (__any(bad)) {
+        const float none = __uint_as_float(0x7fc00000u);
+        return SpanAgain{{none, none, none}, kSpanNone, none};
+    }
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
+    SpanAgain r{{0.0f, 0.0f, 0.0f}, kSpanNone, 0.0f};
+    if (top == -__builtin_inff()) return r;
+    r.m = top;
+    scores([&](bool seen, float x, const char* v, float vs) __attribute__((always_inline)) {
+        const float w = seen ? fast_exp2(x - top) : 0.0f;
+        r.l += w;
+        for (uint64_t left = __ballot(seen); left; left &= left - 1) {
+            const int j = __builtin_ctzll(left);
+            const float f = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), j));
+#pragma unroll
+            for (int c = 0; c < 3; ++c) {
+                const int d = lane + 64 * c;
+                if (d >= a.D) continue;
+                if constexpr (PAGED) r.o[c] = fmaf(f, __builtin_amdgcn_cvt_f32_fp8((int)*(const uint8_t*)(v + j * bytes + d), 0) * vs, r.o[c]);
+                else r.o[c] = fmaf(f, to_float<ET>(*(const uint16_t*)(v + j * bytes + 2 * d)), r.o[c]);
+            }
+        }
+    });
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) r.l += __shfl_xor(r.l, k, 64);
+    return r;
+}
+
 // ---------------------------------------------------------------- the tiled kernel
 
 // Workgroups of NW waves of 32 rows: four, and two or three workgroups a CU, whose waves share the SIMDs without
@@ -172,6 +259,53 @@ __device__ __forceinline__ SpanWhole span_whole(const SpanRun& r) {
     return SpanWhole{(r.lo1 + TK - 1) / TK, r.hi0 / TK, r.sinks / TK};
 }
 
+// Blocks of the last rows, which see most, first; where all workgroups are on the card at once, for the next head
+// last, so that the two of a CU differ (causal, 16 heads of 4096 tokens D = 40 77 -> 65 us; 8192 tokens D = 128, four
+// rounds, 307 -> 374).
+struct SpanPlace {
+    int rb, bh, split;
+};
+__device__ __forceinline__ SpanPlace span_place(const SpanKernel& a, int wg) {
+    const int item = xcd_remap(wg, gridDim.x), turn = item / a.row_blocks;
+    int rb = item - turn * a.row_blocks;
+    if (!(turn & 1) || gridDim.x > 2 * kCus) rb = a.row_blocks - 1 - rb;
+    const int bh = turn / a.splits;
+    return SpanPlace{rb, bh, turn - bh * a.splits};
+}
+
+// The rows of a wave whose bits are set, by span_again, and stored.
+template <int ET, int DP, int NW, bool PAGED>
+__device__ __forceinline__ void span_tile_again(uint32_t rows, int wave) {
+    using G = SpanTile<DP, NW>;
+    const SpanAnew anew = span_anew();
+    const SpanKernel& a = anew.a;
+    const SpanPlace at = span_place(a, anew.wg);
+    const int b = at.bh / a.Hk, hk = at.bh - b * a.Hk, R = a.Lq * a.G, r0 = at.rb * G::kRows, lane = lane_id();
+    const SpanSeq seq = span_seq(a, b);
+    const SpanTiles tiles = span_tiles(a, seq, r0 / a.G, min((r0 + G::kRows - 1) / a.G, seq.count - 1), kSpanTile);
+    const int per = (tiles.count + a.splits - 1) / a.splits, begin = at.split * per, n = min(per, tiles.count - begin);
+    for (; rows; rows &= rows - 1) {
+        const int row = r0 + 32 * wave + __builtin_ctz(rows), token = row / a.G, head = hk * a.G + row - token * a.G;
+        const int hi = span_hi(a, seq, token), lo = span_lo(a, hi);
+        const SpanAgain x = span_again<ET, PAGED, kSpanTile>(a, b, hk, a.q + b * a.qb + head * a.qh + token * a.ql, hi, lo, n,
+                                                             [&](int i) { return tiles.at(begin + i); });
+        const float inv = x.l == 0.0f ? 0.0f : 1.0f / x.l;
+        const size_t all = (size_t)a.B * a.Hk * R, to = at.split * all + (size_t)at.bh * R + row;
+#pragma unroll
+        for (int c = 0; c < 3; ++c) {
+            const int d = lane + 64 * c;
+            if (d >= a.D) continue;
+            if (a.splits > 1) a.part[to * a.D + d] = x.o[c];
+            else a.out[b * a.ob + head * a.oh + token * a.ol + d] = from_float<ET>(x.o[c] * inv);
+        }
+        if (a.splits > 1 && lane == 0) {
+            float* const ml = a.part + a.splits * all * a.D + to * 2;
+            ml[0] = x.m;
+            ml[1] = x.l;
+        }
+    }
+}
+
 template <int ET, int DP, int NW, bool PAGED>
 __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)) void span_tile_kernel(const SpanKernel a) {
     using G = SpanTile<DP, NW>;
@@ -182,14 +316,8 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int D = a.D;
 
-    // Blocks of the last rows, which see most, first; where all workgroups are on the card at once, for the next head
-    // last, so that the two of a CU differ (causal, 16 heads of 4096 tokens D = 40 77 -> 65 us; 8192 tokens D = 128, four
-    // rounds, 307 -> 374).
-    int item = xcd_remap(blockIdx.x, gridDim.x);
-    const int turn = item / a.row_blocks;
-    int rb = item - turn * a.row_blocks;
-    if (!(turn & 1) || gridDim.x > 2 * kCus) rb = a.row_blocks - 1 - rb;
-    const int bh = turn / a.splits, split = turn - bh * a.splits, b = bh / a.Hk, hk = bh - b * a.Hk;
+    const SpanPlace at = span_place(a, blockIdx.x);
+    const int rb = at.rb, bh = at.bh, split = at.split, b = bh / a.Hk, hk = bh - b * a.Hk;
     auto token_of = [&](int row) __attribute__((always_inline)) { return a.G == 1 ? row : row / a.G; };
     // this lane's row, and its query, which waits for nothing
     const int R = a.Lq * a.G, r0 = rb * G::kRows, w0 = r0 + 32 * wave;
@@ -396,6 +524,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
     f32x16 acc[DN];
     float m = kSpanNone, l = 0.0f, alpha = 1.0f;
     int spoiled = 0;   // this lane's query sees a value that is no number
+    float worst = 0.0f;   // the largest |m| that this row has had
 #pragma unroll
     for (int n = 0; n < DN; ++n)
 #pragma unroll
@@ -509,6 +638,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
         if (!G::kOnes) computed_here(l);
         // the products of the sub-tile before were for the m before
         if (__any(alpha != 1.0f)) {
+            worst = span_worst(worst, m);
 #pragma unroll
             for (int n = 0; n < DN; ++n)
 #pragma unroll
@@ -567,7 +697,8 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
             if (t1.t >= 0) load_v(t1, even ^ 1);
             if (t2.t >= 0) load_k(t2, kfree);
             const bool end = !whole.has(t0.t) || (!block.has(t0.t) && *word != 0);
-            const float ct = PAGED ? fmaxf(a.c * t0.ks, __FLT_MIN__) : a.c;   // (minus infinity times it stays that)
+            // (zero and infinities times it stay that)
+            const float ct = PAGED ? __builtin_amdgcn_fmed3f(a.c * t0.ks, __FLT_MIN__, __FLT_MAX__) : a.c;
             if (live) {   // (waves without rows copy tiles for the others)
                 step(c0, even * G::kTileBytes, kbuf * G::kTileBytes, knext * G::kTileBytes, end, t0.t * TK, word, ct);
                 step(c1, even * G::kTileBytes, kbuf * G::kTileBytes, knext * G::kTileBytes, end, t0.t * TK + 32, word, ct);
@@ -606,7 +737,9 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
     } else {
         sum = half_sum(l);
     }
-    if (!valid) return;
+    const bool far = span_far(worst, m);
+    if (const uint32_t again = (uint32_t)__ballot(valid && far); __builtin_expect(again != 0, 0)) span_tile_again<ET, DP, NW, PAGED>(again, wave);
+    if (!valid || far) return;
     if (a.splits > 1) {
         const size_t at = ((size_t)split * a.B * a.Hk + bh) * R + row;
         float* const o = a.part + at * D;

@@ -56,6 +56,34 @@ struct SpanRow {
     }
 };
 
+// The rows of a wave whose bits are set, by span_again: O and m, l in `parts`.
+template <int ET, int D, bool PAGED>
+__device__ __forceinline__ void span_row_again(uint32_t rows, int wave, float* parts) {
+    const SpanAnew anew = span_anew();
+    const SpanKernel& a = anew.a;
+    const int item = a.row_blocks > 1 ? xcd_remap(anew.wg, gridDim.x) : anew.wg, list = item / a.splits, split = item - list * a.splits;
+    const int bh = list / a.row_blocks, b = bh / a.Hk, hk = bh - b * a.Hk, R = a.Lq * a.G, r0 = (list - bh * a.row_blocks) * kSpanRows;
+    const SpanSeq seq = span_seq(a, b);
+    const SpanTiles tiles = span_tiles(a, seq, r0 / a.G, min(min(r0 + kSpanRows - 1, R - 1) / a.G, seq.count - 1), kRowKeys);
+    const int per = (tiles.count + a.splits - 1) / a.splits, first = split * per + wave, last = min(split * per + per, tiles.count);
+    const int lane = lane_id();
+    for (; rows; rows &= rows - 1) {
+        const int j = __builtin_ctz(rows), row = r0 + j, token = min(row / a.G, seq.count - 1), head = hk * a.G + row % a.G;
+        const int hi = span_hi(a, seq, token), lo = span_lo(a, hi);
+        const SpanAgain x = span_again<ET, PAGED, kRowKeys>(a, b, hk, a.q + b * a.qb + head * a.qh + token * a.ql, hi, lo,
+                                                            first < last ? (last - first + a.waves - 1) / a.waves : 0,
+                                                            [&](int i) { return tiles.at(first + i * a.waves); });
+        float* const o = parts + j * (D + 4);
+#pragma unroll
+        for (int c = 0; c < 3; ++c)
+            if (lane + 64 * c < D) o[lane + 64 * c] = x.o[c];
+        if (lane == 0) {
+            o[D] = x.m;
+            o[D + 1] = x.l;
+        }
+    }
+}
+
 template <int ET, int D, bool PAGED>
 __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel(const SpanKernel a) {
     using G = SpanRow<D, PAGED>;
@@ -100,7 +128,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
 
     // pages: of this wave's tiles 64 k .. 64 k + 63, one a lane
     [[maybe_unused]] int pages = 0;
-    [[maybe_unused]] float kss = 0.0f, vss = 0.0f;
+    [[maybe_unused]] float kss = 0.0f, vss = 0.0f;   // of K: times a.c
     auto look_up = [&](int i) __attribute__((always_inline)) {
         if constexpr (PAGED) {
             const int j = min(i + lane, mine - 1);
@@ -108,7 +136,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             const bool there = page >= 0 && page < a.pages;
             const size_t at = (size_t)(there ? page : 0) * a.Hk + hk;
             pages = there ? page : -1;
-            kss = a.ks[at];
+            kss = __builtin_amdgcn_fmed3f(a.c * a.ks[at], __FLT_MIN__, __FLT_MAX__);   // (zero and infinities times it stay that)
             vss = a.vs[at];
         }
     };
@@ -153,7 +181,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
     };
 
     f32x16 acc[DN];
-    float m = kSpanNone, l = 0.0f;
+    float m = kSpanNone, l = 0.0f, worst = 0.0f;
     int spoiled = 0;
 #pragma unroll
     for (int n = 0; n < DN; ++n)
@@ -258,6 +286,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
                 for (int r = 0; r < 16; ++r) acc[n][r] *= alpha;
             l *= alpha;
             m = m_new;
+            worst = span_worst(worst, m);
         }
         float p[16];
 #pragma unroll
@@ -319,7 +348,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             }
             const int t = tile_of(i);
             if (PAGED && slot_page[slot] < 0) return;
-            const float ct = fmaxf(PAGED ? a.c * slot_ks[slot] : a.c, __FLT_MIN__);   // (minus infinity times it stays that)
+            const float ct = PAGED ? slot_ks[slot] : a.c;
             if (run.all(t * TK, TK)) use(whole_c, buf0 + slot * G::kBufBytes, t * TK, ct, slot_vs[slot]);
             else use(end_c, buf0 + slot * G::kBufBytes, t * TK, ct, slot_vs[slot]);
         });
@@ -357,6 +386,8 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
             o[D + 1] = l;
         }
     }
+    if (const uint32_t again = (uint32_t)__ballot(span_far(worst, m) && r0 + l32 < R); __builtin_expect(again != 0, 0))
+        span_row_again<ET, D, PAGED>(again, wave, parts + wave * kSpanRows * kO);
     __syncthreads();
     const size_t rows = (size_t)a.B * a.Hk * R;
     for (int z = tid; z < min(R - r0, kSpanRows) * (D / 4); z += 64 * waves) {

@@ -11,7 +11,7 @@ constexpr int kSpanRows = 32;          // rows of a block of attn_span_row.h
 // Rows of a block of the tiled kernel for heads of D (a multiple of 16).  Wide heads have no registers for the codes of
 // pages beside 128 rows.
 constexpr int span_block(int D, bool paged) { return D > (paged ? 96 : 128) ? 256 : 128; }
-constexpr float kSpanNone = -1e30f;    // the exponent's reference before the first key
+constexpr float kSpanNone = -__FLT_MAX__;   // the exponent's reference before the first key: no finite score is below it
 
 struct SpanKernel {
     const uint16_t* q;
@@ -31,7 +31,7 @@ struct SpanKernel {
     int row_blocks, splits;    // blocks of a key head's rows, parts of their keys
     int part_tiles, waves;     // attn_span_row.h: the most tiles of a part, waves of a workgroup
     uint32_t per_wave;         // 2^32 / waves, rounded up
-    float c;                   // |scale| log2(e); with scale 0, 1 and Q is taken for zeros
+    float c;                   // |scale| log2(e), from __FLT_MIN__ to __FLT_MAX__; with scale 0, 1 and Q is taken for zeros
     int neg;                   // scale < 0
     int zero;                  // scale = 0
 };
@@ -72,6 +72,19 @@ __device__ __forceinline__ SpanTiles span_tiles(const SpanKernel& a, const SpanS
     t.from = max(lo / tk, t.first);
     t.count = t.first + max(0, (hi + tk - 1) / tk - t.from);
     return t;
+}
+
+// The kernel's arguments and its workgroup's number, read anew: what a rare path at a kernel's end derives from them
+// takes no registers before it.
+struct SpanAnew {
+    SpanKernel a;
+    int wg;
+};
+__device__ __forceinline__ SpanAnew span_anew() {
+    const __attribute__((address_space(4))) void* p = (const __attribute__((address_space(4))) void*)__builtin_amdgcn_kernarg_segment_ptr();
+    int wg = blockIdx.x;
+    asm volatile("" : "+s"(p), "+s"(wg));
+    return SpanAnew{*(const SpanKernel*)p, wg};
 }
 
 // What every query of a run of tokens sees of a tile.
