@@ -364,8 +364,10 @@ int sdattn_cache_read(const void *k_pages, const void *v_pages, const float *k_s
  *   hi = min(n, (floor(p / frame) + 1) * frame), or n with frame = 0;  lo = hi - window, or 0 with window = 0
  * it sees key j where j < hi, and j >= lo or j < sinks: everything up to the end of its frame of `frame`
  * tokens (1: up to itself; 0: the whole sequence), of that the last `window` keys (0: all) and
- * the first `sinks`.  Keys that it does not see have no influence, whatever their values; of those that it
- * sees, a value of V that is infinite or no number makes that of its own column, one of K a row of no numbers.
+ * the first `sinks`.  Keys that it does not see have no influence, whatever their values.  Of those that it sees, a value of V
+ * that is infinite or no number makes that of its own column (no number where the key's weight has vanished).  A key
+ * whose product with the query is minus infinity has no weight, and a row that sees none but such is zeros; one whose product
+ * is plus infinity or no number makes the row one of no numbers.
  *
  *   q, out  token rows of H heads of D values in `x_layout` and `y_layout`, [B, Lq tokens]; rows from
  *           counts[b] on are left as they were

@@ -362,6 +362,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
     [[maybe_unused]] const char* Vb = nullptr;
     [[maybe_unused]] const uint32_t row_bytes = (uint32_t)a.kl * 2;
     [[maybe_unused]] uint32_t copy_off[kCopies];
+    [[maybe_unused]] bool copy_k[kCopies];     // a chunk of K, too (past D its values meet zeros of Q: they are zeros)
     // pages: pieces of 16 codes over the threads
     constexpr int kPieces = (4 * DP + G::kThreads - 1) / G::kThreads;
     [[maybe_unused]] u32x4 kraw[kPieces], vraw[kPieces];
@@ -383,9 +384,15 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
 #pragma unroll
         for (int p = 0; p < kCopies; ++p) {
             const int q = (wave + p * NW) * 64 + lane, r = q / KC;
-            int c = (q - r * KC) ^ G::swap(r);
-            if (DP != D) c = min(c, D / 8 - 1);
-            copy_off[p] = (uint32_t)r * row_bytes + c * 16;
+            const int c = (q - r * KC) ^ G::swap(r);
+            copy_k[p] = c < D / 8;
+            copy_off[p] = (uint32_t)r * row_bytes + min(c, D / 8 - 1) * 16;
+        }
+        if (DP != D) {
+            for (int z = tid; z < NKB * TK; z += G::kThreads) {
+                const int r = z % TK;
+                *(u32x4*)(smem + z / TK * G::kTileBytes + (r * KC + ((KC - 1) ^ G::swap(r))) * 16) = u32x4{0u, 0u, 0u, 0u};
+            }
         }
     }
     if (tid < 4) bad[tid] = 0;
@@ -436,7 +443,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
     };
     // A tile of K or of V, from `from` (its batch item's and head's, or the pages), into buffer buf; pages: into
     // registers, as codes.
-    auto load = [&](const Tile& x, const char* from, u32x4 (&raw)[kPieces], int buf) __attribute__((always_inline)) {
+    auto load = [&](const Tile& x, const char* from, u32x4 (&raw)[kPieces], int buf, bool k) __attribute__((always_inline)) {
         if constexpr (PAGED) {
             const char* const at = from + ((size_t)x.page * a.Hk + hk) * TK * D;
 #pragma unroll
@@ -445,22 +452,26 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
         } else {
             const char* const at = from + (long long)x.t * TK * row_bytes;
             const int last = seq.n - 1 - x.t * TK;   // keys past the last one repeat it
+            auto copy = [&](auto some) __attribute__((always_inline)) {
 #pragma unroll
-            for (int p = 0; p < kCopies; ++p) {
-                const int ci = wave + p * NW;
-                if (ci < KC) {
-                    uint32_t off = copy_off[p];
-                    if (last < TK - 1) {
-                        const int r = (ci * 64 + lane) / KC;
-                        if (r > last) off -= (uint32_t)(r - last) * row_bytes;
+                for (int p = 0; p < kCopies; ++p) {
+                    const int ci = wave + p * NW;
+                    if (ci < KC) {
+                        uint32_t off = copy_off[p];
+                        if (last < TK - 1) {
+                            const int r = (ci * 64 + lane) / KC;
+                            if (r > last) off -= (uint32_t)(r - last) * row_bytes;
+                        }
+                        if (!decltype(some)::value || copy_k[p]) copy16_to_lds(at, off, lds0 + buf * G::kTileBytes + ci * 1024);
                     }
-                    copy16_to_lds(at, off, lds0 + buf * G::kTileBytes + ci * 1024);
                 }
-            }
+            };
+            if (k && D != DP) copy(std::true_type{});
+            else copy(std::false_type{});
         }
     };
-    auto load_k = [&](const Tile& x, int buf) __attribute__((always_inline)) { load(x, PAGED ? a.k : Kb, kraw, buf); };
-    auto load_v = [&](const Tile& x, int buf) __attribute__((always_inline)) { load(x, PAGED ? a.v : Vb, vraw, NKB + buf); };
+    auto load_k = [&](const Tile& x, int buf) __attribute__((always_inline)) { load(x, PAGED ? a.k : Kb, kraw, buf, true); };
+    auto load_v = [&](const Tile& x, int buf) __attribute__((always_inline)) { load(x, PAGED ? a.v : Vb, vraw, NKB + buf, false); };
     // pages: the codes read by load as 16-bit values in buffer buf, V's times its scale
     auto store_k = [&](int buf) __attribute__((always_inline)) {
         if constexpr (PAGED) {

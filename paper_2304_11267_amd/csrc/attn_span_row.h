@@ -194,7 +194,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
 #pragma unroll
     for (int s = 0; s < DK; ++s) {
         const int d0 = 16 * s + 8 * half;
-        k_off[s] = G::at(l32, d0 < D ? d0 : 0);   // (past D: any values, for Q's zeros; but no infinite ones)
+        k_off[s] = G::at(l32, d0 < D ? d0 : 0);   // (past D: any values, for Q's zeros; codes are no number only where column 0 is)
     }
     {
         const int g = lane >> 4, e = lane & 15;
@@ -230,6 +230,7 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
                 w = decode8<ET>(c[0], c[1], 1.0f);
             } else {
                 w = *(const u32x4*)(kt + k_off[s]);
+                if (16 * s + 16 > D && half) w = u32x4{0u, 0u, 0u, 0u};   // (Q's zeros there may meet an infinity of a seen key)
             }
             st = mfma32x32x16<ET>(w, qreg[s], st);
         }
