@@ -218,8 +218,7 @@ hipError_t launch_span(const SpanArgs& s) {
     a.frame = s.frame, a.window = s.window, a.sinks = s.sinks;
     a.row_blocks = p.row_blocks, a.splits = p.splits, a.part_tiles = p.part_tiles;
     a.zero = s.scale == 0.0f, a.neg = s.scale < 0;
-    // (zero times it stays that, and minus infinity too)
-    a.c = a.zero ? 1.0f : fmaxf(fminf((a.neg ? -s.scale : s.scale) * kLog2e, __FLT_MAX__), __FLT_MIN__);
+    a.c = a.zero ? 1.0f : fminf((a.neg ? -s.scale : s.scale) * kLog2e, __FLT_MAX__);   // (zero times it stays that)
     const hipStream_t stream = (hipStream_t)s.stream;
     const bool f16 = s.dtype == kF16;
     hipError_t r;

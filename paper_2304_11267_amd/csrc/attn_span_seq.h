@@ -31,7 +31,7 @@ struct SpanKernel {
     int row_blocks, splits;    // blocks of a key head's rows, parts of their keys
     int part_tiles, waves;     // attn_span_row.h: the most tiles of a part, waves of a workgroup
     uint32_t per_wave;         // 2^32 / waves, rounded up
-    float c;                   // |scale| log2(e), from __FLT_MIN__ to __FLT_MAX__; with scale 0, 1 and Q is taken for zeros
+    float c;                   // |scale| log2(e), finite and not 0; with scale 0, 1 and Q is taken for zeros
     int neg;                   // scale < 0
     int zero;                  // scale = 0
 };

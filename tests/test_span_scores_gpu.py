@@ -124,3 +124,13 @@ def test_large_scales(Lq, form):
         q.zero_()
     for scale in (3e38, -3e38, 1e20):
         FORMS[form](B, H, Hk, Lq, 60 if Lq < 250 else 0, 64, "mixed", "bf16", scale=scale, tweak=zero)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("Lq", [1, 40, 250])
+def test_small_scales(Lq, form):
+    """A scale among the subnormals, of products of up to 2^127."""
+    B, H, Hk = sizes.LARGE[:3] if Lq == 250 else (2, 4, 2)
+    for D in (40, 128):
+        for scale in (2.0 ** -127.5, -2.0 ** -127.5):
+            FORMS[form](B, H, Hk, Lq, 60 if Lq < 250 else 0, D, "mixed", "bf16", scale=scale, q_exp=72 if D == 40 else 70)
