@@ -22,11 +22,14 @@ namespace sdattn {
 namespace {
 
 constexpr int kSpanTile = 64;          // keys of a tile: a page of the cache
-// The exponent's reference m is moved when a weight would pass 2^kSpanLimit, to kSpanBias
-// below the largest score: weights near 2^8 keep fp16's small ones above its subnormals' end,
-// and few tiles move it (fp16 holds values below 2^16).
-constexpr float kSpanBias = 8.0f;
-constexpr float kSpanLimit = 15.0f;
+// The exponent's reference m is moved when a weight would pass 2^span_limit, to span_bias
+// below the largest score, 7 octaves that few tiles move it in.  fp16: weights near 2^8 keep the small ones above its
+// subnormals' end (it holds values below 2^16).  bf16, which has 32 bits' range: below 2^-17, so that the sums of values at that
+// range's end over 2^17 keys stay within it.
+template <int ET>
+constexpr float span_bias = ET == kF16 ? 8.0f : -24.0f;
+template <int ET>
+constexpr float span_limit = span_bias<ET> + 7.0f;
 // c s - m is one operation, exact in c s, where m came from a c s that was rounded.  Up to 2^23 that is a quarter of an octave
 // of a weight at most; from 2^28 on a row's largest weight would be anything from 0 to infinity.  Rows whose m has
 // been past 2^23 are computed again at the end (span_again); the largest |m| is noted where m is moved.  (A row whose m is
@@ -215,7 +218,7 @@ __device__ __forceinline__ SpanAgain span_again(const SpanKernel& a, int b, int 
 // which do not depend on each other, a few operations of the vector unit behind each matrix product, in the order
 // written here (sched_barrier keeps it: a wave issues in order, and a run of either leaves the other unit
 // to the SIMD's other wave alone).  An operand of K or V is read from LDS again, for the next step,
-// behind the product that it has fed.  m is moved to a sub-tile's maximum where a weight would pass 2^15.
+// behind the product that it has fed.  m is moved with a sub-tile's maximum where a weight would pass its limit.
 //
 // The matrix core bounds it past D = 96, the vector unit beside it below: 17550 tokens, 16 heads of 128, windows of four
 // frames of 1350 and the first: 890 to 930 us by the card, 880 to 920 TFLOP/s of the visible keys, where a library's product
@@ -579,7 +582,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
         }
         p = fmaxf(fmaxf(p, st[x][14]), st[x][15]);
         const float mx = half_max(fmaxf(p, q)) * ct;
-        const float m_new = mx - m > kSpanLimit ? mx - kSpanBias : m;
+        const float m_new = mx - m > span_limit<ET> ? mx - span_bias<ET> : m;
         alpha = fast_exp2(m - m_new);
         if (!G::kOnes) l *= alpha;
         m = m_new;

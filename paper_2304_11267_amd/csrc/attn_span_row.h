@@ -278,8 +278,8 @@ __global__ __launch_bounds__((SpanRow<D, PAGED>::kThreads)) void span_row_kernel
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, st[r]);
         mx = half_max(mx) * ct;
-        if (__any(mx - m > kSpanLimit)) {
-            const float m_new = fmaxf(m, mx - kSpanBias);
+        if (__any(mx - m > span_limit<ET>)) {
+            const float m_new = fmaxf(m, mx - span_bias<ET>);
             const float alpha = fast_exp2(m - m_new);
 #pragma unroll
             for (int n = 0; n < DN; ++n)
