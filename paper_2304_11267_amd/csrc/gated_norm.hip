@@ -33,8 +33,7 @@ struct GatedKernel {
     uint16_t* y;
     int L, C, M;
     int per_group;         // tokens of a modulation group
-    int groups;            // of a batch item; 0 rows apart for batch items that share them
-    int mod_batch;         // modulation rows from one batch item to the next
+    int mod_batch;         // modulation rows from one batch item to the next; 0 where all share them
     long long sg, ss, st;  // elements from one modulation row to the next: gate, scale, shift
     int post, pre;
     float skip, eps, inv_c;
@@ -253,7 +252,7 @@ hipError_t gated_pick(const GatedKernel& a, void* stream) {
 hipError_t launch_gated_norm(const GatedNormArgs& n) {
     GatedKernel a{n.x, (const uint16_t*)n.r, (const uint16_t*)n.gate, (const uint16_t*)n.scale, (const uint16_t*)n.shift,
                   (const uint16_t*)n.gamma_r, (const uint16_t*)n.gamma, (const uint16_t*)n.beta, n.h, (uint16_t*)n.y,
-                  n.L, n.C, n.B * n.L, n.L / n.groups, n.groups, n.mod_batches == 1 ? 0 : n.groups,
+                  n.L, n.C, n.B * n.L, n.L / n.groups, n.mod_batches == 1 ? 0 : n.groups,
                   n.gate_stride, n.scale_stride, n.shift_stride, n.norm_r, n.norm, n.skip, n.eps, 1.0f / (float)n.C};
     if (n.dtype == kF16) return n.wide ? gated_pick<kF16, true>(a, n.stream) : gated_pick<kF16, false>(a, n.stream);
     return n.wide ? gated_pick<kBF16, true>(a, n.stream) : gated_pick<kBF16, false>(a, n.stream);
