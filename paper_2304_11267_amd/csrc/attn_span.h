@@ -246,6 +246,7 @@ struct SpanTile {
     // With columns to spare in the last 32 rows of O^T, one of them is of ones: the row sum of the weights comes out
     // of the matrix core.  Its lanes read a constant block: a one and zeros, where 16 rows of a tile begin.
     static constexpr bool kOnes = DP % 32 == 16;
+    static_assert(!kOnes || kSwap == 2, "the last 32 columns lie 4 n chunks on, whatever the swap");
     static constexpr int kWords = (kBufsK + 2) * kTileBytes;   // after K and V: four words of keys,
     static constexpr int kConst = kWords + 32;                 // and the constant block
     static constexpr int kLdsBytes = kConst + (kOnes ? 3 * 16 * DP * 2 + 16 : 0);
@@ -554,7 +555,7 @@ __global__ __launch_bounds__((SpanTile<DP, NW>::kThreads), span_waves(DP, PAGED)
     };
     auto read_v = [&](int buf, int sub, int h) __attribute__((always_inline)) {
         const int u = h / DN, n = h % DN, rows = (32 * sub + 16 * u) * KC * 16;
-        const bool ones = G::kOnes && n == DN - 1;   // (kXor is 2 or 4 then: 4 n is added)
+        const bool ones = G::kOnes && n == DN - 1;   // (kXor is 2 then: 4 n is added)
         const char* const xp = smem + (ones ? (buf & c_mask) + c_at : chunk_on(buf + v_at, 4 * n)) + rows;
         const char* const yp = smem + (ones ? (buf & c_mask) + c_up : chunk_on(buf + v_up, 4 * n)) + rows;
         const u32x2 x = lds_read_tr(xp), y = lds_read_tr(yp);
