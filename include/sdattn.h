@@ -299,7 +299,8 @@ int sdattn_sparse_forward(const void *q, const void *k, const void *v, const voi
  *             video); mod_batches = B, or 1 where all batch items share them
  *   gamma_r, gamma, beta  [C] of `dtype` or NULL (for 1, 1, 0)
  *
- * y is computed from h before its rounding; fp32 arithmetic, each output rounded once.
+ * y is computed from h before its rounding; fp32 arithmetic, each output rounded once (sums of squares are within fp32 for values
+ * up to 2^56).
  * One launch on `stream`.  Requirements: C % 8 == 0, C <= 16384; L % groups == 0; skip finite; eps
  * finite and >= 0; strides >= 0 and multiples of 8; every pointer 16-byte aligned; no output may overlap
  * another argument otherwise; no launch of 2^32 threads or more (SDATTN_ERR_UNSUPPORTED,
@@ -329,7 +330,8 @@ int sdattn_gated_norm(const void *x, const void *r, const void *gate, const void
  * sdattn_cache_write puts tokens l < counts[b] of k and v at positions starts[b] + l, which
  * then end their sequence: what a page had behind them is no longer part of it.  The scale is 2^e with the
  * least e in [-100, 120] for which no value of the page is past 448 * 2^e, and never less than
- * the scale of the tokens before starts[b] that the page keeps, which are coded anew if it grows.
+ * the scale of the tokens before starts[b] that the page keeps, which are coded anew if it grows (0 for a page that holds
+ * none, where a sequence begins inside of it).
  * Codes are rounded to nearest even: a value is off by at most 2^-4 of itself, or 2^(e - 10)
  * (once more for each time that its page is coded anew, where that takes it below 2^(e - 6)).  Finite values past 1.875 * 2^15
  * (fp16) or 1.875 * 2^127 (bf16) are held as that; NaN and infinities come back as NaN and do not count for
@@ -381,7 +383,8 @@ int sdattn_cache_read(const void *k_pages, const void *v_pages, const float *k_s
  * sdattn_window_forward reads k, v: token rows of Hk heads and Lk tokens in `x_layout`, `dtype`;
  * starts may be NULL (for Lk - Lq: the queries are the last tokens), and so may counts (for Lq).
  *
- * Weights are rounded to `dtype` before they meet v, as in sdattn_forward.  One launch on `stream`, or two.
+ * Weights are rounded to `dtype` before they meet v, as in sdattn_forward; sums are fp32 (of bf16 values at their type's end: over
+ * 2^17 keys).  One launch on `stream`, or two.
  * Requirements: 32 <= D <= 160 with D % 8 == 0; Hk divides H, H <= 65536; Lq, Lk, 64 slots and Lq H / Hk at
  * most 2^30; frame, window, sinks >= 0; finite scale; q, k, v, pages, out and workspace 16-byte
  * aligned, the rest 4-byte; out and the workspace must not overlap each other or an input.
