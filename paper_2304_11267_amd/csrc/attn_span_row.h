@@ -9,9 +9,9 @@
 // into 16-bit values on their way there (4 instructions), V's through the transposing read of bytes
 // (ds_read_b64_tr_b8).  Rows past R are columns of the products that nobody looks at: the matrix core has
 // time for them.  At the end the waves' parts are joined through LDS.  One token of eight sequences of 11000 to 32768
-// keys in pages, 32 heads of 128 over 8: 78 us and a join of 4.7, 4.8 TB/s where a copy reaches 5.14; a token of 16
-// windows of 1088 16-bit keys, D = 64, 4 key heads: 8.3, a launch and a chain of five tiles a wave on 64
-// CUs; two prompts of 77 in pages, D = 40: 5.1.
+// keys in pages, 32 heads of 128 over 8: 79 us and a join of 4.8, 4.8 TB/s where a copy reaches 5.14; a token of 16
+// windows of 1088 16-bit keys, D = 64, 4 key heads: 8.6, a launch and a chain of five tiles a wave on 64
+// CUs; two prompts of 77 in pages, D = 40: 5.2.
 #pragma once
 
 #include "attn_span.h"
